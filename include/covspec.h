@@ -63,7 +63,9 @@ enum {
 };
 
 enum { COVSPEC_FP32 = 0, COVSPEC_BF16 = 1,
-       COVSPEC_FP16 = 2 /* logits of covspec_verify and covspec_draft_gate only */ };
+       COVSPEC_FP16 = 2, /* logits (covspec_verify, covspec_draft_gate, covspec_adjust_logits), cached tokens and their attention */
+       COVSPEC_INT8 = 3, /* what a cache holds only (covspec_cache_write, covspec_cache_read, covspec_attend) */
+       COVSPEC_E4M3 = 4  /* the same: 8-bit floating point, 4 exponent bits, largest value 448 */ };
 
 /* Query-relevance definition.
  *   COSINE_MAX   : S^query_i = max_j cos(e(v_i), e(q_j))  (paper Sec. III-A.1, query-aware score).
@@ -408,6 +410,140 @@ size_t covspec_draft_workspace_size(const covspec_draft_params* p);
 int covspec_draft_gate(const covspec_draft_params* p, const void* z_draft, const int32_t* tokens,
                        float* margin_out, int32_t* gate_out, int32_t* cand_out,
                        void* workspace, size_t workspace_bytes, covspec_stream_t stream);
+
+/*
+ * Paged cache of keys and values, as the models on both sides of a drafting round keep it (paper Sec. II-A: the
+ * draft model extends y token by token, the target evaluates the drafted segment in one parallel pass over its
+ * cached context).  The paper says nothing of its layout; this one is the library's own.
+ *
+ * The pool (caller-owned, DEVICE):
+ *   k_cache, v_cache [n_pages, n_kv_heads, page_size, head_dim] cache_dtype: `dtype` itself, or 8-bit codes
+ *   k_scale, v_scale [n_pages, n_kv_heads, page_size] fp32, one per token and head; NULL unless the cache is 8-bit
+ * A batch of n_seq sequences (DEVICE, int32):
+ *   start  [n_seq + 1]  rows start[s] .. start[s+1] - 1 of the packed tensors belong to sequence s; ascending,
+ *                       equal neighbours = no rows; rows at or beyond start[n_seq] are padding
+ *   length [n_seq]      tokens of sequence s, the n = start[s+1] - start[s] rows of the call included: row i of
+ *                       the sequence is its position length[s] - n + i
+ *   pages  [n_seq, max_pages]  position j lies in page pages[s, j / page_size], at place j % page_size of it
+ * The same three arrays describe the tokens that are written, the rows of queries behind them and what is read
+ * back.  Sequences may share pages.  Tokens that a verification rejected need no undoing: the next round's
+ * lengths leave them out and its tokens overwrite them.
+ * A position below zero, beyond the table (max_pages * page_size) or on a page outside 0 .. n_pages - 1 does not exist:
+ * nothing is written for it, it reads as zeros, and no query sees it.  Nothing outside the given arrays is touched
+ * whatever they hold.
+ *
+ * covspec_cache_write: rows of k and v into the cache.  Row (token, head) in 8 bits, all in fp32 with each
+ * operation rounded on its own:
+ *   amax = max |x|, Q = 127 (INT8) or 448 (E4M3);  scale = amax / Q;  code = x * (Q / amax) to the nearest, ties to
+ *   even (to the nearest representable value for E4M3).  amax < 2^-100: all codes and the scale are zero.  A row
+ *   with an infinity or NaN gets the scale NaN and zero codes, so that it reads back as NaN.
+ * With cache_dtype == dtype rows are copied bit for bit.
+ * Two rows of one call for the same place: one of them is kept, which one is not said.
+ * covspec_cache_read: code * scale (fp32, rounded once to `dtype`), or the bits, of the positions of the batch.
+ *   k, v        [n_tokens, n_kv_heads, head_dim] dtype, rows `row_pitch` elements apart (0: dense), so that they may
+ *               be columns of a wider tensor, e.g. of a fused projection; 16-byte aligned
+ *   k_out, v_out  the same layout; rows of the batch are written, padding rows are left as they were
+ * dtype: COVSPEC_BF16 or COVSPEC_FP16.  Limits: head_dim 64, 96 or 128; page_size a power of two from 16 to 1024;
+ * row_pitch a multiple of 8, not below n_kv_heads * head_dim; n_tokens * n_kv_heads and max_pages * page_size
+ * below 2^30; pool places (n_pages * n_kv_heads * page_size) below 2^40: else COVSPEC_INVALID_ARG (dtype pairs, non-positive
+ * sizes, misaligned or missing pointers, pitch) or COVSPEC_UNSUPPORTED.  No workspace; enqueues one kernel on
+ * `stream`, does not synchronise, allocates nothing.
+ */
+typedef struct covspec_cache_params {
+  int32_t n_seq;        /* S                                                     */
+  int32_t n_tokens;     /* T: rows of the packed tensors, padding included        */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* D: 64, 96, 128                                        */
+  int32_t page_size;    /* tokens per page                                       */
+  int32_t n_pages;      /* pages of the pool                                     */
+  int32_t max_pages;    /* width of the page table                               */
+  int32_t dtype;        /* COVSPEC_BF16 / COVSPEC_FP16: k, v, q, out             */
+  int32_t cache_dtype;  /* == dtype, COVSPEC_INT8 or COVSPEC_E4M3                */
+  int32_t reserved;     /* 0                                                     */
+  int64_t row_pitch;    /* elements from a token's row of k (v) to the next; 0 = n_kv_heads * head_dim */
+} covspec_cache_params;
+
+int covspec_cache_write(const covspec_cache_params* p, const void* k, const void* v, const int32_t* start,
+                        const int32_t* length, const int32_t* pages, void* k_cache, void* v_cache, float* k_scale,
+                        float* v_scale, covspec_stream_t stream);
+int covspec_cache_read(const covspec_cache_params* p, const void* k_cache, const void* v_cache, const float* k_scale,
+                       const float* v_scale, const int32_t* start, const int32_t* length, const int32_t* pages,
+                       void* k_out, void* v_out, covspec_stream_t stream);
+
+/*
+ * covspec_attend: attention of a batch's rows over its cache (which holds the rows' own keys and values already),
+ * for prompts, drafted segments under verification and single tokens alike (paper Sec. II-A, the target's parallel
+ * pass; NOT defined there beyond "the target evaluates").  For row i of sequence s, position pos, and head h with
+ * key head g = h / (n_heads / n_kv_heads):
+ *   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale * q . k_j - m),  over the positions j it sees:
+ *   j <= pos, and j > pos - window if window > 0; or, with `visible`, every position in front of the chunk and
+ *   of the chunk itself those rows b whose bit b of visible[row] is set (a tree of drafted tokens, paper Sec. III-C: row
+ *   0 is bit 0; rows from the 65th on are then seen by none; a row sees itself only if its own bit says so).
+ *   A row that sees nothing gives zeros and the log-sum -infinity.  What unseen positions hold, NaN included, has no effect.
+ *   q     [n_tokens, n_heads, head_dim] dtype, rows q_pitch elements apart (0: dense), 16-byte aligned
+ *   visible [n_tokens] int64 bits, or NULL (with window == 0 only)
+ *   out   [n_tokens, n_heads, head_dim] dtype, rows out_pitch elements apart (0: dense); padding rows stay as they were
+ *   lse_out [n_tokens, n_heads] fp32 log sum_j exp(scale * q . k_j), or NULL
+ * max_len (HOST) bounds the lengths: it sizes the grid and the workspace; positions at or beyond it are not seen.
+ * Products are taken of 16-bit values with fp32 sums (8-bit codes are exact in 16 bits; their scales enter in fp32),
+ * softmax statistics are fp32, p is rounded to 16 bits for its product with v.  The same call gives the same bits.
+ * Limits: those of the cache (its row_pitch is not used); n_heads a multiple of n_kv_heads, at most 64 times it;
+ * n_tokens * n_heads below 2^30; max_len from 1 to max_pages * page_size; window >= 0; scale finite.  Workspace:
+ * covspec_attend_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on `stream`,
+ * does not synchronise, allocates nothing; the launches depend on the parameters alone, so that a captured graph
+ * serves other lengths and pages of the same parameters.
+ */
+typedef struct covspec_attend_params {
+  covspec_cache_params cache;
+  int32_t n_heads;      /* query heads                                           */
+  int32_t max_len;      /* upper bound of the lengths                            */
+  int32_t window;       /* 0: none                                               */
+  float scale;          /* of q . k                                              */
+  int64_t q_pitch;      /* 0 = n_heads * head_dim                                */
+  int64_t out_pitch;    /* 0 = n_heads * head_dim                                */
+} covspec_attend_params;
+
+size_t covspec_attend_workspace_size(const covspec_attend_params* p);
+int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t* start, const int32_t* length,
+                   const int32_t* pages, const void* k_cache, const void* v_cache, const float* k_scale,
+                   const float* v_scale, const int64_t* visible, void* out, float* lse_out, void* workspace,
+                   size_t workspace_bytes, covspec_stream_t stream);
+
+/*
+ * covspec_adjust_logits: what a sampler does to the logits in front of covspec_verify and covspec_draft_gate:
+ * penalties for words that were said, biases, temperature and a grammar's mask.  NOT in the paper (its softmax
+ * equations, Sec. II-A, take the logits as they are).  For sequence s, position tau and word w, in fp32 with each
+ * operation rounded on its own, x = z[s, tau, w]:
+ *   1. w in the history of s or among drafted[s, 0 .. tau-1]: x = x > 0 ? x * (1 / r) : x * r;
+ *   2. n = occurrences of w in the history behind its first prompt_len[s] words and among drafted[s, 0 .. tau-1]:
+ *      x = x - (f * n + (n > 0 ? c : 0));
+ *   3. x = x + bias of w, if s has one (of several entries for a word the last one counts);
+ *   4. x = x * (1 / T);
+ *   5. w not allowed: x = -infinity;
+ * with (r, c, f, T) = penalties[s] = repetition, presence, frequency, temperature; (1, 0, 0, 1) changes nothing.  A T that
+ * is not > 0 counts as 1.
+ * DEVICE pointers:
+ *   z, z_out  [n_seq, n_pos, vocab] dtype, 16-byte aligned; z_out may be z (not overlap it otherwise)
+ *   history   packed words, int32; history_start [n_seq + 1] int32 ascending; prompt_len [n_seq] int32 or NULL (0)
+ *   drafted   [n_seq, n_pos] int32 or NULL (no row sees another's word); its last column is not read
+ *   penalties [n_seq, 4] fp32
+ *   bias_start [n_seq + 1], bias_word int32, bias_value fp32, or all three NULL
+ *   allowed   [n_seq, n_pos, (vocab + 31) / 32] 32-bit words, bit w % 32 of word w / 32 set = w allowed; or NULL
+ * Words outside [0, vocab) are nobody's.  Limits as covspec_verify, with n_pos in the place of n_draft: n_pos <= 64,
+ * n_seq * n_pos <= 65535, vocab a multiple of 8 (bf16, fp16) or 4 (fp32).  No workspace; one launch on `stream`, does not
+ * synchronise, allocates nothing.
+ */
+typedef struct covspec_logits_params {
+  int32_t n_seq;    /* S                                                    */
+  int32_t n_pos;    /* L: positions per sequence                            */
+  int32_t vocab;    /* V                                                    */
+  int32_t dtype;    /* covspec_dtype of the logits                          */
+} covspec_logits_params;
+
+int covspec_adjust_logits(const covspec_logits_params* p, const void* z, const int32_t* history,
+                          const int32_t* history_start, const int32_t* prompt_len, const int32_t* drafted,
+                          const float* penalties, const int32_t* bias_start, const int32_t* bias_word,
+                          const float* bias_value, const uint32_t* allowed, void* z_out, covspec_stream_t stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* covspec_status_string(int status);

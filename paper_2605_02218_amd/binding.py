@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcovspec.so")
 
 FP32, BF16 = 0, 1
-FP16 = 2          # logits of verify / draft_gate only
+FP16 = 2          # logits, cached tokens and their attention
+INT8, E4M3 = 3, 4  # what a cache holds only
 REL_COSINE_MAX, REL_ATTN_SOFTMAX = 0, 1
 LR_ENERGY_TOPK, LR_GREEDY_RESIDUAL, LR_SCORE_TOPK, LR_RANDOM = 0, 1, 2, 3
 OK, INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED, HIP_ERROR = 0, 1, 2, 3, 4
@@ -25,7 +26,8 @@ EXPORTS = ("covspec_workspace_size", "covspec_resolve", "covspec_score", "covspe
            "covspec_reduce", "covspec_reduce_staged", "covspec_probe_launches", "covspec_status_string",
            "covspec_verify_workspace_size", "covspec_verify", "covspec_verify_static", "covspec_draft_fanout", "covspec_draft_workspace_size",
            "covspec_draft_gate", "covspec_last_error", "covspec_ragged_resolve", "covspec_ragged_workspace_size",
-           "covspec_reduce_ragged", "covspec_lowrank_path", "covspec_image_status", "covspec_set_wait_limit_us", "covspec_stream_workspace_size", "covspec_stream_step")
+           "covspec_reduce_ragged", "covspec_lowrank_path", "covspec_image_status", "covspec_set_wait_limit_us", "covspec_stream_workspace_size", "covspec_stream_step",
+           "covspec_cache_write", "covspec_cache_read", "covspec_attend_workspace_size", "covspec_attend", "covspec_adjust_logits")
 
 
 class CovspecParams(ctypes.Structure):
@@ -51,6 +53,20 @@ class CovspecRagged(ctypes.Structure):
 
 class CovspecStreamParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_frame", "d_model", "dtype", "frame_m", "keep_k", "rank_r")]
+
+
+class CovspecCacheParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "n_tokens", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "dtype", "cache_dtype",
+                                              "reserved")] + [("row_pitch", ctypes.c_int64)]
+
+
+class CovspecAttendParams(ctypes.Structure):
+    _fields_ = [("cache", CovspecCacheParams)] + [(n, ctypes.c_int32) for n in ("n_heads", "max_len", "window")] + [
+        ("scale", ctypes.c_float), ("q_pitch", ctypes.c_int64), ("out_pitch", ctypes.c_int64)]
+
+
+class CovspecLogitsParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "n_pos", "vocab", "dtype")]
 
 
 class CovspecError(RuntimeError):
@@ -126,6 +142,17 @@ def load_library() -> ctypes.CDLL:
     lib.covspec_stream_workspace_size.argtypes = [spp]
     lib.covspec_stream_step.restype = ctypes.c_int
     lib.covspec_stream_step.argtypes = [spp, ctypes.c_int32, ctypes.c_int32] + [vp] * 9 + [ctypes.POINTER(ctypes.c_int32), vp, ctypes.c_size_t, vp]
+    cpp, app, lpp = (ctypes.POINTER(t) for t in (CovspecCacheParams, CovspecAttendParams, CovspecLogitsParams))
+    lib.covspec_cache_write.restype = ctypes.c_int
+    lib.covspec_cache_write.argtypes = [cpp] + [vp] * 10
+    lib.covspec_cache_read.restype = ctypes.c_int
+    lib.covspec_cache_read.argtypes = [cpp] + [vp] * 10
+    lib.covspec_attend_workspace_size.restype = ctypes.c_size_t
+    lib.covspec_attend_workspace_size.argtypes = [app]
+    lib.covspec_attend.restype = ctypes.c_int
+    lib.covspec_attend.argtypes = [app] + [vp] * 12 + [ctypes.c_size_t, vp]
+    lib.covspec_adjust_logits.restype = ctypes.c_int
+    lib.covspec_adjust_logits.argtypes = [lpp] + [vp] * 12
     lib.covspec_last_error.restype = ctypes.c_char_p
     lib.covspec_last_error.argtypes = []
     _lib = lib
@@ -543,3 +570,194 @@ def stream_step(p: StreamParams, n_keep: int, id_base: int, X_frame, s_fused, st
     if st != OK:
         raise CovspecError(st, "covspec_stream_step")
     return nxt.value, (c if (want_c and n_keep + p.frame_m > p.keep_k) else None)
+
+
+@dataclass
+class CacheParams:
+    n_seq: int
+    n_tokens: int
+    n_kv_heads: int
+    head_dim: int
+    page_size: int
+    n_pages: int
+    max_pages: int
+    dtype: int = BF16
+    cache_dtype: int = BF16
+
+    def c_struct(self, row_pitch: int = 0) -> CovspecCacheParams:
+        return CovspecCacheParams(self.n_seq, self.n_tokens, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, self.max_pages, self.dtype,
+                                  self.cache_dtype, 0, row_pitch)
+
+
+def _cache_torch_dtype(dtype: int):
+    import torch
+    return {FP32: torch.float32, BF16: torch.bfloat16, FP16: torch.float16, INT8: torch.int8, E4M3: torch.float8_e4m3fn}[dtype]
+
+
+def _same_device(*tensors):
+    """Device of the tensors (None entries left out); the call's kernels run there, on that device's current stream."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ValueError("tensors must be on one device")
+    return next(iter(devices))
+
+
+def _expect(t, name: str, shape, dtype):
+    """Pointer of a contiguous device tensor, None for None; what the library cannot see (shapes, types) is checked here."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    return _ptr(t)
+
+
+def _rows(t, name: str, n: int, heads: int, dim: int, dtype):
+    """(pointer, pitch) of rows [n, heads, dim] that are dense but for the distance from one to the next."""
+    if t.dtype != dtype or tuple(t.shape) != (n, heads, dim):
+        raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (name, dtype, (n, heads, dim), t.dtype, tuple(t.shape)))
+    if not t.is_cuda or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError("%s must be a device tensor with dense rows" % name)
+    return t.data_ptr(), (t.stride(0) if n > 1 else heads * dim)
+
+
+def cache_alloc(p: CacheParams, device="cuda"):
+    """An empty pool: (k, v, k_scale, v_scale), codes [n_pages, n_kv_heads, page_size, head_dim]; scales None unless in 8 bits."""
+    import torch
+    shape = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim)
+    dt = _cache_torch_dtype(p.cache_dtype)
+    scales = (None, None) if p.cache_dtype == p.dtype else tuple(torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2))
+    return tuple(torch.empty(shape, dtype=dt, device=device) for _ in range(2)) + scales
+
+
+def _cache_ptrs(p: CacheParams, start, length, pages, cache):
+    import torch
+    k, v, ks, vs = cache
+    shape = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim)
+    dt = _cache_torch_dtype(p.cache_dtype)
+    batch = [_expect(start, "start", (p.n_seq + 1,), torch.int32), _expect(length, "length", (p.n_seq,), torch.int32),
+             _expect(pages, "pages", (p.n_seq, p.max_pages), torch.int32)]
+    pool = [_expect(k, "k_cache", shape, dt), _expect(v, "v_cache", shape, dt), _expect(ks, "k_scale", shape[:3], torch.float32),
+            _expect(vs, "v_scale", shape[:3], torch.float32)]
+    return batch, pool
+
+
+def cache_write(p: CacheParams, k, v, start, length, pages, cache):
+    """covspec_cache_write: rows k, v [T, Hkv, D] (columns of a wider tensor allowed, both with the same pitch) into `cache` (of cache_alloc)."""
+    import torch
+    dev = _same_device(k, v, start, length, pages, *cache)
+    dt = _cache_torch_dtype(p.dtype)
+    kp, pitch = _rows(k, "k", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
+    vp, pitch_v = _rows(v, "v", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
+    if pitch != pitch_v:
+        raise ValueError("k and v must have the same distance between rows")
+    batch, pool = _cache_ptrs(p, start, length, pages, cache)
+    cs = p.c_struct(pitch)
+    with torch.cuda.device(dev):
+        st = load_library().covspec_cache_write(ctypes.byref(cs), kp, vp, *batch, *pool, _stream())
+    if st != OK:
+        raise CovspecError(st, "covspec_cache_write")
+    return cache
+
+
+def cache_read(p: CacheParams, cache, start, length, pages, k_out=None, v_out=None):
+    """covspec_cache_read: (k, v) [T, Hkv, D]; padding rows of outputs allocated here are unspecified."""
+    import torch
+    dev = _same_device(start, length, pages, k_out, v_out, *cache)
+    dt = _cache_torch_dtype(p.dtype)
+    shape = (p.n_tokens, p.n_kv_heads, p.head_dim)
+    k_out = torch.empty(shape, dtype=dt, device=dev) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=dt, device=dev) if v_out is None else v_out
+    kp, pitch = _rows(k_out, "k_out", *shape, dt)
+    vp, pitch_v = _rows(v_out, "v_out", *shape, dt)
+    if pitch != pitch_v:
+        raise ValueError("k_out and v_out must have the same distance between rows")
+    batch, pool = _cache_ptrs(p, start, length, pages, cache)
+    cs = p.c_struct(pitch)
+    with torch.cuda.device(dev):
+        st = load_library().covspec_cache_read(ctypes.byref(cs), *pool, *batch, kp, vp, _stream())
+    if st != OK:
+        raise CovspecError(st, "covspec_cache_read")
+    return k_out, v_out
+
+
+@dataclass
+class AttendParams:
+    cache: CacheParams
+    n_heads: int
+    max_len: int
+    scale: float
+    window: int = 0
+
+    def c_struct(self, q_pitch: int = 0, out_pitch: int = 0) -> CovspecAttendParams:
+        return CovspecAttendParams(self.cache.c_struct(), self.n_heads, self.max_len, self.window, self.scale, q_pitch, out_pitch)
+
+
+def attend_workspace_size(p: AttendParams) -> int:
+    cs = p.c_struct()
+    return int(load_library().covspec_attend_workspace_size(ctypes.byref(cs)))
+
+
+def attend(p: AttendParams, q, start, length, pages, cache, visible=None, workspace=None, out=None, want_lse=False):
+    """covspec_attend: (out [T, heads, D], lse [T, heads] fp32 or None); padding rows of outputs allocated here are unspecified."""
+    import torch
+    c = p.cache
+    dev = _same_device(q, start, length, pages, visible, workspace, out, *cache)
+    dt = _cache_torch_dtype(c.dtype)
+    qp, q_pitch = _rows(q, "q", c.n_tokens, p.n_heads, c.head_dim, dt)
+    out = torch.empty(c.n_tokens, p.n_heads, c.head_dim, dtype=dt, device=dev) if out is None else out
+    op, out_pitch = _rows(out, "out", c.n_tokens, p.n_heads, c.head_dim, dt)
+    batch, pool = _cache_ptrs(c, start, length, pages, cache)
+    bits = _expect(visible, "visible", (c.n_tokens,), torch.int64)
+    if workspace is None:
+        n = attend_workspace_size(p)
+        if n == 0:
+            raise CovspecError(INVALID_ARG, "covspec_attend_workspace_size")
+        workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
+    lse = torch.empty(c.n_tokens, p.n_heads, dtype=torch.float32, device=dev) if want_lse else None
+    wp, wb = _ws_args(workspace)
+    cs = p.c_struct(q_pitch, out_pitch)
+    with torch.cuda.device(dev):
+        st = load_library().covspec_attend(ctypes.byref(cs), qp, *batch, *pool, bits, op, _ptr(lse), wp, wb, _stream())
+    if st != OK:
+        raise CovspecError(st, "covspec_attend")
+    return out, lse
+
+
+@dataclass
+class LogitsParams:
+    n_seq: int
+    n_pos: int
+    vocab: int
+    dtype: int = BF16
+
+    def c_struct(self) -> CovspecLogitsParams:
+        return CovspecLogitsParams(self.n_seq, self.n_pos, self.vocab, self.dtype)
+
+
+def adjust_logits(p: LogitsParams, z, history, history_start, penalties, prompt_len=None, drafted=None, bias=None, allowed=None, out=None):
+    """covspec_adjust_logits on z [S, L, V]: the adjusted logits, in `out` (which may be z) or a new tensor.  `bias`: (start [S + 1], word, value)."""
+    import torch
+    bias = (None, None, None) if bias is None else bias
+    dev = _same_device(z, history, history_start, penalties, prompt_len, drafted, allowed, out, *bias)
+    S, L, V = p.n_seq, p.n_pos, p.vocab
+    dt, i32 = _cache_torch_dtype(p.dtype), torch.int32
+    out = torch.empty_like(z) if out is None else out
+    n = bias[1].numel() if bias[1] is not None else 0
+    if history.dtype != i32 or (bias[1] is not None and bias[1].dtype != i32):
+        raise ValueError("words must be int32")
+    if history.numel() == 0:
+        history = history_start          # nothing is read of it
+    args = [_expect(z, "z", (S, L, V), dt), _ptr(history), _expect(history_start, "history_start", (S + 1,), i32),
+            _expect(prompt_len, "prompt_len", (S,), i32), _expect(drafted, "drafted", (S, L), i32),
+            _expect(penalties, "penalties", (S, 4), torch.float32)]
+    if n > 0:
+        args += [_expect(bias[0], "bias start", (S + 1,), i32), _ptr(bias[1]), _expect(bias[2], "bias values", (n,), torch.float32)]
+    else:
+        args += [None, None, None]
+    args += [_expect(allowed, "allowed", (S, L, (V + 31) // 32), i32), _expect(out, "out", (S, L, V), dt)]
+    cs = p.c_struct()
+    with torch.cuda.device(dev):
+        st = load_library().covspec_adjust_logits(ctypes.byref(cs), *args, _stream())
+    if st != OK:
+        raise CovspecError(st, "covspec_adjust_logits")
+    return out

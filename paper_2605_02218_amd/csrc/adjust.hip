@@ -1,0 +1,130 @@
+// What a sampler does to logits before they are verified: penalties for words that were said, biases, temperature, a grammar's mask.
+//
+// For a word with n occurrences in what the model has said, x = z * (said or asked ? (z > 0 ? 1 / r : r) : 1) - (f n + (n > 0 ? c : 0)) + bias,
+// times 1 / T, -infinity where the mask says so.  One workgroup takes a chunk of the vocabulary, a vector of words a thread, for all positions of a
+// sequence: the history is counted once in LDS (a word of it lands in one of the chunks), a thread then keeps the counts of its words in
+// registers, and from one position to the next only the drafted word between them is added.
+#include "vocab.h"
+
+namespace covspec {
+
+namespace {
+
+constexpr int AT = 512;
+
+template <int DT>
+__device__ __forceinline__ void store_logits(void* p, long i, const float (&x)[LogitVec<DT>::N]) {
+  u32x4_t w;
+  if constexpr (DT == DT_F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(x[e]);
+    *(u32x4_t*)((float*)p + i) = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (DT == DT_BF16) {
+        typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
+        w[e] = __builtin_bit_cast(uint32_t, (pair_t){(__bf16)x[2 * e], (__bf16)x[2 * e + 1]});
+      } else {
+        typedef _Float16 pair_t __attribute__((ext_vector_type(2)));
+        w[e] = __builtin_bit_cast(uint32_t, (pair_t){(_Float16)x[2 * e], (_Float16)x[2 * e + 1]});
+      }
+    }
+    *(u32x4_t*)((uint16_t*)p + i) = w;
+  }
+}
+
+template <int DT>
+__global__ __launch_bounds__(AT) void adjust_kernel(Adjust a, int L, int V) {
+#pragma clang fp contract(off)
+  constexpr int N = LogitVec<DT>::N;
+  __shared__ alignas(16) int seen[AT * N];       // bit 0: in the prompt; above it: occurrences behind the prompt
+  __shared__ alignas(16) int entry[AT * N];      // index of the word's last bias, counted from 1 within the sequence's
+  const int s = blockIdx.y, w0 = blockIdx.x * AT * N, tid = threadIdx.x;
+  const int mine = w0 + tid * N;                 // V % N == 0: whole vectors only
+  const bool has = mine < V;
+  const long row0 = (long)s * L;
+  u32x4_t next = {};
+  if (has) next = LogitVec<DT>::load_raw(a.z, row0 * V + mine);
+#pragma unroll
+  for (int e = 0; e < N; e += 4) *(u32x4_t*)(seen + tid * N + e) = (u32x4_t){};
+  if (a.bias_start) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) *(u32x4_t*)(entry + tid * N + e) = (u32x4_t){};
+  }
+  __syncthreads();
+  const int h0 = a.history_start[s], h1 = a.history_start[s + 1];
+  const int cut = h0 + (a.prompt_len ? a.prompt_len[s] : 0);
+  for (int i = h0 + tid; i < h1; i += AT) {
+    const int w = a.history[i];
+    const unsigned at = (unsigned)w - (unsigned)w0;
+    if (w >= 0 && w < V && at < (unsigned)(AT * N)) {
+      if (i < cut) atomicOr(seen + at, 1); else atomicAdd(seen + at, 2);
+    }
+  }
+  int b0 = 0;
+  if (a.bias_start) {
+    b0 = a.bias_start[s];
+    const int b1 = a.bias_start[s + 1];
+    for (int i = b0 + tid; i < b1; i += AT) {
+      const int w = a.bias_word[i];
+      const unsigned at = (unsigned)w - (unsigned)w0;
+      if (w >= 0 && w < V && at < (unsigned)(AT * N)) atomicMax(entry + at, i - b0 + 1);
+    }
+  }
+  __syncthreads();
+  if (!has) return;
+  const float rep = a.penalties[4 * s], pres = a.penalties[4 * s + 1], freq = a.penalties[4 * s + 2], temp = a.penalties[4 * s + 3];
+  const float irep = 1.f / rep, itemp = temp > 0.f ? 1.f / temp : 1.f;
+  int n[N];
+  float bias[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    n[e] = seen[tid * N + e];
+    bias[e] = 0.f;
+    if (a.bias_start) {
+      const int i = entry[tid * N + e];
+      if (i > 0) bias[e] = a.bias_value[b0 + i - 1];
+    }
+  }
+  const int pitch = (V + 31) / 32;
+  for (int t = 0; t < L; ++t) {
+    float x[N];
+    LogitVec<DT>::unpack(next, x);
+    if (t + 1 < L) next = LogitVec<DT>::load_raw(a.z, (row0 + t + 1) * V + mine);
+    uint32_t bits = 0xFFFFFFFFu;
+    if (a.allowed) bits = a.allowed[(row0 + t) * pitch + (mine >> 5)] >> (mine & 31);     // N divides 32: one word holds them all
+    if (t > 0 && a.drafted) {
+      const unsigned at = (unsigned)a.drafted[row0 + t - 1] - (unsigned)mine;
+#pragma unroll
+      for (int e = 0; e < N; ++e) n[e] += at == (unsigned)e ? 2 : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float f = n[e] == 0 ? 1.f : x[e] > 0.f ? irep : rep;
+      const int said = n[e] >> 1;
+      const float less = freq * (float)said + (said > 0 ? pres : 0.f);
+      const float y = (x[e] * f - less + bias[e]) * itemp;
+      x[e] = bits >> e & 1 ? y : -INFINITY;
+    }
+    store_logits<DT>(a.out, (row0 + t) * V + mine, x);
+  }
+}
+
+template <int DT>
+hipError_t launch_adjust_t(const Adjust& a, int S, int L, int V, hipStream_t stream) {
+  constexpr int words = AT * LogitVec<DT>::N;
+  hipLaunchKernelGGL((adjust_kernel<DT>), dim3((V + words - 1) / words, S), dim3(AT), 0, stream, a, L, V);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adjust(const Adjust& a, int S, int L, int V, int dtype, hipStream_t stream) {
+  if (S < 1 || L < 1 || V < 2 || S > 65535) return hipErrorInvalidValue;
+  if (dtype == DT_BF16) return launch_adjust_t<DT_BF16>(a, S, L, V, stream);
+  if (dtype == DT_F16) return launch_adjust_t<DT_F16>(a, S, L, V, stream);
+  return launch_adjust_t<DT_F32>(a, S, L, V, stream);
+}
+
+}  // namespace covspec

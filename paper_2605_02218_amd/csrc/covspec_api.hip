@@ -764,6 +764,128 @@ int covspec_draft_gate(const covspec_draft_params* p, const void* z_draft, const
   return e == hipSuccess ? COVSPEC_OK : COVSPEC_HIP_ERROR;
 }
 
+// ---- paged cache, its attention, and adjustments of logits (around a verification round)
+static int cache_check(const covspec_cache_params* p, Paged* c) {
+  if (!p) return COVSPEC_INVALID_ARG;
+  if (p->n_seq < 1 || p->n_tokens < 1 || p->n_kv_heads < 1 || p->head_dim < 1 || p->page_size < 1 || p->n_pages < 1 || p->max_pages < 1)
+    return COVSPEC_INVALID_ARG;
+  if (p->dtype != COVSPEC_BF16 && p->dtype != COVSPEC_FP16) return COVSPEC_INVALID_ARG;
+  if (p->cache_dtype != p->dtype && p->cache_dtype != COVSPEC_INT8 && p->cache_dtype != COVSPEC_E4M3) return COVSPEC_INVALID_ARG;
+  if (p->row_pitch != 0 && (p->row_pitch < (int64_t)p->n_kv_heads * p->head_dim || p->row_pitch % 8 != 0)) return COVSPEC_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 96 && p->head_dim != 128) return COVSPEC_UNSUPPORTED;
+  if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)) != 0) return COVSPEC_UNSUPPORTED;
+  const int64_t most = 1 << 30;
+  if (p->n_seq >= most || (int64_t)p->n_tokens * p->n_kv_heads >= most || (int64_t)p->max_pages * p->page_size >= most) return COVSPEC_UNSUPPORTED;
+  if (p->row_pitch > (int64_t)1 << 32) return COVSPEC_UNSUPPORTED;
+  if ((double)p->n_pages * p->n_kv_heads * p->page_size >= 1099511627776.0) return COVSPEC_UNSUPPORTED;      // 2^40 places
+  int shift = 0;
+  while ((1 << shift) < p->page_size) ++shift;
+  c->S = p->n_seq; c->T = p->n_tokens; c->H = p->n_kv_heads; c->D = p->head_dim;
+  c->page_shift = shift; c->n_pages = p->n_pages; c->max_pages = p->max_pages;
+  c->dtype = p->dtype; c->kept = p->cache_dtype;
+  c->start = c->length = c->pages = nullptr;
+  return COVSPEC_OK;
+}
+
+static int cache_arrays(Paged* c, const void* x, const void* y, const int32_t* start, const int32_t* length, const int32_t* pages, const void* k_cache,
+                        const void* v_cache, const float* k_scale, const float* v_scale) {
+  if (!x || !y || !start || !length || !pages || !k_cache || !v_cache) return COVSPEC_INVALID_ARG;
+  if (c->kept != c->dtype && (!k_scale || !v_scale)) return COVSPEC_INVALID_ARG;
+  if (((uintptr_t)x | (uintptr_t)y | (uintptr_t)k_cache | (uintptr_t)v_cache) & 15) return COVSPEC_INVALID_ARG;
+  if (((uintptr_t)start | (uintptr_t)length | (uintptr_t)pages | (uintptr_t)k_scale | (uintptr_t)v_scale) & 3) return COVSPEC_INVALID_ARG;
+  c->start = start; c->length = length; c->pages = pages;
+  return COVSPEC_OK;
+}
+
+static int launched(const char* what, hipError_t e) {
+  if (e != hipSuccess) note_error(what, e);
+  return e == hipSuccess ? COVSPEC_OK : COVSPEC_HIP_ERROR;
+}
+
+int covspec_cache_write(const covspec_cache_params* p, const void* k, const void* v, const int32_t* start, const int32_t* length,
+                        const int32_t* pages, void* k_cache, void* v_cache, float* k_scale, float* v_scale, covspec_stream_t stream) {
+  Paged c;
+  int st = cache_check(p, &c);
+  if (st != COVSPEC_OK) return st;
+  if ((st = cache_arrays(&c, k, v, start, length, pages, k_cache, v_cache, k_scale, v_scale)) != COVSPEC_OK) return st;
+  discard_pending_error();
+  const long pitch = p->row_pitch ? p->row_pitch : (long)c.H * c.D;
+  return launched("launch_cache_write", launch_cache_write(c, k, v, pitch, k_cache, v_cache, k_scale, v_scale, (hipStream_t)stream));
+}
+
+int covspec_cache_read(const covspec_cache_params* p, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                       const int32_t* start, const int32_t* length, const int32_t* pages, void* k_out, void* v_out, covspec_stream_t stream) {
+  Paged c;
+  int st = cache_check(p, &c);
+  if (st != COVSPEC_OK) return st;
+  if ((st = cache_arrays(&c, k_out, v_out, start, length, pages, k_cache, v_cache, k_scale, v_scale)) != COVSPEC_OK) return st;
+  discard_pending_error();
+  const long pitch = p->row_pitch ? p->row_pitch : (long)c.H * c.D;
+  return launched("launch_cache_read", launch_cache_read(c, k_cache, v_cache, k_scale, v_scale, k_out, v_out, pitch, (hipStream_t)stream));
+}
+
+static int attend_check(const covspec_attend_params* p, Paged* c) {
+  if (!p) return COVSPEC_INVALID_ARG;
+  const int st = cache_check(&p->cache, c);
+  if (st != COVSPEC_OK) return st;
+  if (p->n_heads < 1 || p->n_heads % c->H != 0 || p->max_len < 1 || p->window < 0) return COVSPEC_INVALID_ARG;
+  if (p->max_len > (int64_t)c->max_pages << c->page_shift) return COVSPEC_INVALID_ARG;
+  if (!(fabsf(p->scale) < INFINITY)) return COVSPEC_INVALID_ARG;
+  const int64_t dense = (int64_t)p->n_heads * c->D;
+  for (const int64_t pitch : {p->q_pitch, p->out_pitch})
+    if (pitch != 0 && (pitch < dense || pitch % 8 != 0)) return COVSPEC_INVALID_ARG;
+  if (p->n_heads / c->H > 64 || (int64_t)c->T * p->n_heads >= 1 << 30) return COVSPEC_UNSUPPORTED;
+  if (p->q_pitch > (int64_t)1 << 32 || p->out_pitch > (int64_t)1 << 32) return COVSPEC_UNSUPPORTED;
+  return COVSPEC_OK;
+}
+
+size_t covspec_attend_workspace_size(const covspec_attend_params* p) {
+  Paged c;
+  if (attend_check(p, &c) != COVSPEC_OK) return 0;
+  return attend_workspace_bytes(c, p->n_heads, p->max_len);
+}
+
+int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t* start, const int32_t* length, const int32_t* pages,
+                   const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, const int64_t* visible, void* out,
+                   float* lse_out, void* workspace, size_t workspace_bytes, covspec_stream_t stream) {
+  Paged c;
+  int st = attend_check(p, &c);
+  if (st != COVSPEC_OK) return st;
+  if ((st = cache_arrays(&c, q, out, start, length, pages, k_cache, v_cache, k_scale, v_scale)) != COVSPEC_OK) return st;
+  if (!workspace || ((uintptr_t)workspace & 255) || ((uintptr_t)visible & 7) || ((uintptr_t)lse_out & 3)) return COVSPEC_INVALID_ARG;
+  if (visible && p->window != 0) return COVSPEC_INVALID_ARG;      // a tree's rows are not its positions
+  if (workspace_bytes < attend_workspace_bytes(c, p->n_heads, p->max_len)) return COVSPEC_WORKSPACE_TOO_SMALL;
+  Attend a;
+  a.q = q; a.q_pitch = p->q_pitch ? p->q_pitch : (long)p->n_heads * c.D;
+  a.heads = p->n_heads; a.max_len = p->max_len; a.window = p->window; a.scale = p->scale;
+  a.kc = k_cache; a.vc = v_cache; a.ks = k_scale; a.vs = v_scale;
+  a.visible = (const long long*)visible;
+  a.out = out; a.out_pitch = p->out_pitch ? p->out_pitch : (long)p->n_heads * c.D;
+  a.lse = lse_out;
+  discard_pending_error();
+  return launched("launch_attend", launch_attend(c, a, workspace, (hipStream_t)stream));
+}
+
+int covspec_adjust_logits(const covspec_logits_params* p, const void* z, const int32_t* history, const int32_t* history_start,
+                          const int32_t* prompt_len, const int32_t* drafted, const float* penalties, const int32_t* bias_start,
+                          const int32_t* bias_word, const float* bias_value, const uint32_t* allowed, void* z_out, covspec_stream_t stream) {
+  if (!p) return COVSPEC_INVALID_ARG;
+  if (p->n_seq < 1 || p->n_pos < 1 || p->vocab < 2) return COVSPEC_INVALID_ARG;
+  if (p->dtype != COVSPEC_FP32 && p->dtype != COVSPEC_BF16 && p->dtype != COVSPEC_FP16) return COVSPEC_INVALID_ARG;
+  if (p->n_pos > 64 || (long)p->n_seq * p->n_pos > 65535) return COVSPEC_UNSUPPORTED;
+  if (p->vocab % (p->dtype == COVSPEC_FP32 ? 4 : 8) != 0) return COVSPEC_UNSUPPORTED;
+  if (!z || !history || !history_start || !penalties || !z_out) return COVSPEC_INVALID_ARG;
+  if ((bias_start != nullptr) != (bias_word != nullptr) || (bias_start != nullptr) != (bias_value != nullptr)) return COVSPEC_INVALID_ARG;
+  if (((uintptr_t)z | (uintptr_t)z_out) & 15) return COVSPEC_INVALID_ARG;
+  if (((uintptr_t)history | (uintptr_t)history_start | (uintptr_t)prompt_len | (uintptr_t)drafted | (uintptr_t)penalties | (uintptr_t)bias_start |
+       (uintptr_t)bias_word | (uintptr_t)bias_value | (uintptr_t)allowed) & 3) return COVSPEC_INVALID_ARG;
+  Adjust a;
+  a.z = z; a.history = history; a.history_start = history_start; a.prompt_len = prompt_len; a.drafted = drafted; a.penalties = penalties;
+  a.bias_start = bias_start; a.bias_word = bias_word; a.bias_value = bias_value; a.allowed = allowed; a.out = z_out;
+  discard_pending_error();
+  return launched("launch_adjust", launch_adjust(a, p->n_seq, p->n_pos, p->vocab, p->dtype, (hipStream_t)stream));
+}
+
 const char* covspec_last_error(void) { return g_last_error; }
 
 const char* covspec_status_string(int status) {

@@ -7,7 +7,7 @@
 
 namespace covspec {
 
-enum { DT_F32 = 0, DT_BF16 = 1, DT_F16 = 2 /* logits of the vocabulary passes only */ };
+enum { DT_F32 = 0, DT_BF16 = 1, DT_F16 = 2 /* logits, cached tokens */, DT_I8 = 3, DT_E4M3 = 4 /* caches only */ };
 
 // ---------------------------------------------------------------- gemm.hip
 // C[M,N] = A[M,K] * B[N,K]^T  (both operands K-contiguous), fp32 accumulation on MFMA.
@@ -246,5 +246,44 @@ int draft_max_vocab();
 size_t draft_workspace_bytes(int S, int L, int V);
 hipError_t launch_draft(const void* zd, const int32_t* tok, int S, int L, int V, int dtype, int F0, const int* fanout, float gamma,
                         float* margin, int32_t* gate, int32_t* cand, void* ws, hipStream_t stream);
+
+// ---------------------------------------------------------------- cache.hip, attend.hip
+// Paged cache: pool [n_pages][H][1 << page_shift][D] of codes and, in 8 bits, fp32 scales; the rows start[s] .. start[s + 1] - 1 of a
+// packed tensor are the last positions of sequence s, length[s] long with them.
+struct Paged {
+  int S, T, H, D;                      // sequences, rows, key heads, head dimension
+  int page_shift, n_pages, max_pages;
+  int dtype, kept;                     // DT_BF16 / DT_F16; the same, DT_I8 or DT_E4M3
+  const int32_t *start, *length, *pages;
+};
+hipError_t launch_cache_write(const Paged& c, const void* k, const void* v, long pitch, void* kc, void* vc, float* ks, float* vs, hipStream_t stream);
+hipError_t launch_cache_read(const Paged& c, const void* kc, const void* vc, const float* ks, const float* vs, void* k, void* v, long pitch,
+                             hipStream_t stream);
+struct Attend {
+  const void* q;
+  long q_pitch;
+  int heads, max_len, window;
+  float scale;
+  const void *kc, *vc;
+  const float *ks, *vs;
+  const long long* visible;            // or null
+  void* out;
+  long out_pitch;
+  float* lse;                          // or null
+};
+size_t attend_workspace_bytes(const Paged& c, int heads, int max_len);
+hipError_t launch_attend(const Paged& c, const Attend& a, void* ws, hipStream_t stream);
+
+// ---------------------------------------------------------------- adjust.hip
+struct Adjust {
+  const void* z;
+  const int32_t *history, *history_start, *prompt_len, *drafted;
+  const float* penalties;
+  const int32_t *bias_start, *bias_word;
+  const float* bias_value;
+  const uint32_t* allowed;
+  void* out;
+};
+hipError_t launch_adjust(const Adjust& a, int S, int L, int V, int dtype, hipStream_t stream);
 
 }  // namespace covspec
