@@ -857,7 +857,7 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
   if (workspace_bytes < attend_workspace_bytes(c, p->n_heads, p->max_len)) return COVSPEC_WORKSPACE_TOO_SMALL;
   Attend a;
   a.q = q; a.q_pitch = p->q_pitch ? p->q_pitch : (long)p->n_heads * c.D;
-  a.heads = p->n_heads; a.max_len = p->max_len; a.window = p->window; a.scale = p->scale;
+  a.heads = p->n_heads; a.max_len = p->max_len; a.window = p->window < 1 << 30 ? p->window : 1 << 30; a.scale = p->scale;
   a.kc = k_cache; a.vc = v_cache; a.ks = k_scale; a.vs = v_scale;
   a.visible = (const long long*)visible;
   a.out = out; a.out_pitch = p->out_pitch ? p->out_pitch : (long)p->n_heads * c.D;
