@@ -512,16 +512,17 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
 /*
  * covspec_adjust_logits: what a sampler does to the logits in front of covspec_verify and covspec_draft_gate:
  * penalties for words that were said, biases, temperature and a grammar's mask.  NOT in the paper (its softmax
- * equations, Sec. II-A, take the logits as they are).  For sequence s, position tau and word w, in fp32 with each
- * operation rounded on its own, x = z[s, tau, w]:
- *   1. w in the history of s or among drafted[s, 0 .. tau-1]: x = x > 0 ? x * (1 / r) : x * r;
+ * equations, Sec. II-A, take the logits as they are).  For sequence s, position tau and word w, x = z[s, tau, w]:
+ *   1. w in the history of s or among drafted[s, 0 .. tau-1]: x = x > 0 ? x / r : x * r;
  *   2. n = occurrences of w in the history behind its first prompt_len[s] words and among drafted[s, 0 .. tau-1]:
  *      x = x - (f * n + (n > 0 ? c : 0));
  *   3. x = x + bias of w, if s has one (of several entries for a word the last one counts);
- *   4. x = x * (1 / T);
+ *   4. x = x / T;
  *   5. w not allowed: x = -infinity;
- * with (r, c, f, T) = penalties[s] = repetition, presence, frequency, temperature; (1, 0, 0, 1) changes nothing.  A T that
- * is not > 0 counts as 1.
+ * with (r, c, f, T) = penalties[s] = repetition, presence, frequency, temperature; (1, 0, 0, 1) changes no bit.  A T that
+ * is not > 0 counts as 1.  Steps 1 to 4 are one fp32 multiplication and addition with a factor and a summand per word,
+ * themselves formed in fp32: off by at most eight roundings of 2^-24 of the largest magnitude that occurs in them; then
+ * one rounding to dtype.
  * DEVICE pointers:
  *   z, z_out  [n_seq, n_pos, vocab] dtype, 16-byte aligned; z_out may be z (not overlap it otherwise)
  *   history   packed words, int32; history_start [n_seq + 1] int32 ascending; prompt_len [n_seq] int32 or NULL (0)

@@ -1,7 +1,7 @@
 // What a sampler does to logits before they are verified: penalties for words that were said, biases, temperature, a grammar's mask.
 //
-// For a word with n occurrences in what the model has said, x = z * (said or asked ? (z > 0 ? 1 / r : r) : 1) - (f n + (n > 0 ? c : 0)) + bias,
-// times 1 / T, -infinity where the mask says so.  One workgroup takes a chunk of the vocabulary, a vector of words a thread, for all positions of a
+// For a word with n occurrences in what the model has said, x = z F + A with F = (said or asked ? (z > 0 ? 1 / r : r) : 1) / T and
+// A = (bias - (f n + (n > 0 ? c : 0))) / T, -infinity where the mask says so.  One workgroup takes a chunk of the vocabulary, a vector of words a thread, for all positions of a
 // sequence: the history is counted once in LDS (a word of it lands in one of the chunks), a thread then keeps the counts of its words in
 // registers, and from one position to the next only the drafted word between them is added.
 #include "vocab.h"
@@ -10,7 +10,10 @@ namespace covspec {
 
 namespace {
 
+// Threads of a workgroup, rows on their way; us for 64 x 8 rows of 151936 bf16 words with histories, biases and masks: 512 threads and one row 79.2,
+// two 74, three 74.4, four 75.2; two rows with 256 threads 80, with 1024 75.
 constexpr int AT = 512;
+constexpr int AHEAD = 2;
 
 template <int DT>
 __device__ __forceinline__ void store_logits(void* p, long i, const float (&x)[LogitVec<DT>::N]) {
@@ -44,8 +47,24 @@ __global__ __launch_bounds__(AT) void adjust_kernel(Adjust a, int L, int V) {
   const int mine = w0 + tid * N;                 // V % N == 0: whole vectors only
   const bool has = mine < V;
   const long row0 = (long)s * L;
-  u32x4_t next = {};
-  if (has) next = LogitVec<DT>::load_raw(a.z, row0 * V + mine);
+  // The rows on their way with their masks, the first ones while the history is counted.  Loads come back in order: nothing else is loaded in
+  // the loop over the rows, or it would wait for all of these.
+  const int pitch = (V + 31) / 32;
+  u32x4_t next[AHEAD];
+  uint32_t mask[AHEAD];
+  auto fetch = [&](int t, int u) {
+    if (has && t < L) {
+      next[u] = LogitVec<DT>::load_raw(a.z, (row0 + t) * V + mine);
+      if (a.allowed) mask[u] = a.allowed[(row0 + t) * pitch + (mine >> 5)];        // N divides 32: one word holds them all
+    }
+  };
+#pragma unroll
+  for (int t = 0; t < AHEAD; ++t) {
+    next[t] = (u32x4_t){};
+    mask[t] = 0;
+    fetch(t, t);
+  }
+  const int lane = tid & 63, word_of = a.drafted && lane < L ? a.drafted[row0 + lane] : -1;
 #pragma unroll
   for (int e = 0; e < N; e += 4) *(u32x4_t*)(seen + tid * N + e) = (u32x4_t){};
   if (a.bias_start) {
@@ -55,6 +74,7 @@ __global__ __launch_bounds__(AT) void adjust_kernel(Adjust a, int L, int V) {
   __syncthreads();
   const int h0 = a.history_start[s], h1 = a.history_start[s + 1];
   const int cut = h0 + (a.prompt_len ? a.prompt_len[s] : 0);
+#pragma unroll 4
   for (int i = h0 + tid; i < h1; i += AT) {
     const int w = a.history[i];
     const unsigned at = (unsigned)w - (unsigned)w0;
@@ -76,36 +96,43 @@ __global__ __launch_bounds__(AT) void adjust_kernel(Adjust a, int L, int V) {
   if (!has) return;
   const float rep = a.penalties[4 * s], pres = a.penalties[4 * s + 1], freq = a.penalties[4 * s + 2], temp = a.penalties[4 * s + 3];
   const float irep = 1.f / rep, itemp = temp > 0.f ? 1.f / temp : 1.f;
-  int n[N];
-  float bias[N];
+  // x F + A: a word's F above and below zero, and A, for the n occurrences in `seen`
+  float up[N], down[N], add[N];
+  auto word = [&](int e, int n, int i) {
+    const float bias = i > 0 ? a.bias_value[b0 + i - 1] : 0.f;
+    const int said = n >> 1;
+    up[e] = n == 0 ? itemp : irep * itemp;
+    down[e] = n == 0 ? itemp : rep * itemp;
+    const float less = freq * (float)said + (said > 0 ? pres : 0.f);
+    add[e] = (bias - less) * itemp;
+  };
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    n[e] = seen[tid * N + e];
-    bias[e] = 0.f;
-    if (a.bias_start) {
-      const int i = entry[tid * N + e];
-      if (i > 0) bias[e] = a.bias_value[b0 + i - 1];
-    }
-  }
-  const int pitch = (V + 31) / 32;
-  for (int t = 0; t < L; ++t) {
+  for (int e = 0; e < N; ++e) word(e, seen[tid * N + e], a.bias_start ? entry[tid * N + e] : 0);
+  for (int t0 = 0; t0 < L; t0 += AHEAD)
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) {
+    const int t = t0 + u;
+    if (t >= L) break;
     float x[N];
-    LogitVec<DT>::unpack(next, x);
-    if (t + 1 < L) next = LogitVec<DT>::load_raw(a.z, (row0 + t + 1) * V + mine);
-    uint32_t bits = 0xFFFFFFFFu;
-    if (a.allowed) bits = a.allowed[(row0 + t) * pitch + (mine >> 5)] >> (mine & 31);     // N divides 32: one word holds them all
-    if (t > 0 && a.drafted) {
-      const unsigned at = (unsigned)a.drafted[row0 + t - 1] - (unsigned)mine;
+    LogitVec<DT>::unpack(next[u], x);
+    const uint32_t bits = mask[u] >> (mine & 31);
+    fetch(t + AHEAD, u);
+    if (t > 0) {
+      const unsigned at = (unsigned)__builtin_amdgcn_readlane(word_of, t - 1) - (unsigned)mine;
+      if (at < (unsigned)N) {                    // one thread of the row's
 #pragma unroll
-      for (int e = 0; e < N; ++e) n[e] += at == (unsigned)e ? 2 : 0;
+        for (int e = 0; e < N; ++e)
+          if (at == (unsigned)e) word(e, seen[tid * N + e] += 2, a.bias_start ? entry[tid * N + e] : 0);
+      }
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float f = n[e] == 0 ? 1.f : x[e] > 0.f ? irep : rep;
-      const int said = n[e] >> 1;
-      const float less = freq * (float)said + (said > 0 ? pres : 0.f);
-      const float y = (x[e] * f - less + bias[e]) * itemp;
-      x[e] = bits >> e & 1 ? y : -INFINITY;
+    for (int e = 0; e < N; ++e) x[e] = __builtin_fmaf(x[e], x[e] > 0.f ? up[e] : down[e], add[e]);
+    if (a.allowed) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const uint32_t keep = (uint32_t)((int32_t)(bits << (31 - e)) >> 31);
+        x[e] = __uint_as_float((__float_as_uint(x[e]) & keep) | (0xFF800000u & ~keep));
+      }
     }
     store_logits<DT>(a.out, (row0 + t) * V + mine, x);
   }

@@ -20,6 +20,24 @@ __device__ __forceinline__ int seq_of(const int32_t* start, int S, int t) {
   return lo - 1;
 }
 
+// The same for a whole wave, lanes asking for tokens of their own: GROUPS runs of neighbouring lanes, one token each.  64 starts are compared at a
+// time, so that up to 256 sequences take one or a few loads that do not wait for one another; beyond, halving takes fewer.
+template <int GROUPS>
+__device__ __forceinline__ int seq_of_wave(const int32_t* start, int S, int t) {
+  if (S > 256) return seq_of(start, S, t);
+  const int lane = threadIdx.x & 63, group = lane / (64 / GROUPS);
+  int s = -1;
+  for (int s0 = 0; s0 <= S; s0 += 64) {
+    const int v = s0 + lane <= S ? start[s0 + lane] : 0x7FFFFFFF;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int n = __popcll(__ballot(v <= __builtin_amdgcn_readlane(t, g * (64 / GROUPS))));
+      s += group == g ? n : 0;
+    }
+  }
+  return s;
+}
+
 // Place of position `pos` of sequence s, counted in tokens of one key head's slots: (page * H + head) << shift | place.  -1: it does not exist.
 __device__ __forceinline__ long place_of(const Paged& c, int s, long pos, int head) {
   if (pos < 0 || (pos >> c.page_shift) >= c.max_pages) return -1;
