@@ -44,14 +44,28 @@ template <int DT, int KEPT, int D> struct Form {
   }
 };
 
-template <int DT> struct Operand;
-template <> struct Operand<DT_BF16> {
+// A product of M columns (positions for S^T, columns of v for O^T) with M rows over KM terms; a lane has eight neighbouring terms of an operand, those
+// of its group of M lanes, and CA values of the result: column 8 b + 4 group + i for value 4 b + i.
+template <int DT, int M> struct Operand;
+template <> struct Operand<DT_BF16, 32> {
   typedef bf16x8_t vec;
-  static __device__ __forceinline__ f32x16_t mfma(vec a, vec b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  typedef f32x16_t acc;
+  static __device__ __forceinline__ acc mfma(vec a, vec b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
-template <> struct Operand<DT_F16> {
+template <> struct Operand<DT_F16, 32> {
   typedef f16x8_t vec;
-  static __device__ __forceinline__ f32x16_t mfma(vec a, vec b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  typedef f32x16_t acc;
+  static __device__ __forceinline__ acc mfma(vec a, vec b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Operand<DT_BF16, 16> {
+  typedef bf16x8_t vec;
+  typedef f32x4_t acc;
+  static __device__ __forceinline__ acc mfma(vec a, vec b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Operand<DT_F16, 16> {
+  typedef f16x8_t vec;
+  typedef f32x4_t acc;
+  static __device__ __forceinline__ acc mfma(vec a, vec b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
 // Eight codes to a 16-bit type, exactly: integers up to 127 and e4m3's four bits of significand fit both.
@@ -81,14 +95,28 @@ __device__ __forceinline__ u32x4_t widen8(u32x2_t w) {
   return r;
 }
 
-// max over the two lanes of a row (lane, lane ^ 32)
-__device__ __forceinline__ float pair_max(float x) {
+// Over the lanes of a row, one in each group of M.
+template <int M, typename F>
+__device__ __forceinline__ float over_groups(float x, F f) {
+  if constexpr (M == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float pair_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+template <int M> __device__ __forceinline__ float row_max(float x) { return over_groups<M>(x, [](float a, float b) { return fmaxf(a, b); }); }
+template <int M> __device__ __forceinline__ float row_sum(float x) { return over_groups<M>(x, [](float a, float b) { return a + b; }); }
+
+// Sums of the lanes up to each, in six steps.
+__device__ __forceinline__ int wave_inscan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
 }
 
 // Pool to LDS, 16 or 4 bytes a lane: to `lds` + lane * 16 (4).  Written out because the compiler, where it knows of such a load, waits for all
@@ -100,16 +128,16 @@ __device__ __forceinline__ void load16_lds(unsigned lds, const void* base, unsig
 __device__ __forceinline__ void load4_lds(unsigned lds, const void* from) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory");
 }
+__device__ __forceinline__ long uniform(long v) {
+  return (long)(((unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)v));
+}
 // Waits that no access to memory is moved across.
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void meet() { asm volatile("s_barrier" ::: "memory"); }
 
-// How the positions are split over workgroups: chunks of `clen` positions, a multiple of 128.
-struct Split { int chunks, clen; };
-
-// Row t of the batch and its range of positions, for whoever needs it row by row: [lo, hi) holds all it can see.
+// What rows i0 .. i1 of a sequence see lies in [lo, hi).
 struct Range { int lo, hi; };
 __device__ __forceinline__ Range seen_range(const Paged& c, const Attend& a, int old, int n, int i0, int i1) {
   const long cap = min((long)a.max_len, (long)c.max_pages << c.page_shift);
@@ -118,60 +146,181 @@ __device__ __forceinline__ Range seen_range(const Paged& c, const Attend& a, int
 }
 __device__ __forceinline__ int tokens_before(int length, int n) { return (int)max((long)length - n, -(1l << 30)); }
 
-template <int DT, int KEPT, int D, int RW, int KW, int KT>
-__global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void attend_kernel(Paged c, Attend a, Split sp, int tiles, float* __restrict__ part, f32x2_t* __restrict__ stat) {
+// The work: an item is a tile of `rows` rows of a sequence and a key head, a unit `unit` of its positions.  Items lie one behind the other, by sequence,
+// head and tile, all of a sequence counted with the units of its longest.
+//   shares > 0: that many workgroups at most take equal pieces of the sequence of units, so that long and short sequences together keep all of them
+//     busy to the end; an item that a piece does not hold whole goes to `part`, and attend_join_kernel adds its pieces up.
+//   shares == 0: a workgroup per item, and no join: many items even out by themselves.
+struct Split { int rows, unit, shares, least, tiles, joins; bool by_item; };
+
+// The sequences, 64 at a time, a lane each: rows, length, tiles, units of an item, units in all and up to here.
+struct Block { int row0, n, len, tiles, units, own, upto, items_upto; };
+template <bool ITEMS>                                 // ITEMS: a unit is a tile, of one head
+__device__ __forceinline__ Block block_of(const Paged& c, const Attend& a, const Split& sp, int s0) {
+  const int mine = s0 + (threadIdx.x & 63), safe = min(mine, c.S - 1), G = a.heads / c.H;
+  Block v;
+  v.row0 = min(max(c.start[safe], 0), c.T);
+  v.n = max(min(c.start[safe + 1], c.T), v.row0) - v.row0;
+  v.len = c.length[safe];
+  v.tiles = mine < c.S ? (int)(((long)v.n * G + sp.rows - 1) / sp.rows) : 0;
+  v.units = 1;
+  if constexpr (!ITEMS) {
+    long most = seen_range(c, a, tokens_before(v.len, v.n), v.n, 0, v.n - 1).hi;
+    if (a.window > 0) most = min(most, (long)a.window + sp.rows / G + 17);       // first and last row of a tile, rounding to 16
+    v.units = max(1, (int)((most + sp.unit - 1) / sp.unit));
+  }
+  v.own = ITEMS ? v.tiles : v.tiles * v.units * c.H;
+  v.upto = wave_inscan(v.own);
+  v.items_upto = ITEMS || !sp.by_item ? 0 : wave_inscan(v.tiles * c.H);
+  return v;
+}
+// at: where the unit asked for lies among the sequence's own; items: items in front of the sequence; s < 0: nowhere
+struct Place { int s, row0, n, len, tiles, units, at, items; };
+// Unit x of the block, which begins at sequence s0, behind `items` items of heads H.
+__device__ __forceinline__ Place place_in(const Block& v, int s0, int x, int items, int H) {
+  Place p;
+  p.s = -1;
+  const unsigned long long over = __ballot(v.upto > x);
+  if (over) {
+    const int at = __ffsll((long long)over) - 1, own = __builtin_amdgcn_readlane(v.own, at);
+    p.s = s0 + at;
+    p.row0 = __builtin_amdgcn_readlane(v.row0, at);
+    p.n = __builtin_amdgcn_readlane(v.n, at);
+    p.len = __builtin_amdgcn_readlane(v.len, at);
+    p.tiles = __builtin_amdgcn_readlane(v.tiles, at);
+    p.units = __builtin_amdgcn_readlane(v.units, at);
+    p.items = items + __builtin_amdgcn_readlane(v.items_upto, at) - p.tiles * H;
+    p.at = x - __builtin_amdgcn_readlane(v.upto, at) + own;
+    if (p.at < 0 || p.at >= own) p.s = -1;                     // `start` does not ascend
+  }
+  return p;
+}
+__device__ __forceinline__ int block_total(const Block& v) { return __builtin_amdgcn_readlane(v.upto, 63); }
+template <bool ITEMS>
+__device__ __forceinline__ Place find(const Paged& c, const Attend& a, const Split& sp, int x) {
+  Place p;
+  p.s = -1;
+  int items = 0;
+  for (int s0 = 0; s0 < c.S && p.s < 0; s0 += 64) {
+    const Block v = block_of<ITEMS>(c, a, sp, s0);
+    p = place_in(v, s0, x, items, c.H);
+    x -= block_total(v);
+    items += __builtin_amdgcn_readlane(v.items_upto, 63);
+  }
+  return p;
+}
+// Shares of `total` units: the first `more` have one unit more than the others.
+struct Shares {
+  int n = 0, each = 0, more = 0;
+  __device__ __forceinline__ Shares() {}
+  __device__ __forceinline__ Shares(const Split& sp, int total) : n(min(sp.shares, max(1, total / sp.least))), each(total / n), more(total - each * n) {}
+  __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
+  __device__ __forceinline__ int of(int x) const { return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each; }
+};
+// For the join: an item in several pieces.  Written by the share in which it begins, to the item's number where there are few items (items in one
+// piece then say so), otherwise to the share's.
+struct Joined { int pieces, share, row0, head0, r0, rows; };   // pieces (0: nothing to do), the first one's share; first row of the sequence in the batch,
+                                                               // first query head, first row of the tile among the sequence's, their count
+
+template <int DT, int KEPT, int D, int M, int RW, int KW, int KT>
+__global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend a, Split sp, float* __restrict__ part, f32x2_t* __restrict__ stat, Joined* __restrict__ joined, int* __restrict__ joined_count) {
   typedef Form<DT, KEPT, D> F;
-  constexpr bool CODES = KEPT != DT;
-  constexpr int VDT = CODES ? DT_BF16 : DT;              // type of the products with v
-  constexpr bool SPLIT_P = CODES && DT == DT_F16;        // p v_scale in two bf16 parts: fp16 has not the range for it, one bf16 not the bits
-  constexpr int TR = 32 * RW, DT32 = D / 32, KS = D / 16, ST = KT / 32;
-  constexpr int TILE = KT * F::ROWB, STAGE = 2 * TILE + (CODES ? 8 * KT : 0), GROUP = 2 * STAGE;
+  // 8-bit codes: a single wave widens what it multiplies; waves that share tiles widen each tile once, in LDS, between them.  Their scales: of K
+  // times the scores; of V times p, in fp32, which bf16 has the range for.  fp16 has not: the shared tiles hold v = code * scale, rounded once
+  // more, and a single wave takes codes and p v_scale in two bf16 parts.
+  constexpr bool CODES = KEPT != DT, WIDE = CODES && RW > 1;
+  constexpr int VDT = CODES && !WIDE ? DT_BF16 : DT;     // type of the products with v
+  constexpr bool SPLIT_P = CODES && !WIDE && DT == DT_F16, SCALE_P = CODES && !(WIDE && DT == DT_F16);
+  typedef Form<DT, WIDE ? DT : KEPT, D> W;               // of the tiles that are multiplied
+  constexpr bool RAW = CODES && !WIDE;
+  typedef Operand<DT, M> P1;
+  typedef Operand<VDT, M> P2;
+  typedef typename P1::vec vec;
+  typedef typename P2::vec vvec;
+  typedef typename P1::acc acc;
+  constexpr int NG = 64 / M, KM = 8 * NG, CA = M * M / 64;               // lanes of a row; terms of a product; values of a result in a lane
+  constexpr int TR = M * RW, DM = D / M, KS = D / KM, ST = KT / M, NX = KT / KM;
+  constexpr int TILE = KT * F::ROWB, STAGE = 2 * TILE + (CODES ? 8 * KT : 0);
+  constexpr int WTILE = KT * W::ROWB, GROUP = 2 * STAGE + (WIDE ? 2 * WTILE : 0);
   constexpr int LOADS = KT / F::RPI / RW;                // of a wave, for one of K and V
-  static_assert(LOADS >= 1 && 2 * LOADS + 1 < 63, "");
-  typedef typename Operand<DT>::vec vec;
-  typedef typename Operand<VDT>::vec vvec;
+  static_assert(LOADS >= 1 && 2 * LOADS + 1 < 63 && D % KM == 0 && KT % KM == 0 && KT % 32 == 0 && KT <= 64, "");
   extern __shared__ __align__(1024) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rw = wave % RW, kw = wave / RW, half = lane >> 5;
+  const int rw = wave % RW, kw = wave / RW, grp = lane / M;
   const int G = a.heads / c.H;
 
-  // ---- which rows: key heads next to each other (an XCD each, for eight of them, so that row tiles of one head meet in its L2), then chunks, then
-  // row tiles from the last to the first, which see most
-  const int g = blockIdx.x % c.H, chunk = blockIdx.x / c.H % sp.chunks;
-  int tile = tiles - 1 - (int)(blockIdx.x / c.H / sp.chunks), s = -1, row0 = 0, n = 0;
-  for (int s0 = 0; s0 < c.S && s < 0; s0 += 64) {
-    const int mine = s0 + lane;
-    const int b = mine < c.S ? min(max(c.start[mine], 0), c.T) : c.T, e = mine < c.S ? max(min(c.start[mine + 1], c.T), b) : c.T;
-    const int own = mine < c.S ? (int)(((long)(e - b) * G + TR - 1) / TR) : 0;
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int w = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += w;
+  // ---- which work.  Items: key heads next to each other (an XCD each, for eight of them, so that row tiles of one head meet in its L2), row tiles
+  // from the last to the first, which see most.  Shares: neighbours on one XCD.
+  int x = 0, x_end = 1, share = 0;
+  Shares share_of_unit;
+  Place p;
+  if (sp.shares > 0) {
+    const Block first = block_of<false>(c, a, sp, 0);                  // in most calls all sequences
+    int total = block_total(first), items = __builtin_amdgcn_readlane(first.items_upto, 63);
+    for (int s0 = 64; s0 < c.S; s0 += 64) {
+      const Block v = block_of<false>(c, a, sp, s0);
+      total += block_total(v);
+      items += __builtin_amdgcn_readlane(v.items_upto, 63);
     }
-    const unsigned long long over = __ballot(upto > tile);
-    if (over) {
-      const int l = __ffsll((long long)over) - 1;
-      s = __builtin_amdgcn_readfirstlane(s0 + l);
-      row0 = __builtin_amdgcn_readlane(b, l);
-      n = __builtin_amdgcn_readlane(e, l) - row0;
-      tile -= __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(own, l);
-    } else {
-      tile -= __builtin_amdgcn_readlane(upto, 63);
+    const Shares shares(sp, total);
+    const int each = (shares.n + 7) / 8;
+    share = (blockIdx.x % 8) * each + blockIdx.x / 8;
+    if ((int)(blockIdx.x / 8) >= each) share = sp.shares - 1 - (blockIdx.x - 8 * each);     // the numbers left, from the last down
+    if (blockIdx.x == 0 && tid == 0) *joined_count = sp.by_item ? items : sp.shares;
+    if (share < shares.n) {
+      x = shares.begin(share);
+      x_end = shares.begin(share + 1);
     }
+    if (share >= shares.n || x >= x_end) {
+      if (tid == 0 && !sp.by_item) joined[share].pieces = 0;
+      return;
+    }
+    p = c.S <= 64 ? place_in(first, 0, x, 0, c.H) : find<false>(c, a, sp, x);
+    share_of_unit = shares;
+  } else {
+    p = find<true>(c, a, sp, sp.tiles - 1 - (int)(blockIdx.x / c.H));
   }
-  if (s < 0) return;
-  tile = __builtin_amdgcn_readfirstlane(tile);
-  const int old = __builtin_amdgcn_readfirstlane(tokens_before(c.length[s], n));
-  const int rows = n * G, r0 = tile * TR;                             // T heads < 2^30
+  while (true) {
+  if (p.s < 0) {
+    if (sp.shares > 0 && !sp.by_item && tid == 0) joined[share].pieces = 0;
+    return;
+  }
+  const int s = p.s, row0 = p.row0, n = p.n;
+  int tile = p.at, g = blockIdx.x % c.H, from = 0, upto = 1;
+  bool whole = true;
+  if (sp.shares > 0) {
+    const int item = p.at / p.units;
+    from = p.at - item * p.units;
+    upto = min(p.units, from + x_end - x);
+    whole = from == 0 && upto == p.units;
+    g = item / p.tiles;
+    tile = item - g * p.tiles;
+    if (tid == 0 && (from == 0 ? sp.by_item || !whole || x + upto >= x_end : !sp.by_item && x + upto - from >= x_end)) {
+      Joined j = {};                                                   // by share: its last segment writes, whatever that is
+      if (from == 0 && !whole) {
+        j.pieces = share_of_unit.of(x + p.units - 1) - share + 1;
+        j.share = share;
+        j.row0 = p.row0;
+        j.head0 = g * G;
+        j.r0 = tile * TR;
+        j.rows = p.n * G;
+      }
+      const int at = sp.by_item ? p.items + item : share;
+      if (at >= 0 && at < sp.joins) joined[at] = j;
+    }
+    x += upto - from;
+  } else {
+    x = x_end;
+  }
+  const int old = tokens_before(p.len, n), rows = n * G, r0 = tile * TR;   // T heads < 2^30
   const int i0 = r0 / G, i1 = (min(r0 + TR, rows) - 1) / G;
   const Range range = seen_range(c, a, old, n, i0, i1);
-  const int lo = __builtin_amdgcn_readfirstlane(max(range.lo, chunk * sp.clen) & ~15), hi = __builtin_amdgcn_readfirstlane(min(range.hi, (chunk + 1) * sp.clen));
-  if (lo >= hi && sp.chunks > 1) return;
+  const int low = range.lo & ~15;
+  const int lo = (int)min((long)low + (long)from * sp.unit, 0x7FFFFFF0l), hi = whole ? range.hi : (int)min((long)range.hi, (long)low + (long)upto * sp.unit);
   const int count = lo < hi ? (hi - lo + KT - 1) / KT : 0;            // tiles; this wave's are kw, kw + KW, ...
 
   // ---- the lane's row and what it sees: positions [klo, khi), and bits of the chunk.  Rows beyond the last count as seeing all, of a query of zeros.
-  const int r = r0 + 32 * rw + (lane & 31);
+  const int rfirst = r0 + M * rw, r = rfirst + lane % M;
   const bool has = r < rows;
   const int token = has ? r / G : 0, head = g * G + (has ? r - token * G : 0), t_row = row0 + token;
   int klo = 0, khi = 0x7FFFFFFF;
@@ -180,19 +329,25 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
     if (a.visible) { khi = old; bits = (unsigned long long)a.visible[t_row]; }
     else { khi = old + token + 1; klo = a.window ? khi - a.window : 0; }
   }
-  const int khi_min = __builtin_amdgcn_readfirstlane(wave_min(khi)), klo_max = __builtin_amdgcn_readfirstlane(wave_max(klo));
-  const int khi_max = a.visible ? 0x7FFFFFFF : __builtin_amdgcn_readfirstlane(wave_max(has ? khi : 0));
-  const int klo_min = __builtin_amdgcn_readfirstlane(wave_min(has ? klo : 0x7FFFFFFF));
+  // of the wave's rows, which see more from one to the next: what all see is [klo_max, khi_min), what any [klo_min, khi_max)
+  int khi_min = 0, khi_max = 0, klo_min = 0, klo_max = 0;
+  if (rfirst < rows) {
+    const int tfirst = rfirst / G, tlast = (min(rfirst + M, rows) - 1) / G;
+    khi_min = a.visible ? old : old + tfirst + 1;
+    khi_max = a.visible ? 0x7FFFFFFF : old + tlast + 1;
+    klo_min = a.window ? khi_min - a.window : 0;
+    klo_max = a.window ? khi_max - a.window : 0;
+  }
 
-  // p = 2^((z - m) c2): z the product q . k, in 8 bits times the scales of the key and of the softmax.  c2 is above zero, so that -infinity stays
+  // p = 2^((z - m) c2): z the product q . k, in 8 bits times the scale of the key.  c2 is above zero, so that -infinity stays
   // what it is.  `unit` brings m back to the scores' own units.
-  const float unit = CODES ? 1.f : fmaxf(fabsf(a.scale), 1.2e-38f), c2 = unit * kLog2E, kscale = fabsf(a.scale);
+  const float unit = fmaxf(fabsf(a.scale), 1.2e-38f), c2 = unit * kLog2E;
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;             // a negative scale negates the query
   vec q[KS];
 #pragma unroll
   for (int k = 0; k < KS; ++k) {
     u32x4_t w = {};
-    if (has) w = *(const u32x4_t*)((const uint16_t*)a.q + t_row * a.q_pitch + (long)head * D + 16 * k + 8 * half) ^ flip;
+    if (has) w = *(const u32x4_t*)((const uint16_t*)a.q + t_row * a.q_pitch + (long)head * D + KM * k + 8 * grp) ^ flip;
     q[k] = __builtin_bit_cast(vec, w);
   }
 
@@ -251,6 +406,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
       }
       const int x = (x0 & 15) + lane / F::CH, piece = (lane % F::CH) ^ F::turn(x);
       if (F::PIECES == F::CH || piece < F::PIECES) {
+        where = uniform(where);
         const unsigned off = (unsigned)min(x, l) * (D * F::ESZ) + piece * 16;
         load16_lds(to + x0 * F::ROWB, (const char*)a.kc + where * (D * F::ESZ), off);
         load16_lds(to + TILE + x0 * F::ROWB, (const char*)a.vc + where * (D * F::ESZ), off);
@@ -258,85 +414,125 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
     }
   };
 
-  f32x16_t o[DT32];
+  acc o[DM];
 #pragma unroll
-  for (int d = 0; d < DT32; ++d)
+  for (int d = 0; d < DM; ++d)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    for (int e = 0; e < CA; ++e) o[d][e] = 0.f;
   float m = -INFINITY, ref = 0.f, sum = 0.f;             // ref = m c2, or zero
   bool far = false;                                      // m c2 is beyond the range of fp32 in some lane
 
-  // K: row 4 h + 8 b + ... of an S^T tile is position 16 t + 8 h + 4 b + i, so that a lane's values 8 t .. 8 t + 7 are eight positions in a row
-  const int krow = (lane & 3) | (lane & 8) >> 1 | (lane & 4) << 1 | (lane & 16);
-  const int kbase = krow * F::ROWB + (CODES ? F::turn(krow) * 16 + 8 * half : (half ^ F::turn(krow)) * 16);
-  // V: a group of 16 lanes reads 4 (8, codes) positions x 16 columns, which come out as a column for each lane
-  const int vgrp = lane >> 4, vj = lane & 15;
-  int vbase[CODES ? 1 : 2];
-  if constexpr (CODES) {
-    const int x = 8 * (vgrp >> 1) + vj / 2;
-    vbase[0] = x * F::ROWB + ((vgrp & 1) ^ F::turn(x)) * 16 + 8 * (vj & 1);
+  // K: which position is which column of S^T is chosen so that a lane's values 8 x .. 8 x + 7 are the eight positions KM x + 8 group + 0 .. 7
+  int kbase[M == 16 ? 2 : 1];
+#pragma unroll
+  for (int b = 0; b < (M == 16 ? 2 : 1); ++b) {
+    const int x = M == 16 ? (lane & 3) | (lane & 12) << 1 | b << 2 : (lane & 3) | (lane & 8) >> 1 | (lane & 4) << 1 | (lane & 16);
+    kbase[b] = x * W::ROWB + (RAW ? ((grp >> 1) ^ W::turn(x)) * 16 + 8 * (grp & 1) : (grp ^ W::turn(x)) * 16);
+  }
+  // V: 16 lanes read 4 (8, codes) positions x 16 columns, which come out as a column for each lane
+  const int vcol = M == 16 ? 0 : lane >> 4 & 1, vj = lane & 15;
+  int vbase[RAW ? 1 : 2];
+  if constexpr (RAW) {
+    const int x = 8 * grp + vj / 2;
+    vbase[0] = x * W::ROWB + (vcol ^ W::turn(x)) * 16 + 8 * (vj & 1);
   } else {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int x = 8 * (vgrp >> 1) + 4 * b + vj / 4;
-      vbase[b] = x * F::ROWB + ((2 * (vgrp & 1) + (vj >> 1 & 1)) ^ F::turn(x)) * 16 + 8 * (vj & 1);
+      const int x = 8 * grp + 4 * b + vj / 4;
+      vbase[b] = x * W::ROWB + ((2 * vcol + (vj >> 1 & 1)) ^ W::turn(x)) * 16 + 8 * (vj & 1);
     }
   }
 
+  // The codes of a stage to 16 bits, by the waves that share them.
+  auto widen = [&](int stage) {
+    const lds_char* const raw = (const lds_char*)(base + stage * STAGE);
+    const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(raw + 2 * TILE);
+    lds_char* const wide = (lds_char*)(base + 2 * STAGE);
+    const int me = rw * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < KT * F::CH / (64 * RW); ++i) {
+      const int y = i * 64 * RW + me, row = y / F::CH, piece = y % F::CH;
+      if (F::PIECES == F::CH || piece < F::PIECES) {
+        const int from = row * F::ROWB + (piece ^ F::turn(row)) * 16, to = row * W::ROWB + ((2 * piece) ^ W::turn(row)) * 16;
+        const u32x4_t kk = *(const __attribute__((address_space(3))) u32x4_t*)(raw + from), vv = *(const __attribute__((address_space(3))) u32x4_t*)(raw + TILE + from);
+        const float vs = DT == DT_F16 ? scales[KT + row] : 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int at = h == 0 ? to : to ^ 16;                        // the next piece
+          *(__attribute__((address_space(3))) u32x4_t*)(wide + at) = widen8<DT, KEPT>((u32x2_t){kk[2 * h], kk[2 * h + 1]});
+          u32x4_t v;
+          if constexpr (DT == DT_F16) {
+            const f32x4_t p0 = decode4<KEPT>(vv[2 * h]), p1 = decode4<KEPT>(vv[2 * h + 1]);
+            v = (u32x4_t){Half<DT>::pack(p0[0] * vs, p0[1] * vs), Half<DT>::pack(p0[2] * vs, p0[3] * vs), Half<DT>::pack(p1[0] * vs, p1[1] * vs),
+                          Half<DT>::pack(p1[2] * vs, p1[3] * vs)};
+          } else {
+            v = widen8<DT, KEPT>((u32x2_t){vv[2 * h], vv[2 * h + 1]});
+          }
+          *(__attribute__((address_space(3))) u32x4_t*)(wide + WTILE + at) = v;
+        }
+      }
+    }
+  };
+
   auto compute = [&](int t, unsigned ok, int stage) {
-    const lds_char* const kt = (const lds_char*)(base + stage * STAGE);
-    const lds_char* const vt = kt + TILE;
+    const lds_char* const kt = (const lds_char*)(base + (WIDE ? 2 * STAGE : stage * STAGE));
+    const lds_char* const vt = kt + WTILE;
     const int j0 = lo + t * KT;
     if (j0 >= khi_max || j0 + KT <= klo_min) return;                   // no row of this wave sees any of it
     // all pieces of K on their way before the first product
-    typedef std::conditional_t<CODES, u32x2_t, u32x4_t> raw_t;
+    typedef std::conditional_t<RAW, u32x2_t, u32x4_t> raw_t;
     raw_t kf[ST][KS];
 #pragma unroll
     for (int st = 0; st < ST; ++st)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) kf[st][k] = *(const __attribute__((address_space(3))) raw_t*)(kt + st * 32 * F::ROWB + (kbase ^ k * (CODES ? 16 : 32)));
+      for (int k = 0; k < KS; ++k) kf[st][k] = *(const __attribute__((address_space(3))) raw_t*)(kt + (M == 16 ? st / 2 : st) * 32 * W::ROWB + (kbase[M == 16 ? st & 1 : 0] ^ k * KM * W::ESZ));
     __builtin_amdgcn_sched_barrier(0);
-    f32x16_t z[ST];
+    acc sc[ST];
 #pragma unroll
     for (int st = 0; st < ST; ++st)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) z[st][e] = 0.f;
+      for (int e = 0; e < CA; ++e) sc[st][e] = 0.f;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int st = 0; st < ST; ++st) {
         u32x4_t w;
-        if constexpr (CODES) w = widen8<DT, KEPT>(kf[st][k]); else w = kf[st][k];
-        z[st] = Operand<DT>::mfma(__builtin_bit_cast(vec, w), q[k], z[st]);
+        if constexpr (RAW) w = widen8<DT, KEPT>(kf[st][k]); else w = kf[st][k];
+        sc[st] = P1::mfma(__builtin_bit_cast(vec, w), q[k], sc[st]);
       }
-    // V of step x: 16 positions
-    raw_t vf[2][DT32];
+    float z[NX][8];                                                    // position KM x + 8 group + e
+#pragma unroll
+    for (int x = 0; x < NX; ++x)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[x][e] = M == 16 ? sc[2 * x + e / 4][e % 4] : sc[x / 2][8 * (x & 1) + e];
+    // V of step x: KM positions
+    raw_t vf[2][DM];
     auto load_v = [&](int x) {
 #pragma unroll
-      for (int d = 0; d < DT32; ++d) {
-        if constexpr (CODES) {
+      for (int d = 0; d < DM; ++d) {
+        if constexpr (RAW) {
           typedef __attribute__((address_space(3))) i32x2_t L;
-          vf[x & 1][d] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((L*)(vt + x * 16 * F::ROWB + (vbase[0] ^ d * 32))));
+          vf[x & 1][d] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((L*)(vt + x * KM * W::ROWB + (vbase[0] ^ d * M))));
         } else {
           typedef __attribute__((address_space(3))) s16x4_t L;
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            const u32x2_t raw = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(vt + x * 16 * F::ROWB + (vbase[b] ^ d * 64))));
+            const u32x2_t raw = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(vt + x * KM * W::ROWB + (vbase[b] ^ d * 2 * M))));
             vf[x & 1][d][2 * b] = raw[0];
             vf[x & 1][d][2 * b + 1] = raw[1];
           }
         }
       }
     };
-    const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(vt + TILE);
+    const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(base + stage * STAGE + 2 * TILE);
     if constexpr (CODES) {
 #pragma unroll
-      for (int st = 0; st < ST; ++st)
+      for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-          const f32x4_t w = *(const __attribute__((address_space(3))) f32x4_t*)(scales + 32 * st + 16 * (f / 2) + 8 * half + 4 * (f & 1));
+        for (int f = 0; f < 2; ++f) {
+          const f32x4_t w = *(const __attribute__((address_space(3))) f32x4_t*)(scales + KM * x + 8 * grp + 4 * f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) z[st][4 * f + e] *= w[e] * kscale;
+          for (int e = 0; e < 4; ++e) z[x][4 * f + e] *= w[e];
         }
     }
     const bool partial = j0 + KT > min(khi_min, hi) || j0 < klo_max || ok != (1u << KT / 16) - 1;
@@ -352,29 +548,29 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
       unsigned long long there = 0;
 #pragma unroll
       for (int u = 0; u < KT / 16; ++u) there |= (ok >> u & 1 ? 0xFFFFull : 0ull) << (16 * u);
-      see = (see & there) >> (8 * half);
+      see = (see & there) >> (8 * grp);
 #pragma unroll
-      for (int st = 0; st < ST; ++st) {
-        const uint32_t w = (uint32_t)(see >> (32 * st));
+      for (int x = 0; x < NX; ++x) {
+        const uint32_t w = (uint32_t)(see >> (KM * x));
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[st][e] = w & (1u << (16 * (e / 8) + e % 8)) ? z[st][e] : -INFINITY;
+        for (int e = 0; e < 8; ++e) z[x][e] = w & (1u << e) ? z[x][e] : -INFINITY;
       }
     }
     float top = z[0][0];
 #pragma unroll
-    for (int st = 0; st < ST; ++st)
+    for (int x = 0; x < NX; ++x)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, z[st][e]);
-    top = pair_max(top);
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, z[x][e]);
+    top = row_max<M>(top);
     const bool grow = (top - m) * c2 > kSlack;                         // m = -infinity: whenever something is seen
     if (__any(grow)) {
       const float next = grow ? top : m;
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - next) * c2);
       sum *= keep;
 #pragma unroll
-      for (int d = 0; d < DT32; ++d)
+      for (int d = 0; d < DM; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] *= keep;
+        for (int e = 0; e < CA; ++e) o[d][e] *= keep;
       m = next;
       ref = m == -INFINITY ? 0.f : m * c2;
       far = __any(fabsf(ref) > 1e38f);
@@ -383,50 +579,50 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
     float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
     if (__builtin_expect(far, 0)) {
 #pragma unroll
-      for (int st = 0; st < ST; ++st)
+      for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[st][e] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((z[st][e] - m) * c2);
+        for (int e = 0; e < 8; ++e) z[x][e] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((z[x][e] - m) * c2);
     } else {
 #pragma unroll
-      for (int st = 0; st < ST; ++st)
+      for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[st][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[st][e], c2, -ref));
+        for (int e = 0; e < 8; ++e) z[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[x][e], c2, -ref));
     }
 #pragma unroll
-    for (int st = 0; st < ST; ++st)
+    for (int x = 0; x < NX; ++x)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) part_sum[e & 3] += z[st][e];
+      for (int e = 0; e < 8; ++e) part_sum[e & 3] += z[x][e];
     sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
-    if constexpr (CODES) {
+    if constexpr (SCALE_P) {
+      auto scale = [&](auto some) {                                    // the scale of a row that is not seen may be anything
 #pragma unroll
-      for (int st = 0; st < ST; ++st)
+        for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-          const f32x4_t w = *(const __attribute__((address_space(3))) f32x4_t*)(scales + KT + 32 * st + 16 * (f / 2) + 8 * half + 4 * (f & 1));
+          for (int f = 0; f < 2; ++f) {
+            const f32x4_t w = *(const __attribute__((address_space(3))) f32x4_t*)(scales + KT + KM * x + 8 * grp + 4 * f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = z[st][4 * f + e], y = p * w[e];
-            z[st][4 * f + e] = partial && p == 0.f ? 0.f : y;          // the scale of an unseen row may be anything
+            for (int e = 0; e < 4; ++e) z[x][4 * f + e] = some.value && z[x][4 * f + e] == 0.f ? 0.f : z[x][4 * f + e] * w[e];
           }
-        }
+      };
+      if (partial) scale(std::true_type{}); else scale(std::false_type{});
     }
 #pragma unroll
-    for (int x = 0; x < KT / 16; ++x) {
+    for (int x = 0; x < NX; ++x) {
       u32x4_t p, rest;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float a0 = z[x / 2][8 * (x & 1) + 2 * e], a1 = z[x / 2][8 * (x & 1) + 2 * e + 1];
+        const float a0 = z[x][2 * e], a1 = z[x][2 * e + 1];
         p[e] = Half<VDT>::pack(a0, a1);
         if constexpr (SPLIT_P) rest[e] = Half<VDT>::pack(a0 - bf16lo_to_f32(p[e]), a1 - bf16hi_to_f32(p[e]));
       }
-      if (x + 1 < KT / 16) load_v(x + 1);
+      if (x + 1 < NX) load_v(x + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int d = 0; d < DT32; ++d) {
+      for (int d = 0; d < DM; ++d) {
         u32x4_t w;
-        if constexpr (CODES) w = widen8<VDT, KEPT>(vf[x & 1][d]); else w = vf[x & 1][d];
-        o[d] = Operand<VDT>::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, p), o[d]);
-        if constexpr (SPLIT_P) o[d] = Operand<VDT>::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, rest), o[d]);
+        if constexpr (RAW) w = widen8<VDT, KEPT>(vf[x & 1][d]); else w = vf[x & 1][d];
+        o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, p), o[d]);
+        if constexpr (SPLIT_P) o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, rest), o[d]);
       }
     }
   };
@@ -441,20 +637,32 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
       const bool work = t < mine, more = t + 1 < mine;
       unsigned ok = 0;
       if (work) ok = exist(now);
-      if (more) {
+      auto ahead = [&] {
         fetch(kw + (t + 1) * KW, next, (t + 1) & 1);
         now = next;
         if (t + 2 < mine) next = look_up(kw + (t + 2) * KW);
-        wait_loads<2 * LOADS + (CODES ? 1 : 0)>();
-      } else {
+      };
+      if constexpr (WIDE) {
         wait_loads<0>();
+        meet();                                                        // the tile is there, and the one before has been used
+        if (more) ahead();
+        if (work) widen(t & 1);
+        wait_lds();
+        meet();
+      } else {
+        if (more) {
+          ahead();
+          wait_loads<2 * LOADS + (CODES ? 1 : 0)>();
+        } else {
+          wait_loads<0>();
+        }
+        if constexpr (RW > 1) meet();                                  // the others' parts of the tile are there as well
       }
-      if constexpr (RW > 1) meet();                                    // the others' parts of the tile are there as well
       __builtin_amdgcn_sched_barrier(0);
       if (work) compute(kw + t * KW, ok, t & 1);
       __builtin_amdgcn_sched_barrier(0);
       wait_lds();                                                      // nothing reads the stage that is filled next
-      if constexpr (RW > 1) meet();
+      if constexpr (RW > 1 && !WIDE) meet();
     }
   }
 
@@ -462,14 +670,14 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
   // term by term with the products left out.
   bool nan = false;
 #pragma unroll
-  for (int d = 0; d < DT32; ++d)
+  for (int d = 0; d < DM; ++d)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) nan |= o[d][e] != o[d][e];
+    for (int e = 0; e < CA; ++e) nan |= o[d][e] != o[d][e];
   if (__any(nan)) {
 #pragma unroll
-    for (int d = 0; d < DT32; ++d)
+    for (int d = 0; d < DM; ++d)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+      for (int e = 0; e < CA; ++e) o[d][e] = 0.f;
     for (int t = kw; t < count; t += KW)
       for (int j = lo + t * KT; j < min(lo + t * KT + KT, hi); ++j) {
         const long x = place_of(c, s, j, g);
@@ -481,23 +689,23 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
         for (int k = 0; k < KS; ++k) {
           const u32x4_t w = __builtin_bit_cast(u32x4_t, q[k]);
           u32x4_t kk;
-          if constexpr (CODES) kk = widen8<DT, KEPT>(*(const u32x2_t*)((const char*)a.kc + x * D + 16 * k + 8 * half));
-          else kk = *(const u32x4_t*)((const char*)a.kc + (x * D + 16 * k + 8 * half) * 2);
+          if constexpr (CODES) kk = widen8<DT, KEPT>(*(const u32x2_t*)((const char*)a.kc + x * D + KM * k + 8 * grp));
+          else kk = *(const u32x4_t*)((const char*)a.kc + (x * D + KM * k + 8 * grp) * 2);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const f32x2_t u = Half<DT>::unpack(w[e]), v = Half<DT>::unpack(kk[e]);
             y += u[0] * v[0] + u[1] * v[1];
           }
         }
-        y = pair_sum(y);
-        if constexpr (CODES) y *= a.ks[x] * kscale;
+        y = row_sum<M>(y);
+        if constexpr (CODES) y *= a.ks[x];
         float p = __builtin_amdgcn_exp2f((y - m) * c2);
         if constexpr (CODES) p *= a.vs[x];
 #pragma unroll
-        for (int d = 0; d < DT32; ++d)
+        for (int d = 0; d < DM; ++d)
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const long from = x * D + 32 * d + 8 * b + 4 * half;
+          for (int b = 0; b < CA / 4; ++b) {
+            const long from = x * D + M * d + 8 * b + 4 * grp;
             float v[4];
             if constexpr (CODES) {
               const f32x4_t f = decode4<KEPT>(*(const uint32_t*)((const char*)a.vc + from));
@@ -512,137 +720,194 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 4 && RW == 1 ? 1 : 2) void
           }
       }
   }
-  sum = pair_sum(sum);
+  sum = row_sum<M>(sum);
   m *= unit;                                             // in units of the scores
 
   // ---- the waves that shared the rows
   if constexpr (KW > 1) {
-    constexpr int SLOT = D * 32 * 4 + 512;                             // sums, then references and sums of p of a wave's lanes
+    constexpr int SLOT = D * M * 4 + 512;                              // sums, then references and sums of p of a wave's lanes
     __syncthreads();
     if (kw > 0) {
       char* const to = smem + ((kw - 1) * RW + rw) * SLOT;
 #pragma unroll
-      for (int d = 0; d < DT32; ++d)
+      for (int d = 0; d < DM; ++d)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) *(f32x4_t*)(to + (d * 4 + b) * 1024 + lane * 16) = (f32x4_t){o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
-      *(float*)(to + D * 128 + lane * 4) = m;
-      *(float*)(to + D * 128 + 256 + lane * 4) = sum;
+        for (int b = 0; b < CA / 4; ++b) *(f32x4_t*)(to + (d * (CA / 4) + b) * 1024 + lane * 16) = (f32x4_t){o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+      *(float*)(to + D * M * 4 + lane * 4) = m;
+      *(float*)(to + D * M * 4 + 256 + lane * 4) = sum;
     }
     __syncthreads();
-    if (kw > 0) return;
+    if (kw == 0) {
 #pragma unroll
-    for (int w = 0; w < KW - 1; ++w) {
-      const char* const from = smem + (w * RW + rw) * SLOT;
-      const float m2 = *(const float*)(from + D * 128 + lane * 4), s2 = *(const float*)(from + D * 128 + 256 + lane * 4);
-      const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-      const float f1 = __builtin_amdgcn_exp2f((m - ref) * kLog2E), f2 = __builtin_amdgcn_exp2f((m2 - ref) * kLog2E);
-      sum = sum * f1 + s2 * f2;
+      for (int w = 0; w < KW - 1; ++w) {
+        const char* const other = smem + (w * RW + rw) * SLOT;
+        const float m2 = *(const float*)(other + D * M * 4 + lane * 4), s2 = *(const float*)(other + D * M * 4 + 256 + lane * 4);
+        const float top = fmaxf(m, m2), zero = top == -INFINITY ? 0.f : top;
+        const float f1 = __builtin_amdgcn_exp2f((m - zero) * kLog2E), f2 = __builtin_amdgcn_exp2f((m2 - zero) * kLog2E);
+        sum = sum * f1 + s2 * f2;
 #pragma unroll
-      for (int d = 0; d < DT32; ++d)
+        for (int d = 0; d < DM; ++d)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const f32x4_t v = *(const f32x4_t*)(from + (d * 4 + b) * 1024 + lane * 16);
+          for (int b = 0; b < CA / 4; ++b) {
+            const f32x4_t v = *(const f32x4_t*)(other + (d * (CA / 4) + b) * 1024 + lane * 16);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[d][4 * b + e] = o[d][4 * b + e] * f1 + v[e] * f2;
-        }
-      m = top;
+            for (int e = 0; e < 4; ++e) o[d][4 * b + e] = o[d][4 * b + e] * f1 + v[e] * f2;
+          }
+        m = top;
+      }
     }
   }
-  if (!has) return;
-  if (sp.chunks > 1) {
-    const long row = ((long)chunk * c.T + t_row) * a.heads + head;
+  if (kw == 0 && has) {
+    if (whole) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint16_t* const out = (uint16_t*)a.out + t_row * a.out_pitch + (long)head * D;
 #pragma unroll
-    for (int d = 0; d < DT32; ++d)
+      for (int d = 0; d < DM; ++d)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) *(f32x4_t*)(part + row * D + 32 * d + 8 * b + 4 * half) = (f32x4_t){o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
-    if (half == 0) stat[row] = (f32x2_t){m, sum};
-    return;
+        for (int b = 0; b < CA / 4; ++b)
+          *(u32x2_t*)(out + M * d + 8 * b + 4 * grp) = (u32x2_t){Half<DT>::pack(o[d][4 * b] * inv, o[d][4 * b + 1] * inv), Half<DT>::pack(o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv)};
+      if (a.lse && grp == 0) a.lse[(long)t_row * a.heads + head] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
+    } else {
+      // a share begins inside at most one item and ends inside at most one other
+      const long row = (long)(2 * share + (from > 0 ? 0 : 1)) * TR + (r - r0);
+#pragma unroll
+      for (int d = 0; d < DM; ++d)
+#pragma unroll
+        for (int b = 0; b < CA / 4; ++b) *(f32x4_t*)(part + row * D + M * d + 8 * b + 4 * grp) = (f32x4_t){o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+      if (grp == 0) stat[row] = (f32x2_t){m, sum};
+    }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint16_t* const out = (uint16_t*)a.out + t_row * a.out_pitch + (long)head * D;
-#pragma unroll
-  for (int d = 0; d < DT32; ++d)
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-      *(u32x2_t*)(out + 32 * d + 8 * b + 4 * half) = (u32x2_t){Half<DT>::pack(o[d][4 * b] * inv, o[d][4 * b + 1] * inv), Half<DT>::pack(o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv)};
-  if (a.lse && half == 0) a.lse[(long)t_row * a.heads + head] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
+  if (x >= x_end) return;
+  __syncthreads();                                                     // the tiles' LDS is used again
+  p = find<false>(c, a, sp, x);
+  }
 }
 
-// Joins the chunks of a row, a wave per row and head; the chunks that touch what the row can see are the ones that were written for it.
-template <int DT, int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(Paged c, Attend a, Split sp, const float* __restrict__ part, const f32x2_t* __restrict__ stat) {
-  const int lane = threadIdx.x & 63;
-  const long x = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (x >= (long)c.T * a.heads) return;
-  const int t = (int)(x / a.heads), head = (int)(x % a.heads);
-  const int s = seq_of(c.start, c.S, t);
-  if (s < 0 || s >= c.S) return;
-  const int n = c.start[s + 1] - c.start[s], i = t - c.start[s];
-  const Range range = seen_range(c, a, tokens_before(c.length[s], n), n, i, i);
-  const int first = range.lo / sp.clen, last = range.lo < range.hi ? (range.hi - 1) / sp.clen : first - 1;
-  float m = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int k = first; k <= last; ++k) {
-    const long row = ((long)k * c.T + t) * a.heads + head;
-    const f32x2_t w = stat[row];
-    const float p0 = lane * 2 < D ? part[row * D + lane * 2] : 0.f, p1 = lane * 2 < D ? part[row * D + lane * 2 + 1] : 0.f;
-    const float top = fmaxf(m, w[0]), ref = top == -INFINITY ? 0.f : top;
-    const float f1 = __builtin_amdgcn_exp2f((m - ref) * kLog2E), f2 = __builtin_amdgcn_exp2f((w[0] - ref) * kLog2E);
-    sum = sum * f1 + w[1] * f2;
-    o0 = o0 * f1 + p0 * f2;
-    o1 = o1 * f1 + p1 * f2;
-    m = top;
+// Adds up the items in several pieces, 32 lanes a row's sums from one piece: ROWS = 8, a row each for few pieces; ROWS = 1, every eighth piece of the
+// same row for many.  Eight pieces are on their way at once.
+constexpr int JT = 256;
+template <int DT, int D, int ROWS>
+__global__ __launch_bounds__(JT) void attend_join_kernel(Attend a, int T, int G, int tile_rows, int shares, const float* __restrict__ part, const f32x2_t* __restrict__ stat,
+                                                         const Joined* __restrict__ joined, const int* __restrict__ joined_count) {
+  constexpr int PARTS = JT / 32 / ROWS;
+  __shared__ f32x4_t sums[PARTS][32];
+  __shared__ float totals[PARTS];
+  const int at = threadIdx.x & 31, group = threadIdx.x / 32, in_tile = blockIdx.y * ROWS + (ROWS == 1 ? 0 : group), mine = ROWS == 1 ? group : 0;
+  if ((int)blockIdx.x >= *joined_count) return;
+  const Joined it = joined[blockIdx.x];
+  const int r = it.r0 + in_tile;
+  if (it.pieces == 0 || r >= it.rows) return;          // ROWS == 1: all threads alike
+  const int t = it.row0 + r / G, head = it.head0 + r % G;
+  // a record that nobody wrote, where `start` does not ascend, leads nowhere
+  if (it.pieces < 0 || it.share < 0 || it.pieces > shares - it.share || r < 0 || t < 0 || t >= T || it.head0 < 0 || it.head0 > a.heads - G) return;
+  auto row_of = [&](int k) { return (long)(2 * (it.share + k) + (k == 0 ? 1 : 0)) * tile_rows + in_tile; };
+  float m = -INFINITY;
+  for (int k = at; k < it.pieces; k += 32) m = fmaxf(m, stat[row_of(k)][0]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float zero = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = mine; k0 < it.pieces; k0 += 8 * PARTS) {
+    f32x2_t st[8];
+    f32x4_t v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const long row = row_of(min(k0 + k * PARTS, it.pieces - 1));
+      st[k] = stat[row];
+      v[k] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      if (at * 4 < D) v[k] = *(const f32x4_t*)(part + row * D + at * 4);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool has = k0 + k * PARTS < it.pieces;
+      const float f = has ? __builtin_amdgcn_exp2f((st[k][0] - zero) * kLog2E) : 0.f;
+      sum += has ? st[k][1] * f : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += has ? v[k][e] * f : 0.f;
+    }
+  }
+  if constexpr (PARTS > 1) {
+    sums[mine][at] = o;
+    if (at == 0) totals[mine] = sum;
+    __syncthreads();
+    if (mine > 0) return;
+#pragma unroll
+    for (int k = 1; k < PARTS; ++k) {
+      sum += totals[k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += sums[k][at][e];
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  if (lane * 2 < D) *(uint32_t*)((uint16_t*)a.out + t * a.out_pitch + (long)head * D + lane * 2) = Half<DT>::pack(o0 * inv, o1 * inv);
-  if (a.lse && lane == 0) a.lse[x] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
+  if (at * 4 < D)
+    *(u32x2_t*)((uint16_t*)a.out + t * a.out_pitch + (long)head * D + at * 4) = (u32x2_t){Half<DT>::pack(o[0] * inv, o[1] * inv), Half<DT>::pack(o[2] * inv, o[3] * inv)};
+  if (a.lse && at == 0) a.lse[(long)t * a.heads + head] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
 }
 
 // ---- the rule for the form of the workgroups and the split
-struct Plan { int rw, tiles; Split sp; };
+#ifndef LEAST
+#define LEAST 2
+#define PLAIN 512
+#define SHARES16 512
+#define SHARES32 512
+#endif
+struct Plan { int width, rw; Split sp; unsigned grid; bool many; };     // many: pieces for an item
 
 Plan plan_of(const Paged& c, int heads, int max_len) {
   const long G = heads / c.H, rows = (long)c.T * G, mean = (rows + c.S - 1) / c.S;
   Plan p;
+  p.width = mean <= 16 ? 16 : 32;
   p.rw = mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
-  const int TR = 32 * p.rw;
-  p.tiles = (int)(rows / TR + c.S);
-  const long groups = (long)p.tiles * c.H;
-  const long want = p.rw == 4 ? 512 : 2048, least = p.rw == 4 ? 1024 : 512;
-  long chunks = (want + groups - 1) / groups;
-  const long most = (max_len + least - 1) / least;
-  chunks = chunks < most ? chunks : most;
-  const long clen = ((max_len + chunks - 1) / chunks + 127) / 128 * 128;
-  p.sp.clen = (int)clen;
-  p.sp.chunks = (int)((max_len + clen - 1) / clen);
+  const int TR = p.width * p.rw;
+  p.sp.rows = TR;
+  p.sp.unit = p.rw == 1 ? 128 : 64;
+  p.sp.tiles = (int)(rows / TR + c.S);               // at most: a sequence begins a tile
+  p.sp.least = LEAST;
+  const long items = (long)p.sp.tiles * c.H, units = (max_len + p.sp.unit - 1) / p.sp.unit;
+  // beyond some rounds of workgroups the items even out by themselves; the units are counted in 32 bits
+  const bool share = (mean <= 128 || items < PLAIN) && (double)items * units < 2e9;
+  p.sp.shares = share ? (p.width == 16 ? SHARES16 : SHARES32) : 0;
+  p.sp.by_item = items <= p.sp.shares;
+  p.sp.joins = p.sp.by_item ? (int)items : p.sp.shares;
+  p.many = p.sp.shares >= 8 * items;
+  p.grid = share ? p.sp.shares : (unsigned)items;
   return p;
 }
 
-size_t part_bytes(const Paged& c, int heads, const Split& sp) { return ((size_t)sp.chunks * c.T * heads * c.D * sizeof(float) + 255) / 256 * 256; }
+size_t part_bytes(const Paged& c, const Split& sp) { return (size_t)2 * sp.shares * sp.rows * c.D * sizeof(float); }
 
-template <int DT, int KEPT, int D, int RW, int KW, int KT>
+template <int DT, int KEPT, int D, int M, int RW, int KW, int KT>
 hipError_t launch_form(const Paged& c, const Attend& a, const Plan& p, void* ws, hipStream_t stream) {
   typedef Form<DT, KEPT, D> F;
-  constexpr size_t stage = 2 * KT * F::ROWB + (KEPT != DT ? 8 * KT : 0), slots = (size_t)(KW - 1) * RW * (D * 128 + 512);
-  constexpr size_t lds = 2 * KW * stage > slots ? 2 * KW * stage : slots;
+  constexpr size_t stage = 2 * KT * F::ROWB + (KEPT != DT ? 8 * KT : 0), wide = KEPT != DT && RW > 1 ? 2 * KT * Form<DT, DT, D>::ROWB : 0, slots = (size_t)(KW - 1) * RW * (D * M * 4 + 512);
+  constexpr size_t tiles = KW * (2 * stage + wide), lds = tiles > slots ? tiles : slots;
   static PerDeviceInt raised;
-  hipError_t e = ensure_dynamic_lds(raised, (const void*)attend_kernel<DT, KEPT, D, RW, KW, KT>, lds);
+  hipError_t e = ensure_dynamic_lds(raised, (const void*)attend_kernel<DT, KEPT, D, M, RW, KW, KT>, lds);
   if (e != hipSuccess) return e;
   float* part = (float*)ws;
-  f32x2_t* stat = (f32x2_t*)((char*)ws + part_bytes(c, a.heads, p.sp));
-  const unsigned grid = (unsigned)p.tiles * c.H * p.sp.chunks;
-  hipLaunchKernelGGL((attend_kernel<DT, KEPT, D, RW, KW, KT>), dim3(grid), dim3(64 * RW * KW), lds, stream, c, a, p.sp, p.tiles, part, stat);
-  if ((e = hipGetLastError()) != hipSuccess || p.sp.chunks == 1) return e;
-  const unsigned joins = (unsigned)(((long)c.T * a.heads + 3) / 4);
-  hipLaunchKernelGGL((attend_join_kernel<DT, D>), dim3(joins), dim3(256), 0, stream, c, a, p.sp, (const float*)part, (const f32x2_t*)stat);
+  f32x2_t* stat = (f32x2_t*)((char*)ws + part_bytes(c, p.sp));
+  Joined* joined = (Joined*)(stat + (size_t)2 * p.sp.shares * p.sp.rows);
+  int* joined_count = (int*)(joined + p.sp.joins);
+  hipLaunchKernelGGL((attend_kernel<DT, KEPT, D, M, RW, KW, KT>), dim3(p.grid), dim3(64 * RW * KW), lds, stream, c, a, p.sp, part, stat, joined, joined_count);
+  if ((e = hipGetLastError()) != hipSuccess || p.sp.shares == 0) return e;
+  const int G = a.heads / c.H;
+  if (p.many)
+    hipLaunchKernelGGL((attend_join_kernel<DT, D, 1>), dim3((unsigned)p.sp.joins, p.sp.rows), dim3(JT), 0, stream, a, c.T, G, p.sp.rows, p.sp.shares, (const float*)part, (const f32x2_t*)stat,
+                       (const Joined*)joined, (const int*)joined_count);
+  else
+    hipLaunchKernelGGL((attend_join_kernel<DT, D, 8>), dim3((unsigned)p.sp.joins, p.sp.rows / 8), dim3(JT), 0, stream, a, c.T, G, p.sp.rows, p.sp.shares, (const float*)part, (const f32x2_t*)stat,
+                       (const Joined*)joined, (const int*)joined_count);
   return hipGetLastError();
 }
 
 template <int DT, int KEPT, int D>
 hipError_t launch_attend_d(const Paged& c, const Attend& a, void* ws, hipStream_t stream) {
   const Plan p = plan_of(c, a.heads, a.max_len);
-  if (p.rw == 1) return launch_form<DT, KEPT, D, 1, 4, 32>(c, a, p, ws, stream);
-  if (p.rw == 2) return launch_form<DT, KEPT, D, 2, 2, 32>(c, a, p, ws, stream);
-  return launch_form<DT, KEPT, D, 4, 1, 64>(c, a, p, ws, stream);
+  if (p.width == 16) return launch_form<DT, KEPT, D, 16, 1, 4, 32>(c, a, p, ws, stream);
+  if (p.rw == 1) return launch_form<DT, KEPT, D, 32, 1, 4, 32>(c, a, p, ws, stream);
+  if (p.rw == 2) return launch_form<DT, KEPT, D, 32, 2, 2, 32>(c, a, p, ws, stream);
+  return launch_form<DT, KEPT, D, 32, 4, 1, 64>(c, a, p, ws, stream);
 }
 
 template <int DT, int KEPT>
@@ -665,8 +930,7 @@ hipError_t launch_attend_t(const Paged& c, const Attend& a, void* ws, hipStream_
 
 size_t attend_workspace_bytes(const Paged& c, int heads, int max_len) {
   const Plan p = plan_of(c, heads, max_len);
-  if (p.sp.chunks == 1) return 256;
-  return part_bytes(c, heads, p.sp) + (size_t)p.sp.chunks * c.T * heads * sizeof(f32x2_t);
+  return p.sp.shares == 0 ? 256 : part_bytes(c, p.sp) + (size_t)2 * p.sp.shares * p.sp.rows * sizeof(f32x2_t) + p.sp.joins * sizeof(Joined) + sizeof(int);
 }
 
 hipError_t launch_attend(const Paged& c, const Attend& a, void* ws, hipStream_t stream) {
