@@ -486,7 +486,8 @@ int covspec_cache_read(const covspec_cache_params* p, const void* k_cache, const
  *   lse_out [n_tokens, n_heads] fp32 log sum_j exp(scale * q . k_j), or NULL
  * max_len (HOST) bounds the lengths: it sizes the grid and the workspace; positions at or beyond it are not seen.
  * Products are taken of 16-bit values with fp32 sums (8-bit codes are exact in 16 bits; their scales enter in fp32),
- * softmax statistics are fp32, p is rounded to 16 bits for its product with v.  The same call gives the same bits.
+ * softmax statistics are fp32, p is rounded to 16 bits for its product with v, and v = code * scale of an 8-bit cache may be.  The
+ * same call gives the same bits.
  * Limits: those of the cache (its row_pitch is not used); n_heads a multiple of n_kv_heads, at most 64 times it;
  * n_tokens * n_heads below 2^30; max_len from 1 to max_pages * page_size; window >= 0; scale finite.  Workspace:
  * covspec_attend_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on `stream`,

@@ -233,6 +233,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
   constexpr bool SPLIT_P = CODES && !WIDE && DT == DT_F16, SCALE_P = CODES && !(WIDE && DT == DT_F16);
   typedef Form<DT, WIDE ? DT : KEPT, D> W;               // of the tiles that are multiplied
   constexpr bool RAW = CODES && !WIDE;
+  constexpr bool TURNS = RW == 8;                        // see the loop over the tiles
+  static_assert(!TURNS || (KW == 1 && KT == 64 && !CODES), "");
   typedef Operand<DT, M> P1;
   typedef Operand<VDT, M> P2;
   typedef typename P1::vec vec;
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
   constexpr int NG = 64 / M, KM = 8 * NG, CA = M * M / 64;               // lanes of a row; terms of a product; values of a result in a lane
   constexpr int TR = M * RW, DM = D / M, KS = D / KM, ST = KT / M, NX = KT / KM;
   constexpr int TILE = KT * F::ROWB, STAGE = 2 * TILE + (CODES ? 8 * KT : 0);
-  constexpr int WTILE = KT * W::ROWB, GROUP = 2 * STAGE + (WIDE ? 2 * WTILE : 0);
+  constexpr int WTILE = KT * W::ROWB, GROUP = (TURNS ? 4 : 2) * STAGE + (WIDE ? 2 * WTILE : 0);
   constexpr int LOADS = KT / F::RPI / RW;                // of a wave, for one of K and V
   static_assert(LOADS >= 1 && 2 * LOADS + 1 < 63 && D % KM == 0 && KT % KM == 0 && KT % 32 == 0 && KT <= 64, "");
   extern __shared__ __align__(1024) char smem[];
@@ -474,56 +476,68 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
     }
   };
 
-  auto compute = [&](int t, unsigned ok, int stage) {
+  // A tile in three steps: the scores, the probabilities, the sums of v.
+  typedef std::conditional_t<RAW, u32x2_t, u32x4_t> raw_t;
+  float z[NX][8];                                                      // position KM x + 8 group + e
+  u32x4_t prob[NX], rest[SPLIT_P ? NX : 1];
+  auto seen = [&](int t) { const int j0 = lo + t * KT; return j0 < khi_max && j0 + KT > klo_min; };       // by any row of this wave
+  raw_t kf[ST][KS];
+  auto load_k = [&](int stage, int st) {
     const lds_char* const kt = (const lds_char*)(base + (WIDE ? 2 * STAGE : stage * STAGE));
-    const lds_char* const vt = kt + WTILE;
-    const int j0 = lo + t * KT;
-    if (j0 >= khi_max || j0 + KT <= klo_min) return;                   // no row of this wave sees any of it
-    // all pieces of K on their way before the first product
-    typedef std::conditional_t<RAW, u32x2_t, u32x4_t> raw_t;
-    raw_t kf[ST][KS];
 #pragma unroll
-    for (int st = 0; st < ST; ++st)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) kf[st][k] = *(const __attribute__((address_space(3))) raw_t*)(kt + (M == 16 ? st / 2 : st) * 32 * W::ROWB + (kbase[M == 16 ? st & 1 : 0] ^ k * KM * W::ESZ));
-    __builtin_amdgcn_sched_barrier(0);
-    acc sc[ST];
+    for (int k = 0; k < KS; ++k) kf[st][k] = *(const __attribute__((address_space(3))) raw_t*)(kt + (M == 16 ? st / 2 : st) * 32 * W::ROWB + (kbase[M == 16 ? st & 1 : 0] ^ k * KM * W::ESZ));
+  };
+  acc sc[ST];
+  auto multiply_k = [&](int st, int k) {
+    u32x4_t w;
+    if constexpr (RAW) w = widen8<DT, KEPT>(kf[st][k]); else w = kf[st][k];
+    sc[st] = P1::mfma(__builtin_bit_cast(vec, w), q[k], sc[st]);
+  };
+  auto clear_scores = [&] {
 #pragma unroll
     for (int st = 0; st < ST; ++st)
 #pragma unroll
       for (int e = 0; e < CA; ++e) sc[st][e] = 0.f;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int st = 0; st < ST; ++st) {
-        u32x4_t w;
-        if constexpr (RAW) w = widen8<DT, KEPT>(kf[st][k]); else w = kf[st][k];
-        sc[st] = P1::mfma(__builtin_bit_cast(vec, w), q[k], sc[st]);
-      }
-    float z[NX][8];                                                    // position KM x + 8 group + e
+  };
+  auto take_scores = [&] {
 #pragma unroll
     for (int x = 0; x < NX; ++x)
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[x][e] = M == 16 ? sc[2 * x + e / 4][e % 4] : sc[x / 2][8 * (x & 1) + e];
-    // V of step x: KM positions
-    raw_t vf[2][DM];
-    auto load_v = [&](int x) {
+  };
+  auto scores = [&](int stage) {
+    // all pieces of K on their way before the first product
 #pragma unroll
-      for (int d = 0; d < DM; ++d) {
-        if constexpr (RAW) {
-          typedef __attribute__((address_space(3))) i32x2_t L;
-          vf[x & 1][d] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((L*)(vt + x * KM * W::ROWB + (vbase[0] ^ d * M))));
-        } else {
-          typedef __attribute__((address_space(3))) s16x4_t L;
+    for (int st = 0; st < ST; ++st) load_k(stage, st);
+    __builtin_amdgcn_sched_barrier(0);
+    clear_scores();
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const u32x2_t raw = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(vt + x * KM * W::ROWB + (vbase[b] ^ d * 2 * M))));
-            vf[x & 1][d][2 * b] = raw[0];
-            vf[x & 1][d][2 * b + 1] = raw[1];
-          }
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int st = 0; st < ST; ++st) multiply_k(st, k);
+    take_scores();
+  };
+  raw_t vf[2][DM];                                                     // V of step x, KM positions, and of the next
+  auto load_v = [&](int stage, int x) {
+    const lds_char* const vt = (const lds_char*)(base + (WIDE ? 2 * STAGE : stage * STAGE)) + WTILE;
+#pragma unroll
+    for (int d = 0; d < DM; ++d) {
+      if constexpr (RAW) {
+        typedef __attribute__((address_space(3))) i32x2_t L;
+        vf[x & 1][d] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((L*)(vt + x * KM * W::ROWB + (vbase[0] ^ d * M))));
+      } else {
+        typedef __attribute__((address_space(3))) s16x4_t L;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const u32x2_t raw = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(vt + x * KM * W::ROWB + (vbase[b] ^ d * 2 * M))));
+          vf[x & 1][d][2 * b] = raw[0];
+          vf[x & 1][d][2 * b + 1] = raw[1];
         }
       }
-    };
+    }
+  };
+  auto probabilities = [&](int t, unsigned ok, int stage, auto early) {
+    const int j0 = lo + t * KT;
     const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(base + stage * STAGE + 2 * TILE);
     if constexpr (CODES) {
 #pragma unroll
@@ -575,7 +589,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       ref = m == -INFINITY ? 0.f : m * c2;
       far = __any(fabsf(ref) > 1e38f);
     }
-    load_v(0);
+    early();                                                           // what is loaded while the exponentials are taken
     float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
     if (__builtin_expect(far, 0)) {
 #pragma unroll
@@ -607,27 +621,99 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       if (partial) scale(std::true_type{}); else scale(std::false_type{});
     }
 #pragma unroll
-    for (int x = 0; x < NX; ++x) {
-      u32x4_t p, rest;
+    for (int x = 0; x < NX; ++x)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float a0 = z[x][2 * e], a1 = z[x][2 * e + 1];
-        p[e] = Half<VDT>::pack(a0, a1);
-        if constexpr (SPLIT_P) rest[e] = Half<VDT>::pack(a0 - bf16lo_to_f32(p[e]), a1 - bf16hi_to_f32(p[e]));
+        prob[x][e] = Half<VDT>::pack(a0, a1);
+        if constexpr (SPLIT_P) rest[x][e] = Half<VDT>::pack(a0 - bf16lo_to_f32(prob[x][e]), a1 - bf16hi_to_f32(prob[x][e]));
       }
-      if (x + 1 < NX) load_v(x + 1);
-      __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply_v = [&](int x) {
 #pragma unroll
-      for (int d = 0; d < DM; ++d) {
-        u32x4_t w;
-        if constexpr (RAW) w = widen8<VDT, KEPT>(vf[x & 1][d]); else w = vf[x & 1][d];
-        o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, p), o[d]);
-        if constexpr (SPLIT_P) o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, rest), o[d]);
-      }
+    for (int d = 0; d < DM; ++d) {
+      u32x4_t w;
+      if constexpr (RAW) w = widen8<VDT, KEPT>(vf[x & 1][d]); else w = vf[x & 1][d];
+      o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, prob[x]), o[d]);
+      if constexpr (SPLIT_P) o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, rest[x]), o[d]);
+    }
+  };
+  auto sums = [&](int stage) {                                         // the first step is on its way
+#pragma unroll
+    for (int x = 0; x < NX; ++x) {
+      if (x + 1 < NX) load_v(stage, x + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply_v(x);
     }
   };
 
-  if (count > 0) {
+  if constexpr (TURNS) {
+    // Two waves on every SIMD, one of each half of the workgroup, take turns: while one multiplies (the sums of a tile, the scores of the next), the
+    // other exponentiates.  Slot 2 t: the first half multiplies for tile t, the second has the probabilities of tile t - 1; then the other way round.
+    // Tile t is read in the slots 2 t .. 2 t + 3 and sent for in slot 2 t - 4, when the tile four before it has been used.
+    const bool second = rw >= RW / 2;
+    Pages next;
+    unsigned ring = 0;                                                 // what exists of the tiles in the four stages
+    int sent = 0;
+    auto send = [&] {
+      if (sent < count) {
+        ring = (ring & ~(15u << 4 * (sent & 3))) | exist(next) << 4 * (sent & 3);
+        fetch(sent, next, sent & 3);
+        ++sent;
+        if (sent < count) next = look_up(sent);
+      }
+    };
+    auto arrived = [&](int t) {                                        // tile t, of which at most the next one is sent behind it
+      if (sent > t + 1) wait_loads<2 * LOADS>(); else wait_loads<0>();
+    };
+    auto slot = [&] {
+      __builtin_amdgcn_sched_barrier(0);
+      wait_lds();                                                      // nothing of a stage is still being read
+      meet();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    if (count > 0) {
+      next = look_up(0);
+      send();
+      send();
+      arrived(0);
+      slot();
+      if (second) {
+        send();
+        slot();
+      }
+      for (int t = 0; t < count; ++t) {
+        if (!second) send();
+        // the first half of K on its way before the products with V, the second before those with the first
+        load_k(t & 3, 0);
+        if (t > 0 && seen(t - 1)) {
+          load_v((t - 1) & 3, 0);
+          sums((t - 1) & 3);
+        }
+        load_k(t & 3, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        clear_scores();
+#pragma unroll
+        for (int st = 0; st < ST; ++st)
+#pragma unroll
+          for (int k = 0; k < KS; ++k) multiply_k(st, k);
+        take_scores();
+        if (second) arrived(t + 1);
+        slot();
+        if (second) send();
+        if (seen(t)) {
+          probabilities(t, ring >> 4 * (t & 3) & 15, t & 3, [] {});
+        }
+        if (!second) arrived(t + 1);
+        slot();
+      }
+      if (!second) slot();
+      if (seen(count - 1)) {
+        load_v((count - 1) & 3, 0);
+        sums((count - 1) & 3);
+      }
+    }
+  } else if (count > 0) {
     // tile t of the group's: fetched while the one before is computed.  All waves of a workgroup meet as often as the group with most tiles needs.
     const int mine = kw < count ? (count - kw + KW - 1) / KW : 0, most = (count + KW - 1) / KW;
     Pages now, next;
@@ -659,7 +745,11 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
         if constexpr (RW > 1) meet();                                  // the others' parts of the tile are there as well
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (work) compute(kw + t * KW, ok, t & 1);
+      if (work && seen(kw + t * KW)) {
+        scores(t & 1);
+        probabilities(kw + t * KW, ok, t & 1, [&] { load_v(t & 1, 0); });
+        sums(t & 1);
+      }
       __builtin_amdgcn_sched_barrier(0);
       wait_lds();                                                      // nothing reads the stage that is filled next
       if constexpr (RW > 1 && !WIDE) meet();
@@ -845,33 +935,38 @@ __global__ __launch_bounds__(JT) void attend_join_kernel(Attend a, int T, int G,
   if (a.lse && at == 0) a.lse[(long)t * a.heads + head] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
 }
 
-// ---- the rule for the form of the workgroups and the split
-#ifndef LEAST
-#define LEAST 2
-#define PLAIN 512
-#define SHARES16 512
-#define SHARES32 512
-#endif
+// ---- the rule for the form of the workgroups and the split, by the rows of a sequence (tokens x heads for each key head) in the mean.
+// Tiles of 16 rows up to 16, of 32 (64, 128) up to 32 (64, any more); us for 64 x 8192 positions of a 16-bit cache, 8 key heads: 4 rows for each in
+// 16-row tiles 352, in 32-row tiles 372; 64 rows 357, 88 rows 397, all near the 370 that the bytes take at 5.8 TB/s.
+// 256 rows whose waves take turns (16-bit caches) from 512 on, where the workgroups, one on a compute unit, are shares or many: 512 tokens behind 32256
+// 587 instead of 658 with 128 rows, 1024 behind 15360 565 instead of 626, prompts of 4 x 3008 741 instead of 752; but 376 items, one prompt of
+// 3000, 113 instead of 107.
+// Shares for few rows, and where a workgroup per item would not fill the device once: 256 tokens behind 32512 (128 items of 128 rows) 361 instead of 909, 512 (256)
+// 675 instead of 905; 544 items of a window over several sequences 181 instead of 112, as their tiles' workgroups no longer read the same positions
+// at the same time.
 struct Plan { int width, rw; Split sp; unsigned grid; bool many; };     // many: pieces for an item
 
 Plan plan_of(const Paged& c, int heads, int max_len) {
   const long G = heads / c.H, rows = (long)c.T * G, mean = (rows + c.S - 1) / c.S;
+  const long wide_items = (rows / 256 + c.S) * c.H;
   Plan p;
   p.width = mean <= 16 ? 16 : 32;
-  p.rw = mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
+  p.rw = mean <= 32 ? 1 : mean <= 64 ? 2 : c.kept == c.dtype && mean >= 512 && (wide_items <= 256 || wide_items >= 1024) ? 8 : 4;
   const int TR = p.width * p.rw;
   p.sp.rows = TR;
-  p.sp.unit = p.rw == 1 ? 128 : 64;
+  p.sp.unit = p.rw == 1 ? 128 : 64;                  // a tile for each wave that takes tiles of its own
+  p.sp.least = 2;                                    // a share's own beginning and end cost some units' time
   p.sp.tiles = (int)(rows / TR + c.S);               // at most: a sequence begins a tile
-  p.sp.least = LEAST;
+  // as many shares as are at work at once: one or two on each of 256 compute units, by the LDS and registers of the form
+  const bool alone = p.rw == 8 || (p.width == 16 && c.kept == c.dtype && c.D > 64);
+  const int slots = alone ? 256 : 512;
   const long items = (long)p.sp.tiles * c.H, units = (max_len + p.sp.unit - 1) / p.sp.unit;
-  // beyond some rounds of workgroups the items even out by themselves; the units are counted in 32 bits
-  const bool share = (mean <= 128 || items < PLAIN) && (double)items * units < 2e9;
-  p.sp.shares = share ? (p.width == 16 ? SHARES16 : SHARES32) : 0;
-  p.sp.by_item = items <= p.sp.shares;
-  p.sp.joins = p.sp.by_item ? (int)items : p.sp.shares;
-  p.many = p.sp.shares >= 8 * items;
-  p.grid = share ? p.sp.shares : (unsigned)items;
+  const bool share = (mean <= 128 || items <= slots) && (double)items * units < 2e9;       // units are counted in 32 bits
+  p.sp.shares = share ? slots : 0;
+  p.sp.by_item = items <= slots;
+  p.sp.joins = p.sp.by_item ? (int)items : slots;
+  p.many = slots >= 8 * items;
+  p.grid = share ? slots : (unsigned)items;
   return p;
 }
 
@@ -881,7 +976,7 @@ template <int DT, int KEPT, int D, int M, int RW, int KW, int KT>
 hipError_t launch_form(const Paged& c, const Attend& a, const Plan& p, void* ws, hipStream_t stream) {
   typedef Form<DT, KEPT, D> F;
   constexpr size_t stage = 2 * KT * F::ROWB + (KEPT != DT ? 8 * KT : 0), wide = KEPT != DT && RW > 1 ? 2 * KT * Form<DT, DT, D>::ROWB : 0, slots = (size_t)(KW - 1) * RW * (D * M * 4 + 512);
-  constexpr size_t tiles = KW * (2 * stage + wide), lds = tiles > slots ? tiles : slots;
+  constexpr size_t tiles = KW * ((RW == 8 ? 4 : 2) * stage + wide), lds = tiles > slots ? tiles : slots;
   static PerDeviceInt raised;
   hipError_t e = ensure_dynamic_lds(raised, (const void*)attend_kernel<DT, KEPT, D, M, RW, KW, KT>, lds);
   if (e != hipSuccess) return e;
@@ -907,6 +1002,8 @@ hipError_t launch_attend_d(const Paged& c, const Attend& a, void* ws, hipStream_
   if (p.width == 16) return launch_form<DT, KEPT, D, 16, 1, 4, 32>(c, a, p, ws, stream);
   if (p.rw == 1) return launch_form<DT, KEPT, D, 32, 1, 4, 32>(c, a, p, ws, stream);
   if (p.rw == 2) return launch_form<DT, KEPT, D, 32, 2, 2, 32>(c, a, p, ws, stream);
+  if constexpr (DT == KEPT)
+    if (p.rw == 8) return launch_form<DT, KEPT, D, 32, 8, 1, 64>(c, a, p, ws, stream);
   return launch_form<DT, KEPT, D, 32, 4, 1, 64>(c, a, p, ws, stream);
 }
 
