@@ -553,6 +553,74 @@ def stream_bench(a):
     print(json.dumps(line), flush=True)
 
 
+def round_bench(a):
+    """One verification round's memory-side work: the drafted tokens of one layer into the 8-bit cache, their attention over it, the adjustments of the
+    logits, the verification.  S = 32 sequences of about 4000 cached tokens, 8 drafted tokens each, 64 query and 8 key heads of 128, 151 936 words."""
+    import torch
+
+    import paper_2605_02218_amd as C
+    C.load_library()
+    torch.cuda.set_device(0)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    S, L, V, heads, H, D, page = 32, 8, 151936, 64, 8, 128, 64
+    lengths = [2000 + 129 * ((s * 13) % 32) for s in range(S)]
+    need = [-(-n // page) for n in lengths]
+    width, n_pages = max(need), sum(need)
+    order = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)
+    pages = torch.zeros(S, width, dtype=torch.int32, device="cuda")
+    at = 0
+    for s, n in enumerate(need):
+        pages[s, :n] = order[at:at + n]
+        at += n
+    start = torch.arange(0, S * L + 1, L, dtype=torch.int32, device="cuda")
+    length = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    cp = C.CacheParams(n_seq=S, n_tokens=S * L, n_kv_heads=H, head_dim=D, page_size=page, n_pages=n_pages, max_pages=width, dtype=C.BF16, cache_dtype=C.E4M3)
+    whole = C.CacheParams(n_seq=S, n_tokens=sum(lengths), n_kv_heads=H, head_dim=D, page_size=page, n_pages=n_pages, max_pages=width, dtype=C.BF16,
+                          cache_dtype=C.E4M3)
+    cache = C.cache_alloc(cp)
+    rows = lambda n, h: torch.randn(n, h, D, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    ends = torch.tensor([0] + lengths, device="cuda").cumsum(0).to(torch.int32)
+    C.cache_write(whole, rows(sum(lengths), H), rows(sum(lengths), H), ends, length, pages, cache)
+    qkv = rows(S * L, heads + 2 * H)
+    ap = C.AttendParams(cache=cp, n_heads=heads, max_len=max(lengths), scale=D ** -0.5)
+    lp, vp = C.LogitsParams(S, L, V), C.VerifyParams(S, L, V)
+    zt, zd = (2.0 * torch.randn(S, L, V, generator=g, device="cuda")).to(torch.bfloat16), (2.0 * torch.randn(S, L, V, generator=g, device="cuda")).to(torch.bfloat16)
+    drafted = torch.randint(0, V, (S, L), generator=g, device="cuda", dtype=torch.int32)
+    history = torch.randint(0, V, (S * 1000,), generator=g, device="cuda", dtype=torch.int32)
+    hstart = torch.arange(0, S * 1000 + 1, 1000, dtype=torch.int32, device="cuda")
+    pen = torch.tensor([[1.1, 0.2, 0.1, 0.8]] * S, device="cuda")
+    ua, ur = torch.rand(S, L, generator=g, device="cuda"), torch.rand(S, generator=g, device="cuda")
+    ws_a = torch.empty(C.attend_workspace_size(ap) + 256, dtype=torch.uint8, device="cuda")
+    ws_v = torch.empty(C.verify_workspace_size(vp) + 256, dtype=torch.uint8, device="cuda")
+    out, z = torch.empty(S * L, heads, D, dtype=torch.bfloat16, device="cuda"), torch.empty_like(zt)
+    calls = {
+        "cache_write": lambda: C.cache_write(cp, qkv[:, heads:heads + H], qkv[:, heads + H:], start, length, pages, cache),
+        "attend": lambda: C.attend(ap, qkv[:, :heads], start, length, pages, cache, workspace=ws_a, out=out),
+        "adjust_logits": lambda: C.adjust_logits(lp, zt, history, hstart, pen, drafted=drafted, out=z),
+        "verify": lambda: C.verify(vp, z, zd, drafted, ua, ur, workspace=ws_v),
+    }
+
+    def timed(fns):
+        for _ in range(a.warmup):
+            for f in fns:
+                f()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(a.steps):
+            for f in fns:
+                f()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) / a.steps
+
+    dt = timed(list(calls.values()))
+    parts = {n: round(timed([f]) * 1e6, 1) for n, f in calls.items()}
+    print(json.dumps({
+        "metric": "drafted positions/s through one layer's cache and attention, the adjustments and the verification", "value": S * L / dt, "unit": "positions/s",
+        "n_gpus": 1, "steps": a.steps, "warmup": a.warmup, "ms_per_step": dt * 1e3, "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
+        "dtype": "bf16, e4m3 cache", "data": "synthetic", "us_alone": parts,
+        "config": {"n_seq": S, "n_draft": L, "cached": sum(lengths), "heads": heads, "kv_heads": H, "head_dim": D, "vocab": V, "page": page}}), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -569,6 +637,7 @@ def main():
     ap.add_argument("--ragged", action="store_true", help="time covspec_reduce_ragged on a dynamic-resolution batch (own JSON line)")
     ap.add_argument("--ablations", action="store_true", help="time the selector ablations on the chosen workload (own JSON line)")
     ap.add_argument("--stream", action="store_true", help="time covspec_stream_step in its steady state (own JSON line)")
+    ap.add_argument("--round", action="store_true", help="time cache write, attention, logit adjustments and verification of a drafting round (own JSON line)")
     ap.add_argument("--no-comparison", action="store_true", help="with --stream: leave out the from-scratch comparison (clean kernel profiles)")
     ap.add_argument("--copy-calibration", action="store_true",
                     help="run three plain 1 GiB device copies and exit (reference reading for the HBM byte counters)")
@@ -602,6 +671,9 @@ def main():
         return
     if a.ablations:
         ablation_bench(a)
+        return
+    if a.round:
+        round_bench(a)
         return
     import covspec_inputs as I
     import paper_2605_02218_amd as C

@@ -589,71 +589,89 @@ class CacheParams:
                                   self.cache_dtype, 0, row_pitch)
 
 
-def _cache_torch_dtype(dtype: int):
-    import torch
-    return {FP32: torch.float32, BF16: torch.bfloat16, FP16: torch.float16, INT8: torch.int8, E4M3: torch.float8_e4m3fn}[dtype]
+_TORCH = {}        # torch types by the library's numbers, and by name; filled with torch's first use here
+
+
+def _types():
+    if not _TORCH:
+        import torch
+        _TORCH.update({FP32: torch.float32, BF16: torch.bfloat16, FP16: torch.float16, INT8: torch.int8, E4M3: torch.float8_e4m3fn, "i32": torch.int32,
+                       "i64": torch.int64, "f32": torch.float32})
+    return _TORCH
 
 
 def _same_device(*tensors):
     """Device of the tensors (None entries left out); the call's kernels run there, on that device's current stream."""
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) != 1 or next(iter(devices)).type != "cuda":
-        raise ValueError("tensors must be on one device")
-    return next(iter(devices))
+    dev = None
+    for t in tensors:
+        if t is not None:
+            if dev is None:
+                dev = t.device
+            elif t.device != dev:
+                raise ValueError("tensors must be on one device")
+    if dev is None or dev.type != "cuda":
+        raise ValueError("tensors must be on a device")
+    return dev
+
+
+def _call_on(dev, fn, *args):
+    """fn(*args, stream) with `dev` current, on its current stream."""
+    import torch
+    if torch.cuda.current_device() == dev.index:
+        return fn(*args, torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(dev):
+        return fn(*args, torch.cuda.current_stream().cuda_stream)
 
 
 def _expect(t, name: str, shape, dtype):
     """Pointer of a contiguous device tensor, None for None; what the library cannot see (shapes, types) is checked here."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     return _ptr(t)
 
 
 def _rows(t, name: str, n: int, heads: int, dim: int, dtype):
     """(pointer, pitch) of rows [n, heads, dim] that are dense but for the distance from one to the next."""
-    if t.dtype != dtype or tuple(t.shape) != (n, heads, dim):
+    if t.dtype != dtype or t.shape != (n, heads, dim):
         raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (name, dtype, (n, heads, dim), t.dtype, tuple(t.shape)))
-    if not t.is_cuda or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+    pitch, head, one = t.stride()
+    if not t.is_cuda or one != 1 or (heads > 1 and head != dim):
         raise ValueError("%s must be a device tensor with dense rows" % name)
-    return t.data_ptr(), (t.stride(0) if n > 1 else heads * dim)
+    return t.data_ptr(), (pitch if n > 1 else heads * dim)
 
 
 def cache_alloc(p: CacheParams, device="cuda"):
     """An empty pool: (k, v, k_scale, v_scale), codes [n_pages, n_kv_heads, page_size, head_dim]; scales None unless in 8 bits."""
     import torch
     shape = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim)
-    dt = _cache_torch_dtype(p.cache_dtype)
+    dt = _types()[p.cache_dtype]
     scales = (None, None) if p.cache_dtype == p.dtype else tuple(torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2))
     return tuple(torch.empty(shape, dtype=dt, device=device) for _ in range(2)) + scales
 
 
 def _cache_ptrs(p: CacheParams, start, length, pages, cache):
-    import torch
     k, v, ks, vs = cache
     shape = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim)
-    dt = _cache_torch_dtype(p.cache_dtype)
-    batch = [_expect(start, "start", (p.n_seq + 1,), torch.int32), _expect(length, "length", (p.n_seq,), torch.int32),
-             _expect(pages, "pages", (p.n_seq, p.max_pages), torch.int32)]
-    pool = [_expect(k, "k_cache", shape, dt), _expect(v, "v_cache", shape, dt), _expect(ks, "k_scale", shape[:3], torch.float32),
-            _expect(vs, "v_scale", shape[:3], torch.float32)]
+    types = _types()
+    dt, i32, f32 = types[p.cache_dtype], types["i32"], types["f32"]
+    batch = [_expect(start, "start", (p.n_seq + 1,), i32), _expect(length, "length", (p.n_seq,), i32), _expect(pages, "pages", (p.n_seq, p.max_pages), i32)]
+    pool = [_expect(k, "k_cache", shape, dt), _expect(v, "v_cache", shape, dt), _expect(ks, "k_scale", shape[:3], f32), _expect(vs, "v_scale", shape[:3], f32)]
     return batch, pool
 
 
 def cache_write(p: CacheParams, k, v, start, length, pages, cache):
     """covspec_cache_write: rows k, v [T, Hkv, D] (columns of a wider tensor allowed, both with the same pitch) into `cache` (of cache_alloc)."""
-    import torch
     dev = _same_device(k, v, start, length, pages, *cache)
-    dt = _cache_torch_dtype(p.dtype)
+    dt = _types()[p.dtype]
     kp, pitch = _rows(k, "k", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
     vp, pitch_v = _rows(v, "v", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
     if pitch != pitch_v:
         raise ValueError("k and v must have the same distance between rows")
     batch, pool = _cache_ptrs(p, start, length, pages, cache)
     cs = p.c_struct(pitch)
-    with torch.cuda.device(dev):
-        st = load_library().covspec_cache_write(ctypes.byref(cs), kp, vp, *batch, *pool, _stream())
+    st = _call_on(dev, load_library().covspec_cache_write, ctypes.byref(cs), kp, vp, *batch, *pool)
     if st != OK:
         raise CovspecError(st, "covspec_cache_write")
     return cache
@@ -663,7 +681,7 @@ def cache_read(p: CacheParams, cache, start, length, pages, k_out=None, v_out=No
     """covspec_cache_read: (k, v) [T, Hkv, D]; padding rows of outputs allocated here are unspecified."""
     import torch
     dev = _same_device(start, length, pages, k_out, v_out, *cache)
-    dt = _cache_torch_dtype(p.dtype)
+    dt = _types()[p.dtype]
     shape = (p.n_tokens, p.n_kv_heads, p.head_dim)
     k_out = torch.empty(shape, dtype=dt, device=dev) if k_out is None else k_out
     v_out = torch.empty(shape, dtype=dt, device=dev) if v_out is None else v_out
@@ -673,8 +691,7 @@ def cache_read(p: CacheParams, cache, start, length, pages, k_out=None, v_out=No
         raise ValueError("k_out and v_out must have the same distance between rows")
     batch, pool = _cache_ptrs(p, start, length, pages, cache)
     cs = p.c_struct(pitch)
-    with torch.cuda.device(dev):
-        st = load_library().covspec_cache_read(ctypes.byref(cs), *pool, *batch, kp, vp, _stream())
+    st = _call_on(dev, load_library().covspec_cache_read, ctypes.byref(cs), *pool, *batch, kp, vp)
     if st != OK:
         raise CovspecError(st, "covspec_cache_read")
     return k_out, v_out
@@ -702,12 +719,12 @@ def attend(p: AttendParams, q, start, length, pages, cache, visible=None, worksp
     import torch
     c = p.cache
     dev = _same_device(q, start, length, pages, visible, workspace, out, *cache)
-    dt = _cache_torch_dtype(c.dtype)
+    dt = _types()[c.dtype]
     qp, q_pitch = _rows(q, "q", c.n_tokens, p.n_heads, c.head_dim, dt)
     out = torch.empty(c.n_tokens, p.n_heads, c.head_dim, dtype=dt, device=dev) if out is None else out
     op, out_pitch = _rows(out, "out", c.n_tokens, p.n_heads, c.head_dim, dt)
     batch, pool = _cache_ptrs(c, start, length, pages, cache)
-    bits = _expect(visible, "visible", (c.n_tokens,), torch.int64)
+    bits = _expect(visible, "visible", (c.n_tokens,), _types()["i64"])
     if workspace is None:
         n = attend_workspace_size(p)
         if n == 0:
@@ -716,8 +733,7 @@ def attend(p: AttendParams, q, start, length, pages, cache, visible=None, worksp
     lse = torch.empty(c.n_tokens, p.n_heads, dtype=torch.float32, device=dev) if want_lse else None
     wp, wb = _ws_args(workspace)
     cs = p.c_struct(q_pitch, out_pitch)
-    with torch.cuda.device(dev):
-        st = load_library().covspec_attend(ctypes.byref(cs), qp, *batch, *pool, bits, op, _ptr(lse), wp, wb, _stream())
+    st = _call_on(dev, load_library().covspec_attend, ctypes.byref(cs), qp, *batch, *pool, bits, op, _ptr(lse), wp, wb)
     if st != OK:
         raise CovspecError(st, "covspec_attend")
     return out, lse
@@ -740,7 +756,7 @@ def adjust_logits(p: LogitsParams, z, history, history_start, penalties, prompt_
     bias = (None, None, None) if bias is None else bias
     dev = _same_device(z, history, history_start, penalties, prompt_len, drafted, allowed, out, *bias)
     S, L, V = p.n_seq, p.n_pos, p.vocab
-    dt, i32 = _cache_torch_dtype(p.dtype), torch.int32
+    dt, i32 = _types()[p.dtype], _types()["i32"]
     out = torch.empty_like(z) if out is None else out
     n = bias[1].numel() if bias[1] is not None else 0
     if history.dtype != i32 or (bias[1] is not None and bias[1].dtype != i32):
@@ -756,8 +772,7 @@ def adjust_logits(p: LogitsParams, z, history, history_start, penalties, prompt_
         args += [None, None, None]
     args += [_expect(allowed, "allowed", (S, L, (V + 31) // 32), i32), _expect(out, "out", (S, L, V), dt)]
     cs = p.c_struct()
-    with torch.cuda.device(dev):
-        st = load_library().covspec_adjust_logits(ctypes.byref(cs), *args, _stream())
+    st = _call_on(dev, load_library().covspec_adjust_logits, ctypes.byref(cs), *args)
     if st != OK:
         raise CovspecError(st, "covspec_adjust_logits")
     return out
