@@ -434,8 +434,8 @@ int covspec_draft_gate(const covspec_draft_params* p, const void* z_draft, const
  *
  * covspec_cache_write: rows of k and v into the cache.  Row (token, head) in 8 bits, all in fp32 with each
  * operation rounded on its own:
- *   amax = max |x|, Q = 127 (INT8) or 448 (E4M3);  scale = amax / Q;  code = x * (Q / amax) to the nearest, ties to
- *   even (to the nearest representable value for E4M3).  amax < 2^-100: all codes and the scale are zero.  A row
+ *   amax = max |x|, Q = 127 (INT8) or 448 (E4M3);  scale = amax / Q;  code = x * ((1 / amax) * Q) to the nearest, ties
+ *   to even (to the nearest representable value for E4M3).  amax < 2^-100: all codes and the scale are zero.  A row
  *   with an infinity or NaN gets the scale NaN and zero codes, so that it reads back as NaN.
  * With cache_dtype == dtype rows are copied bit for bit.
  * Two rows of one call for the same place: one of them is kept, which one is not said.
@@ -486,8 +486,8 @@ int covspec_cache_read(const covspec_cache_params* p, const void* k_cache, const
  *   lse_out [n_tokens, n_heads] fp32 log sum_j exp(scale * q . k_j), or NULL
  * max_len (HOST) bounds the lengths: it sizes the grid and the workspace; positions at or beyond it are not seen.
  * Products are taken of 16-bit values with fp32 sums (8-bit codes are exact in 16 bits; their scales enter in fp32),
- * softmax statistics are fp32, p is rounded to 16 bits for its product with v, and v = code * scale of an 8-bit cache may be.  The
- * same call gives the same bits.
+ * softmax statistics are fp32, p (of an fp16 batch over codes: p times the scale, to 16 bits of
+ * significand) is rounded to 16 bits for its product with v.  The same call gives the same bits.
  * Limits: those of the cache (its row_pitch is not used); n_heads a multiple of n_kv_heads, at most 64 times it;
  * n_tokens * n_heads below 2^30; max_len from 1 to max_pages * page_size; window >= 0; scale finite.  Workspace:
  * covspec_attend_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on `stream`,

@@ -30,7 +30,7 @@ def quantise(x, kept):
     use = finite & (top >= TINY)
     safe = np.where(use, top, np.float32(1.0)).astype(np.float32)
     scale = np.where(finite, np.where(use, safe / Q[kept], np.float32(0.0)), np.float32(np.nan)).astype(np.float32)
-    inv = (Q[kept] / safe).astype(np.float32)
+    inv = (np.float32(1.0) / safe).astype(np.float32) * Q[kept]
     with np.errstate(invalid="ignore"):
         y = np.where(use[..., None], x * inv[..., None], np.float32(0.0)).astype(np.float32)
     y = np.clip(y, -Q[kept], Q[kept])

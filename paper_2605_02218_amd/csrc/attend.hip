@@ -225,12 +225,13 @@ struct Joined { int pieces, share, row0, head0, r0, rows; };   // pieces (0: not
 template <int DT, int KEPT, int D, int M, int RW, int KW, int KT>
 __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend a, Split sp, float* __restrict__ part, f32x2_t* __restrict__ stat, Joined* __restrict__ joined, int* __restrict__ joined_count) {
   typedef Form<DT, KEPT, D> F;
-  // 8-bit codes: a single wave widens what it multiplies; waves that share tiles widen each tile once, in LDS, between them.  Their scales: of K
-  // times the scores; of V times p, in fp32, which bf16 has the range for.  fp16 has not: the shared tiles hold v = code * scale, rounded once
-  // more, and a single wave takes codes and p v_scale in two bf16 parts.
+  // 8-bit codes: a single wave widens what it multiplies; waves that share tiles widen each tile once, in LDS, between them.  Their scales, in fp32:
+  // of K times the scores, of V times p, which bf16 has the range for.  fp16 has not; there p v_scale goes in as two bf16 parts (one has not the bits:
+  // with v = code * scale rounded to fp16 instead the error against 64 bits was 1.65 times that of the output's own rounding, a tree
+  // of 88 rows behind 120001 tokens took 74 us instead of 83).
   constexpr bool CODES = KEPT != DT, WIDE = CODES && RW > 1;
-  constexpr int VDT = CODES && !WIDE ? DT_BF16 : DT;     // type of the products with v
-  constexpr bool SPLIT_P = CODES && !WIDE && DT == DT_F16, SCALE_P = CODES && !(WIDE && DT == DT_F16);
+  constexpr int VDT = CODES ? DT_BF16 : DT;              // type of the products with v
+  constexpr bool SPLIT_P = CODES && DT == DT_F16;
   typedef Form<DT, WIDE ? DT : KEPT, D> W;               // of the tiles that are multiplied
   constexpr bool RAW = CODES && !WIDE;
   constexpr bool TURNS = RW == 8;                        // see the loop over the tiles
@@ -448,7 +449,6 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
   // The codes of a stage to 16 bits, by the waves that share them.
   auto widen = [&](int stage) {
     const lds_char* const raw = (const lds_char*)(base + stage * STAGE);
-    const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(raw + 2 * TILE);
     lds_char* const wide = (lds_char*)(base + 2 * STAGE);
     const int me = rw * 64 + lane;
 #pragma unroll
@@ -457,20 +457,11 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       if (F::PIECES == F::CH || piece < F::PIECES) {
         const int from = row * F::ROWB + (piece ^ F::turn(row)) * 16, to = row * W::ROWB + ((2 * piece) ^ W::turn(row)) * 16;
         const u32x4_t kk = *(const __attribute__((address_space(3))) u32x4_t*)(raw + from), vv = *(const __attribute__((address_space(3))) u32x4_t*)(raw + TILE + from);
-        const float vs = DT == DT_F16 ? scales[KT + row] : 0.f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = h == 0 ? to : to ^ 16;                        // the next piece
           *(__attribute__((address_space(3))) u32x4_t*)(wide + at) = widen8<DT, KEPT>((u32x2_t){kk[2 * h], kk[2 * h + 1]});
-          u32x4_t v;
-          if constexpr (DT == DT_F16) {
-            const f32x4_t p0 = decode4<KEPT>(vv[2 * h]), p1 = decode4<KEPT>(vv[2 * h + 1]);
-            v = (u32x4_t){Half<DT>::pack(p0[0] * vs, p0[1] * vs), Half<DT>::pack(p0[2] * vs, p0[3] * vs), Half<DT>::pack(p1[0] * vs, p1[1] * vs),
-                          Half<DT>::pack(p1[2] * vs, p1[3] * vs)};
-          } else {
-            v = widen8<DT, KEPT>((u32x2_t){vv[2 * h], vv[2 * h + 1]});
-          }
-          *(__attribute__((address_space(3))) u32x4_t*)(wide + WTILE + at) = v;
+          *(__attribute__((address_space(3))) u32x4_t*)(wide + WTILE + at) = widen8<VDT, KEPT>((u32x2_t){vv[2 * h], vv[2 * h + 1]});
         }
       }
     }
@@ -607,7 +598,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
 #pragma unroll
       for (int e = 0; e < 8; ++e) part_sum[e & 3] += z[x][e];
     sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
-    if constexpr (SCALE_P) {
+    if constexpr (CODES) {
       auto scale = [&](auto some) {                                    // the scale of a row that is not seen may be anything
 #pragma unroll
         for (int x = 0; x < NX; ++x)

@@ -1,6 +1,6 @@
 // Paged cache of keys and values: rows of new tokens into it, in 16 bits or quantised to 8, and positions back out of it.
 //
-// A row is the D values of one token and key head.  In 8 bits amax = max |x|, scale = amax / Q, code = x (Q / amax) to the nearest, ties to even
+// A row is the D values of one token and key head.  In 8 bits amax = max |x|, scale = amax / Q, code = x ((1 / amax) Q) to the nearest, ties to even
 // (Q = 127 for integers, 448 for e4m3): a code is off by at most half a step, so |x - scale code| <= scale / 2 for integers.
 //
 // D / 8 lanes take a row of k and the same row of v, 16 bytes of each, so that the maximum is four exchanges inside a row of 16 lanes and every
@@ -20,7 +20,7 @@ constexpr int HEADS = 2;
 
 // lanes of a row: a power of two, so that exchanges stay inside; head dimension 96 leaves a quarter of them without work
 constexpr int row_lanes(int D) { return D == 64 ? 8 : 16; }
-constexpr float kTiny = 0x1p-100f;              // smaller maxima: Q / amax and the products with it would leave the range of fp32
+constexpr float kTiny = 0x1p-100f;              // smaller maxima: (1 / amax) Q and the products with it would leave the range of fp32
 
 template <int KEPT> constexpr float kTop = KEPT == DT_I8 ? 127.f : 448.f;
 
@@ -53,14 +53,14 @@ __device__ __forceinline__ u32x2_t quantise(const u32x4_t& raw, float& scale) {
   for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
   const float amax = __uint_as_float(top);
   const bool finite = top < 0x7F800000u;
-  const float inv = finite && amax >= kTiny ? kTop<KEPT> / amax : 0.f;
+  const float inv = finite && amax >= kTiny ? (1.f / amax) * kTop<KEPT> : 0.f;
   scale = !finite ? __uint_as_float(0x7FC00000u) : amax >= kTiny ? amax / kTop<KEPT> : 0.f;
   u32x2_t out;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float y[4];
 #pragma unroll
-    // inv has one rounding and the product another: the largest may come out one part in 2^23 above Q
+    // three roundings: the largest may come out some parts in 2^23 above Q
     for (int e = 0; e < 4; ++e) y[e] = finite ? __builtin_amdgcn_fmed3f(x[4 * h + e] * inv, -kTop<KEPT>, kTop<KEPT>) : 0.f;
     out[h] = encode4<KEPT>(y);
   }
