@@ -444,8 +444,8 @@ int covspec_draft_gate(const covspec_draft_params* p, const void* z_draft, const
  *               be columns of a wider tensor, e.g. of a fused projection; 16-byte aligned
  *   k_out, v_out  the same layout; rows of the batch are written, padding rows are left as they were
  * dtype: COVSPEC_BF16 or COVSPEC_FP16.  Limits: head_dim 64, 96 or 128; page_size a power of two from 16 to 1024;
- * row_pitch a multiple of 8, not below n_kv_heads * head_dim; n_tokens * n_kv_heads and max_pages * page_size
- * below 2^30; pool places (n_pages * n_kv_heads * page_size) below 2^40: else COVSPEC_INVALID_ARG (dtype pairs, non-positive
+ * row_pitch a multiple of 8, not below n_kv_heads * head_dim; n_tokens * n_kv_heads below 2^27 and
+ * max_pages * page_size below 2^30; pool places (n_pages * n_kv_heads * page_size) below 2^40: else COVSPEC_INVALID_ARG (dtype pairs, non-positive
  * sizes, misaligned or missing pointers, pitch) or COVSPEC_UNSUPPORTED.  No workspace; enqueues one kernel on
  * `stream`, does not synchronise, allocates nothing.
  */
@@ -489,7 +489,7 @@ int covspec_cache_read(const covspec_cache_params* p, const void* k_cache, const
  * softmax statistics are fp32, p (of an fp16 batch over codes: p times the scale, to 16 bits of
  * significand) is rounded to 16 bits for its product with v.  The same call gives the same bits.
  * Limits: those of the cache (its row_pitch is not used); n_heads a multiple of n_kv_heads, at most 64 times it;
- * n_tokens * n_heads below 2^30; max_len from 1 to max_pages * page_size; window >= 0; scale finite.  Workspace:
+ * n_tokens * n_heads and n_seq * n_kv_heads below 2^30 (and a grid of less than 2^32 threads); max_len from 1 to max_pages * page_size; window >= 0; scale finite.  Workspace:
  * covspec_attend_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on `stream`,
  * does not synchronise, allocates nothing; the launches depend on the parameters alone, so that a captured graph
  * serves other lengths and pages of the same parameters.

@@ -1021,6 +1021,12 @@ size_t attend_workspace_bytes(const Paged& c, int heads, int max_len) {
   return p.sp.shares == 0 ? 256 : part_bytes(c, p.sp) + (size_t)2 * p.sp.shares * p.sp.rows * sizeof(f32x2_t) + p.sp.joins * sizeof(Joined) + sizeof(int);
 }
 
+// A launch has fewer than 2^32 threads.
+bool attend_fits(const Paged& c, int heads, int max_len) {
+  const Plan p = plan_of(c, heads, max_len);
+  return (double)(c.S + (long)c.T * (heads / c.H) / p.sp.rows) * c.H * 512 < 4e9 || p.sp.shares > 0;
+}
+
 hipError_t launch_attend(const Paged& c, const Attend& a, void* ws, hipStream_t stream) {
   if (c.dtype == DT_BF16) return launch_attend_t<DT_BF16>(c, a, ws, stream);
   if (c.dtype == DT_F16) return launch_attend_t<DT_F16>(c, a, ws, stream);

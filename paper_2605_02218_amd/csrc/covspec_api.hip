@@ -775,7 +775,7 @@ static int cache_check(const covspec_cache_params* p, Paged* c) {
   if (p->head_dim != 64 && p->head_dim != 96 && p->head_dim != 128) return COVSPEC_UNSUPPORTED;
   if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)) != 0) return COVSPEC_UNSUPPORTED;
   const int64_t most = 1 << 30;
-  if (p->n_seq >= most || (int64_t)p->n_tokens * p->n_kv_heads >= most || (int64_t)p->max_pages * p->page_size >= most) return COVSPEC_UNSUPPORTED;
+  if (p->n_seq >= most || (int64_t)p->n_tokens * p->n_kv_heads >= 1 << 27 || (int64_t)p->max_pages * p->page_size >= most) return COVSPEC_UNSUPPORTED;
   if (p->row_pitch > (int64_t)1 << 32) return COVSPEC_UNSUPPORTED;
   if ((double)p->n_pages * p->n_kv_heads * p->page_size >= 1099511627776.0) return COVSPEC_UNSUPPORTED;      // 2^40 places
   int shift = 0;
@@ -836,6 +836,7 @@ static int attend_check(const covspec_attend_params* p, Paged* c) {
     if (pitch != 0 && (pitch < dense || pitch % 8 != 0)) return COVSPEC_INVALID_ARG;
   if (p->n_heads / c->H > 64 || (int64_t)c->T * p->n_heads >= 1 << 30) return COVSPEC_UNSUPPORTED;
   if (p->q_pitch > (int64_t)1 << 32 || p->out_pitch > (int64_t)1 << 32) return COVSPEC_UNSUPPORTED;
+  if ((int64_t)p->cache.n_seq * c->H >= 1 << 30 || !attend_fits(*c, p->n_heads, p->max_len)) return COVSPEC_UNSUPPORTED;
   return COVSPEC_OK;
 }
 

@@ -272,6 +272,7 @@ struct Attend {
   float* lse;                          // or null
 };
 size_t attend_workspace_bytes(const Paged& c, int heads, int max_len);
+bool attend_fits(const Paged& c, int heads, int max_len);
 hipError_t launch_attend(const Paged& c, const Attend& a, void* ws, hipStream_t stream);
 
 // ---------------------------------------------------------------- adjust.hip

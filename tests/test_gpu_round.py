@@ -70,7 +70,7 @@ def test_rounds_of_drafting_and_verification(dtype, kept):
     step(prompts)
     history = [list(rng.integers(0, V, n)) for n in prompts]
     asked = list(prompts)
-    head = torch.randn(heads * D, V, device="cuda") * 0.3
+    head = dev(rng.standard_normal((heads * D, V)).astype(np.float32)) * 0.3
     accepted_any = rejected_any = False
     for r in range(rounds):
         drafted = rng.integers(0, 40, (S, L)).astype(np.int32)
@@ -78,7 +78,7 @@ def test_rounds_of_drafting_and_verification(dtype, kept):
         zt = (out.reshape(S, L, heads * D).float() @ head)
         zt[:, :, :40] += 6.0
         zt = zt.to(torch_dtype(dtype))
-        zd = (zt.float() + 0.5 * torch.randn(S, L, V, device="cuda")).to(zt.dtype)
+        zd = (zt.float() + 1.5 * dev(rng.standard_normal((S, L, V)).astype(np.float32))).to(zt.dtype)
         hs = np.concatenate([[0], np.cumsum([len(h) for h in history])]).astype(np.int32)
         pen = np.tile(np.array([[1.3, 0.4, 0.2, 0.9]], dtype=np.float32), (S, 1))
         bits = np.full((S, L, V // 32), 0xFFFFFFFF, dtype=np.uint32)

@@ -20,7 +20,7 @@ CACHE_REFUSALS = [
     (dict(max_pages=0), Bd.INVALID_ARG), (dict(page_size=0), Bd.INVALID_ARG), (dict(head_dim=-64), Bd.INVALID_ARG),
     (dict(dtype=C.FP32), Bd.INVALID_ARG), (dict(dtype=C.INT8), Bd.INVALID_ARG), (dict(cache_dtype=C.FP16), Bd.INVALID_ARG), (dict(cache_dtype=C.FP32), Bd.INVALID_ARG),
     (dict(cache_dtype=5), Bd.INVALID_ARG), (dict(head_dim=80), Bd.UNSUPPORTED), (dict(head_dim=256), Bd.UNSUPPORTED), (dict(page_size=8), Bd.UNSUPPORTED),
-    (dict(page_size=48), Bd.UNSUPPORTED), (dict(page_size=2048), Bd.UNSUPPORTED), (dict(n_tokens=1 << 28), Bd.UNSUPPORTED), (dict(max_pages=1 << 24), Bd.UNSUPPORTED),
+    (dict(page_size=48), Bd.UNSUPPORTED), (dict(page_size=2048), Bd.UNSUPPORTED), (dict(n_tokens=1 << 28), Bd.UNSUPPORTED), (dict(n_tokens=1 << 24), Bd.UNSUPPORTED), (dict(max_pages=1 << 24), Bd.UNSUPPORTED),
     (dict(n_pages=1 << 30, page_size=1024), Bd.UNSUPPORTED),
 ]
 
@@ -69,7 +69,8 @@ def test_attend_parameters_are_checked():
         kw.get("visible"), kw.get("out", FAKE), kw.get("lse"), kw.get("ws", FAKE), kw.get("bytes", BIG), None]
     for kw, status in [(dict(n_heads=0), Bd.INVALID_ARG), (dict(n_heads=12), Bd.INVALID_ARG), (dict(max_len=0), Bd.INVALID_ARG), (dict(max_len=1025), Bd.INVALID_ARG),
                        (dict(window=-1), Bd.INVALID_ARG), (dict(scale=float("nan")), Bd.INVALID_ARG), (dict(scale=float("inf")), Bd.INVALID_ARG),
-                       (dict(n_heads=8 * 65), Bd.UNSUPPORTED), (dict(cache=_cache(n_tokens=1 << 25), n_heads=64), Bd.UNSUPPORTED)]:
+                       (dict(n_heads=8 * 65), Bd.UNSUPPORTED), (dict(cache=_cache(n_tokens=1 << 25), n_heads=64), Bd.UNSUPPORTED),
+                       (dict(cache=_cache(n_seq=1 << 27)), Bd.UNSUPPORTED), (dict(cache=_cache(n_seq=1 << 26), n_heads=512), Bd.UNSUPPORTED)]:
         p = C.AttendParams(**{**ok, **kw})
         assert C.attend_workspace_size(p) == 0, kw
         cs = p.c_struct()
