@@ -932,17 +932,19 @@ __global__ __launch_bounds__(JT) void attend_join_kernel(Attend a, int T, int G,
 // 256 rows whose waves take turns (16-bit caches) from 512 on, where the workgroups, one on a compute unit, are shares or many: 512 tokens behind 32256
 // 587 instead of 658 with 128 rows, 1024 behind 15360 565 instead of 626, prompts of 4 x 3008 741 instead of 752; but 376 items, one prompt of
 // 3000, 113 instead of 107.
-// Shares for few rows, and where a workgroup per item would not fill the device once: 256 tokens behind 32512 (128 items of 128 rows) 361 instead of 909, 512 (256)
-// 675 instead of 905; 544 items of a window over several sequences 181 instead of 112, as their tiles' workgroups no longer read the same positions
-// at the same time.
+// Shares where a workgroup per item would not fill the device once: 256 tokens behind 32512 (128 items of 128 rows) 361 instead of 909, 512 (256)
+// 675 instead of 905, 64 single tokens behind 700 to 7900 123 instead of 150.  Beyond, items even out by themselves, and a share's way from one item
+// to the next is not hidden: 96 segments of 64 rows (768 items) behind up to 3000 positions 151 by items and 184 by shares, 128 segments 187 and 233, 256 single
+// tokens of a 16-bit cache 280 and 408, of an 8-bit one 165 and 202; 544 items of a window over several sequences 112 and 181, as shares do not
+// read the same positions at the same time.
 struct Plan { int width, rw; Split sp; unsigned grid; bool many; };     // many: pieces for an item
 
 Plan plan_of(const Paged& c, int heads, int max_len) {
   const long G = heads / c.H, rows = (long)c.T * G, mean = (rows + c.S - 1) / c.S;
-  const long wide_items = (rows / 256 + c.S) * c.H;
+  auto about = [&](long tile) { return (mean + tile - 1) / tile * c.S * c.H; };       // items, if the sequences were alike
   Plan p;
   p.width = mean <= 16 ? 16 : 32;
-  p.rw = mean <= 32 ? 1 : mean <= 64 ? 2 : c.kept == c.dtype && mean >= 512 && (wide_items <= 256 || wide_items >= 1024) ? 8 : 4;
+  p.rw = mean <= 32 ? 1 : mean <= 64 ? 2 : c.kept == c.dtype && mean >= 512 && (about(256) <= 256 || about(256) >= 1024) ? 8 : 4;
   const int TR = p.width * p.rw;
   p.sp.rows = TR;
   p.sp.unit = p.rw == 1 ? 128 : 64;                  // a tile for each wave that takes tiles of its own
@@ -952,7 +954,7 @@ Plan plan_of(const Paged& c, int heads, int max_len) {
   const bool alone = p.rw == 8 || (p.width == 16 && c.kept == c.dtype && c.D > 64);
   const int slots = alone ? 256 : 512;
   const long items = (long)p.sp.tiles * c.H, units = (max_len + p.sp.unit - 1) / p.sp.unit;
-  const bool share = (mean <= 128 || items <= slots) && (double)items * units < 2e9;       // units are counted in 32 bits
+  const bool share = about(TR) <= slots && (double)items * units < 2e9;       // units are counted in 32 bits
   p.sp.shares = share ? slots : 0;
   p.sp.by_item = items <= slots;
   p.sp.joins = p.sp.by_item ? (int)items : slots;
