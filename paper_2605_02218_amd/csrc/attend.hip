@@ -932,11 +932,12 @@ __global__ __launch_bounds__(JT) void attend_join_kernel(Attend a, int T, int G,
 // 256 rows whose waves take turns (16-bit caches) from 512 on, where the workgroups, one on a compute unit, are shares or many: 512 tokens behind 32256
 // 587 instead of 658 with 128 rows, 1024 behind 15360 565 instead of 626, prompts of 4 x 3008 741 instead of 752; but 376 items, one prompt of
 // 3000, 113 instead of 107.
-// Shares where a workgroup per item would not fill the device once: 256 tokens behind 32512 (128 items of 128 rows) 361 instead of 909, 512 (256)
-// 675 instead of 905, 64 single tokens behind 700 to 7900 123 instead of 150.  Beyond, items even out by themselves, and a share's way from one item
-// to the next is not hidden: 96 segments of 64 rows (768 items) behind up to 3000 positions 151 by items and 184 by shares, 128 segments 187 and 233, 256 single
-// tokens of a 16-bit cache 280 and 408, of an 8-bit one 165 and 202; 544 items of a window over several sequences 112 and 181, as shares do not
-// read the same positions at the same time.
+// Shares where a workgroup per item would leave half of the device idle: 256 tokens behind 32512 (128 items of 128 rows) 361 instead of 909, single tokens
+// of 8 sequences 40 instead of 70, 8 drafted tokens of 4 sequences 37 instead of 128, a tree behind 120001 positions 84 instead of 5450; 32 segments
+// behind 900 to 6100 (256 items) 119.5 and 121.5.  With more items there is nothing to gain, as those that still run have the memory to themselves: 64
+// single tokens behind 700 to 7900 (512 items) 126 by shares and 123 by items; and a share's way from one item to the next is not hidden: 96 segments
+// (768 items) 184 and 151, 256 single tokens of a 16-bit cache 408 and 280, of an 8-bit one 202 and 165; 544 items of a window over several
+// sequences 181 and 112, as shares do not read the same positions at the same time.
 struct Plan { int width, rw; Split sp; unsigned grid; bool many; };     // many: pieces for an item
 
 Plan plan_of(const Paged& c, int heads, int max_len) {
@@ -954,7 +955,7 @@ Plan plan_of(const Paged& c, int heads, int max_len) {
   const bool alone = p.rw == 8 || (p.width == 16 && c.kept == c.dtype && c.D > 64);
   const int slots = alone ? 256 : 512;
   const long items = (long)p.sp.tiles * c.H, units = (max_len + p.sp.unit - 1) / p.sp.unit;
-  const bool share = about(TR) <= slots && (double)items * units < 2e9;       // units are counted in 32 bits
+  const bool share = 2 * about(TR) <= slots && (double)items * units < 2e9;       // units are counted in 32 bits
   p.sp.shares = share ? slots : 0;
   p.sp.by_item = items <= slots;
   p.sp.joins = p.sp.by_item ? (int)items : slots;
