@@ -151,7 +151,7 @@ __device__ __forceinline__ int tokens_before(int length, int n) { return (int)ma
 //   shares > 0: that many workgroups at most take equal pieces of the sequence of units, so that long and short sequences together keep all of them
 //     busy to the end; an item that a piece does not hold whole goes to `part`, and attend_join_kernel adds its pieces up.
 //   shares == 0: a workgroup per item, and no join: many items even out by themselves.
-struct Split { int rows, unit, shares, least, tiles, joins; bool by_item; };
+struct Split { int rows, unit, shares, least, tiles, joins; };
 
 // The sequences, 64 at a time, a lane each: rows, length, tiles, units of an item, units in all and up to here.
 struct Block { int row0, n, len, tiles, units, own, upto, items_upto; };
@@ -171,7 +171,7 @@ __device__ __forceinline__ Block block_of(const Paged& c, const Attend& a, const
   }
   v.own = ITEMS ? v.tiles : v.tiles * v.units * c.H;
   v.upto = wave_inscan(v.own);
-  v.items_upto = ITEMS || !sp.by_item ? 0 : wave_inscan(v.tiles * c.H);
+  v.items_upto = ITEMS ? 0 : wave_inscan(v.tiles * c.H);
   return v;
 }
 // at: where the unit asked for lies among the sequence's own; items: items in front of the sequence; s < 0: nowhere
@@ -217,10 +217,9 @@ struct Shares {
   __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
   __device__ __forceinline__ int of(int x) const { return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each; }
 };
-// For the join: an item in several pieces.  Written by the share in which it begins, to the item's number where there are few items (items in one
-// piece then say so), otherwise to the share's.
-struct Joined { int pieces, share, row0, head0, r0, rows; };   // pieces (0: nothing to do), the first one's share; first row of the sequence in the batch,
-                                                               // first query head, first row of the tile among the sequence's, their count
+// For the join, by the item's number: its pieces (0: it is in one), the first one's share; first row of the sequence in the batch, first query head, first row
+// of the tile among the sequence's, their count.  Written by the share in which the item begins.
+struct Joined { int pieces, share, row0, head0, r0, rows; };
 
 template <int DT, int KEPT, int D, int M, int RW, int KW, int KT>
 __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend a, Split sp, float* __restrict__ part, f32x2_t* __restrict__ stat, Joined* __restrict__ joined, int* __restrict__ joined_count) {
@@ -268,26 +267,18 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
     const Shares shares(sp, total);
     const int each = (shares.n + 7) / 8;
     share = (blockIdx.x % 8) * each + blockIdx.x / 8;
-    if ((int)(blockIdx.x / 8) >= each) share = sp.shares - 1 - (blockIdx.x - 8 * each);     // the numbers left, from the last down
-    if (blockIdx.x == 0 && tid == 0) *joined_count = sp.by_item ? items : sp.shares;
-    if (share < shares.n) {
-      x = shares.begin(share);
-      x_end = shares.begin(share + 1);
-    }
-    if (share >= shares.n || x >= x_end) {
-      if (tid == 0 && !sp.by_item) joined[share].pieces = 0;
-      return;
-    }
+    if (blockIdx.x == 0 && tid == 0) *joined_count = items;
+    if ((int)(blockIdx.x / 8) >= each || share >= shares.n) return;
+    x = shares.begin(share);
+    x_end = shares.begin(share + 1);
+    if (x >= x_end) return;
     p = c.S <= 64 ? place_in(first, 0, x, 0, c.H) : find<false>(c, a, sp, x);
     share_of_unit = shares;
   } else {
     p = find<true>(c, a, sp, sp.tiles - 1 - (int)(blockIdx.x / c.H));
   }
   while (true) {
-  if (p.s < 0) {
-    if (sp.shares > 0 && !sp.by_item && tid == 0) joined[share].pieces = 0;
-    return;
-  }
+  if (p.s < 0) return;
   const int s = p.s, row0 = p.row0, n = p.n;
   int tile = p.at, g = blockIdx.x % c.H, from = 0, upto = 1;
   bool whole = true;
@@ -298,9 +289,10 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
     whole = from == 0 && upto == p.units;
     g = item / p.tiles;
     tile = item - g * p.tiles;
-    if (tid == 0 && (from == 0 ? sp.by_item || !whole || x + upto >= x_end : !sp.by_item && x + upto - from >= x_end)) {
-      Joined j = {};                                                   // by share: its last segment writes, whatever that is
-      if (from == 0 && !whole) {
+    const int number = p.items + item;
+    if (tid == 0 && from == 0 && number >= 0 && number < sp.joins) {
+      Joined j = {};
+      if (!whole) {
         j.pieces = share_of_unit.of(x + p.units - 1) - share + 1;
         j.share = share;
         j.row0 = p.row0;
@@ -308,8 +300,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
         j.r0 = tile * TR;
         j.rows = p.n * G;
       }
-      const int at = sp.by_item ? p.items + item : share;
-      if (at >= 0 && at < sp.joins) joined[at] = j;
+      joined[number] = j;
     }
     x += upto - from;
   } else {
@@ -957,8 +948,7 @@ Plan plan_of(const Paged& c, int heads, int max_len) {
   const long items = (long)p.sp.tiles * c.H, units = (max_len + p.sp.unit - 1) / p.sp.unit;
   const bool share = 2 * about(TR) <= slots && (double)items * units < 2e9;       // units are counted in 32 bits
   p.sp.shares = share ? slots : 0;
-  p.sp.by_item = items <= slots;
-  p.sp.joins = p.sp.by_item ? (int)items : slots;
+  p.sp.joins = (int)items;                           // of shares at most `slots`: rows / TR + S is at most twice what `about` says
   p.many = slots >= 8 * items;
   p.grid = share ? slots : (unsigned)items;
   return p;

@@ -323,3 +323,86 @@ def test_many_short_sequences():
     new = [int(x) for x in rng.integers(0, 4, 300)]
     b = Batch(rng, new, [n + int(rng.integers(0, 60)) for n in new], 16, pad=9)
     run(b, 2, 1, 64, "bf16", "bf16")
+
+
+@pytest.mark.parametrize("dtype,kept,new,heads,H", [("bf16", "e4m3", 1, 8, 4), ("bf16", "bf16", 1, 8, 4), ("fp16", "int8", 9, 16, 4), ("bf16", "bf16", 9, 32, 4)])
+def test_more_items_than_the_device_holds(dtype, kept, new, heads, H):
+    """A workgroup for each item, no shares: 150 sequences x 4 key heads, more of them than lanes."""
+    rng = np.random.default_rng(14)
+    b = Batch(rng, [new] * 150, [new + int(x) for x in rng.integers(0, 400, 150)], 16, pad=1)
+    run(b, heads, H, 64, dtype, kept, rows=set(range(0, b.T, 37)) | {0, b.T - 2})
+
+
+@pytest.mark.parametrize("dtype,kept,new", [("bf16", "bf16", 1), ("fp16", "e4m3", 5)])
+def test_shares_over_more_sequences_than_lanes(dtype, kept, new):
+    rng = np.random.default_rng(15)
+    b = Batch(rng, [new] * 120, [new + int(x) for x in rng.integers(0, 900, 120)], 16, pad=1)
+    run(b, 2, 1, 64, dtype, kept, rows=set(range(0, b.T, 7)) | {0, b.T - 2})
+
+
+@pytest.mark.parametrize("dtype,kept", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "int8")])
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_trees_and_chunks_of_many_rows(dtype, kept, D):
+    """512 rows and more: the waves of 16-bit caches take turns."""
+    rng = np.random.default_rng(16)
+    b = Batch(rng, [64, 70], [300, 90], 32, pad=1)
+    vis = [int(x) - (1 << 63) for x in rng.integers(0, 1 << 62, b.T)]
+    run(b, 16, 2, D, dtype, kept, visible=np.array(vis, dtype=np.int64), rows=set(range(0, b.T, 9)) | {63, 64, 133})
+    b = Batch(rng, [129, 1, 300], [129, 400, 777], 16)
+    run(b, 8, 1, D, dtype, kept, rows=set(range(0, b.T, 41)) | {0, 128, 129, 130, 429})
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1e-30, 3.0])
+@pytest.mark.parametrize("dtype,kept,new", [("bf16", "bf16", [1, 3]), ("fp16", "int8", [3, 1]), ("bf16", "e4m3", [150, 8]), ("fp16", "fp16", [200, 9])])
+def test_scales_of_any_sign(scale, dtype, kept, new):
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(17)
+    b = Batch(rng, new, [333, 210], 16)
+    k, v, q, q64 = setup(rng, b, 8, 2, 64, dtype, kept)
+    p = C.AttendParams(cache=b.params(2, 64, dtype, kept), n_heads=8, max_len=333, scale=scale)
+    out, lse = C.attend(p, q.cuda(), *b.device(), upload(k, v), want_lse=True)
+    torch.cuda.synchronize()
+    check(b, 8, 2, 64, dtype, kept, k[2], v[2], q64, out, lse, float(np.float32(scale)), rows=set(range(0, b.T, 11)) | {0, b.T - 1})
+
+
+def test_a_batch_of_padding_only():
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(18)
+    b = Batch(rng, [0, 0, 0], [5, 0, 70], 16, pad=6)
+    run(b, 4, 2, 64, "bf16", "bf16")
+    k, v, q, _ = setup(rng, b, 4, 2, 64, "bf16", "int8")
+    pool = upload(k, v)
+    before = [t.clone() for t in pool]
+    x = torch.randn(b.T, 2, 64, device="cuda").to(torch.bfloat16)
+    C.cache_write(b.params(2, 64, "bf16", "int8"), x, x, *b.device(), pool)
+    torch.cuda.synchronize()
+    for t, u in zip(pool, before):
+        assert torch.equal(t, u)
+
+
+@pytest.mark.parametrize("dtype,kept,heads", [("bf16", "bf16", 4), ("fp16", "e4m3", 64), ("bf16", "int8", 16)])
+def test_arrays_that_describe_nothing_sensible_touch_nothing_else(dtype, kept, heads):
+    """Rows that do not ascend, lengths and pages out of range: results are what they are, memory around the outputs stays as it was.  (Every index
+    formed from these arrays is checked by the kernels.)"""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(19)
+    H, D = 2, 64
+    b = Batch(rng, [8, 8, 8], [90, 40, 64], 16)
+    k, v, q, _ = setup(rng, b, heads, H, D, dtype, kept)
+    pool = upload(k, v)
+    p = C.AttendParams(cache=b.params(H, D, dtype, kept), n_heads=heads, max_len=b.width * 16, scale=0.1)
+    room = torch.full((b.T + 2, heads, D), 7.0, dtype=torch_dtype(dtype), device="cuda")
+    ws = torch.empty(C.attend_workspace_size(p) + 256, dtype=torch.uint8, device="cuda")
+    x = torch.zeros(b.T, H, D, dtype=torch_dtype(dtype), device="cuda")
+    for start, length in (([5, 0, 24, 3], [90, 40, 64]), ([-9, 400, -1, 7], [1 << 30, -5, 77]), ([24, 24, 0, 24], [-(1 << 31), (1 << 31) - 1, 0]), ([0, 24, 24, 0], [3, 0, 9])):
+        ws.fill_(0x7F)
+        dev = [torch.tensor(a, dtype=torch.int32, device="cuda") for a in (start, length)]
+        pages = torch.from_numpy(rng.integers(-3, b.n_pages + 3, b.pages.shape).astype(np.int32)).cuda()
+        C.attend(p, q.cuda(), *dev, pages, pool, workspace=ws, out=room[1:-1])
+        C.cache_read(p.cache, pool, *dev, pages)
+        C.cache_write(p.cache, x, x, *dev, pages, pool)
+        torch.cuda.synchronize()
+        assert bool((room[0] == 7.0).all()) and bool((room[-1] == 7.0).all())
