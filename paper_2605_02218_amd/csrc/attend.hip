@@ -5,12 +5,12 @@
 // waves, and workgroups, may share a long sequence.
 //
 // Rows: the group's query heads of one token are rows of the same key head, so a sequence with n tokens and G heads for each key head has n G rows,
-// r = token * G + head, which one read of its keys and values serves.  A wave takes 32 rows; a workgroup RW waves with rows of their own,
-// which share the tiles of keys and values in LDS, times KW waves that take every KW-th tile.  Few rows (single tokens, segments) are bound by
+// r = token * G + head, which one read of its keys and values serves.  A wave takes 16 or 32 rows (M); a workgroup RW waves with rows of
+// their own, which share the tiles of keys and values in LDS, times KW waves that take every KW-th tile.  Few rows (single tokens, segments) are bound by
 // the bytes of the cache: all waves on different tiles; many rows are bound by the matrix pipes: waves on different rows.
 //
 // A tile of KT positions is 2 KT rows of the pool, 16 bytes a lane straight into LDS, the next tile's while this one is computed.  S^T = K Q^T
-// leaves row r of the queries in the lanes r and r + 32 (16 positions each of 32), so the softmax statistics of a row are plain
+// leaves row r of the queries in the lanes r and r + 32 (16 positions each of 32; with M = 16 in four lanes, r + 16 i), so the softmax statistics of a row are plain
 // registers of its lanes, the factors of a rescaling too, and the probabilities already lie as the operand of O^T = V^T P^T wants them:
 // the k-th slot of an operand may be any position as long as both operands agree.  V^T comes out of LDS by transposing reads.
 #include <type_traits>
