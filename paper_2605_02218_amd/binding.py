@@ -644,6 +644,9 @@ def _rows(t, name: str, n: int, heads: int, dim: int, dtype):
     if t.dtype != dtype or t.shape != (n, heads, dim):
         raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (name, dtype, (n, heads, dim), t.dtype, tuple(t.shape)))
     pitch, head, one = t.stride()
+    # an expanded tensor's rows are all the same one, a distance of 0, which the library takes for dense rows
+    if n > 1 and pitch < heads * dim:
+        raise ValueError("%s must have rows that do not overlap, not %d elements apart" % (name, pitch))
     if not t.is_cuda or one != 1 or (heads > 1 and head != dim):
         raise ValueError("%s must be a device tensor with dense rows" % name)
     return t.data_ptr(), (pitch if n > 1 else heads * dim)

@@ -1,0 +1,29 @@
+"""Host-side checks of what the binding makes of tensors before the library sees them (no GPU work is launched)."""
+import pytest
+
+from paper_2605_02218_amd import binding as Bd
+
+
+class _OnDevice:
+    """What the binding asks of a device tensor, for its checks on the host."""
+
+    def __init__(self, host):
+        self.host, self.is_cuda, self.dtype, self.shape, self.device = host, True, host.dtype, host.shape, "a device"
+
+    def __getattr__(self, name):
+        return getattr(self.host, name)
+
+
+@pytest.mark.parametrize("heads", [1, 8])
+def test_rows_that_overlap_are_refused(heads):
+    """Rows 0 elements apart (an expanded tensor) are no dense rows, for which 0 stands in the library's parameters."""
+    import torch
+    x = torch.zeros(5, heads, 128, dtype=torch.bfloat16)
+    assert Bd._rows(_OnDevice(x), "k", 5, heads, 128, torch.bfloat16) == (x.data_ptr(), heads * 128)
+    assert Bd._rows(_OnDevice(x[:1]), "k", 1, heads, 128, torch.bfloat16) == (x.data_ptr(), heads * 128)
+    assert Bd._rows(_OnDevice(x[:1].expand(1, heads, 128)), "k", 1, heads, 128, torch.bfloat16) == (x.data_ptr(), heads * 128)
+    wide = torch.zeros(5, heads + 3, 128, dtype=torch.bfloat16)[:, 2:2 + heads]
+    assert Bd._rows(_OnDevice(wide), "k", 5, heads, 128, torch.bfloat16) == (wide.data_ptr(), (heads + 3) * 128)
+    for bad in (x[:1].expand(5, heads, 128), x.view(-1).as_strided((5, heads, 128), (8, 128, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            Bd._rows(_OnDevice(bad), "k", 5, heads, 128, torch.bfloat16)
