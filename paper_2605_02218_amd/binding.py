@@ -232,9 +232,10 @@ def alloc_workspace(p: Params, device="cuda"):
 
 
 def _ws_args(ws):
-    base = ws.data_ptr()
+    """(address on 256 bytes, bytes from there): none where the tensor ends in front of that address."""
+    base = _ptr(ws)
     aligned = (base + 255) // 256 * 256
-    return aligned, ws.numel() - (aligned - base)
+    return aligned, max(ws.numel() * ws.element_size() - (aligned - base), 0)
 
 
 def score(p: Params, X, hidden, Q, Wq, Wk, workspace=None):

@@ -27,3 +27,17 @@ def test_rows_that_overlap_are_refused(heads):
     for bad in (x[:1].expand(5, heads, 128), x.view(-1).as_strided((5, heads, 128), (8, 128, 1))):
         with pytest.raises(ValueError, match="overlap"):
             Bd._rows(_OnDevice(bad), "k", 5, heads, 128, torch.bfloat16)
+
+
+def test_a_workspace_is_what_lies_behind_its_first_aligned_byte():
+    import torch
+    x = torch.zeros(2048, dtype=torch.uint8)
+    first = -x.data_ptr() % 256
+    assert Bd._ws_args(_OnDevice(x[first:])) == (x.data_ptr() + first, 2048 - first)
+    assert Bd._ws_args(_OnDevice(x[first:first + 1024].view(torch.float32))) == (x.data_ptr() + first, 1024)
+    assert Bd._ws_args(_OnDevice(x[first + 1:first + 600])) == (x.data_ptr() + first + 256, 600 - 256)
+    # it ends in front of that byte: nothing is left, not a size below zero, which the library would take for a huge one
+    assert Bd._ws_args(_OnDevice(x[first + 1:first + 11]))[1] == 0
+    for bad in (_OnDevice(x[:1].expand(4096)), _OnDevice(x[::2]), x):       # the last one is not on a device
+        with pytest.raises(ValueError):
+            Bd._ws_args(bad)
