@@ -96,10 +96,11 @@ __global__ __launch_bounds__(AT) void adjust_kernel(Adjust a, int L, int V) {
   if (!has) return;
   const float rep = a.penalties[4 * s], pres = a.penalties[4 * s + 1], freq = a.penalties[4 * s + 2], temp = a.penalties[4 * s + 3];
   const float irep = 1.f / rep, itemp = temp > 0.f ? 1.f / temp : 1.f;
-  // x F + A: a word's F above and below zero, and A, for the n occurrences in `seen`
+  // x F + A: a word's F above and below zero, and A, for the n occurrences in `seen`.  Without a bias the zero is the negative one, and A with it where
+  // nothing is subtracted either: x + -0 is x for both zeros.
   float up[N], down[N], add[N];
   auto word = [&](int e, int n, int i) {
-    const float bias = i > 0 ? a.bias_value[b0 + i - 1] : 0.f;
+    const float bias = i > 0 ? a.bias_value[b0 + i - 1] : -0.f;
     const int said = n >> 1;
     up[e] = n == 0 ? itemp : irep * itemp;
     down[e] = n == 0 ? itemp : rep * itemp;

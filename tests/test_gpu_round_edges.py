@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from round_util import Batch
+from round_util import Batch, torch_dtype
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +23,30 @@ def test_expanded_tensors_are_refused_before_anything_is_launched():
         with pytest.raises(ValueError, match="overlap"):
             call()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_adjustments_without_an_effect_keep_every_number(dtype):
+    """(1, 0, 0, 1) for all 16-bit patterns, or those of fp32 with the same upper halves: zeros of both signs, subnormals, infinities."""
+    import torch
+    import paper_2605_02218_amd as C
+    bits = np.arange(1 << 16, dtype=np.uint32)
+    if dtype == "fp32":
+        z = torch.from_numpy((bits << 16 | bits * 40503 & 0xFFFF).astype(np.uint32).view(np.int32)).view(torch.float32)
+        z[0], z[1 << 15], z[0x7F80], z[0xFF80] = 0.0, -0.0, float("inf"), -float("inf")
+    else:
+        z = torch.from_numpy(bits.astype(np.uint16).view(np.int16)).view(torch_dtype(dtype))
+    z = z.reshape(2, 4, -1)
+    V = z.shape[2]
+    starts = torch.tensor([0, V, 2 * V], dtype=torch.int32, device="cuda")
+    words = torch.arange(V, dtype=torch.int32, device="cuda").repeat(2)
+    pen = torch.tensor([[1.0, 0, 0, 1], [1.0, 0, 0, 0]], device="cuda")
+    p = C.LogitsParams(2, 4, V, {"bf16": C.BF16, "fp16": C.FP16, "fp32": C.FP32}[dtype])
+    for history, at, kw in ((words[:0], torch.zeros_like(starts), {}), (words, starts, {}),
+                            (words, starts, dict(prompt_len=torch.tensor([V, 7], dtype=torch.int32, device="cuda"), drafted=words[:8].reshape(2, 4).contiguous())),
+                            (words, starts, dict(allowed=torch.full((2, 4, V // 32), -1, dtype=torch.int32, device="cuda")))):
+        out = C.adjust_logits(p, z.cuda(), history, at, pen, **kw).cpu()
+        number = ~torch.isnan(z)
+        kind = torch.int32 if dtype == "fp32" else torch.int16
+        assert torch.equal(out.view(kind)[number], z.view(kind)[number])
+        assert bool(torch.isnan(out)[~number].all())
