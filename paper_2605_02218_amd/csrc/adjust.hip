@@ -72,14 +72,15 @@ __global__ __launch_bounds__(AT) void adjust_kernel(Adjust a, int L, int V) {
     for (int e = 0; e < N; e += 4) *(u32x4_t*)(entry + tid * N + e) = (u32x4_t){};
   }
   __syncthreads();
-  const int h0 = a.history_start[s], h1 = a.history_start[s + 1];
-  const int cut = h0 + (a.prompt_len ? a.prompt_len[s] : 0);
+  // counted from the history's own beginning: a prompt_len of any size, the largest there is included, only ever means the words in front of it
+  const int h0 = a.history_start[s], asked = a.prompt_len ? a.prompt_len[s] : 0;
+  const unsigned words = (unsigned)max(a.history_start[s + 1] - h0, 0);
 #pragma unroll 4
-  for (int i = h0 + tid; i < h1; i += AT) {
-    const int w = a.history[i];
+  for (unsigned i = tid; i < words; i += AT) {
+    const int w = a.history[h0 + (int)i];
     const unsigned at = (unsigned)w - (unsigned)w0;
     if (w >= 0 && w < V && at < (unsigned)(AT * N)) {
-      if (i < cut) atomicOr(seen + at, 1); else atomicAdd(seen + at, 2);
+      if ((int)i < asked) atomicOr(seen + at, 1); else atomicAdd(seen + at, 2);
     }
   }
   int b0 = 0;

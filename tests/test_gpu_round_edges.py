@@ -50,3 +50,20 @@ def test_adjustments_without_an_effect_keep_every_number(dtype):
         kind = torch.int32 if dtype == "fp32" else torch.int16
         assert torch.equal(out.view(kind)[number], z.view(kind)[number])
         assert bool(torch.isnan(out)[~number].all())
+
+
+@pytest.mark.parametrize("most", [1 << 20, (1 << 31) - 100, (1 << 31) - 1])
+def test_a_prompt_longer_than_the_history_is_all_of_it(most):
+    import torch
+    import paper_2605_02218_amd as C
+    S, L, V = 3, 2, 4096
+    z = torch.linspace(-3, 3, S * L * V, device="cuda").reshape(S, L, V)
+    words = torch.arange(0, 900, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 300, 600, 900], dtype=torch.int32, device="cuda")
+    pen = torch.tensor([[1.5, 0.5, 0.25, 1.0]] * S, device="cuda")
+    asked = lambda n: torch.full((S,), n, dtype=torch.int32, device="cuda")  # noqa: E731
+    p = C.LogitsParams(S, L, V, C.FP32)
+    want = C.adjust_logits(p, z, words, starts, pen, prompt_len=asked(300))
+    assert torch.equal(C.adjust_logits(p, z, words, starts, pen, prompt_len=asked(most)), want)
+    # and one below zero is none
+    assert torch.equal(C.adjust_logits(p, z, words, starts, pen, prompt_len=asked(-most)), C.adjust_logits(p, z, words, starts, pen))
