@@ -532,8 +532,8 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
  *   bias_start [n_seq + 1], bias_word int32, bias_value fp32, or all three NULL
  *   allowed   [n_seq, n_pos, (vocab + 31) / 32] 32-bit words, bit w % 32 of word w / 32 set = w allowed; or NULL
  * Words outside [0, vocab) are nobody's.  Limits as covspec_verify, with n_pos in the place of n_draft: n_pos <= 64,
- * n_seq * n_pos <= 65535, vocab a multiple of 8 (bf16, fp16) or 4 (fp32).  No workspace; one launch on `stream`, does not
- * synchronise, allocates nothing.
+ * n_seq * n_pos <= 65535, vocab a multiple of 8 (bf16, fp16) or 4 (fp32) and below 2^30.  No workspace; one launch on
+ * `stream`, does not synchronise, allocates nothing.
  */
 typedef struct covspec_logits_params {
   int32_t n_seq;    /* S                                                    */

@@ -874,7 +874,7 @@ int covspec_adjust_logits(const covspec_logits_params* p, const void* z, const i
   if (p->n_seq < 1 || p->n_pos < 1 || p->vocab < 2) return COVSPEC_INVALID_ARG;
   if (p->dtype != COVSPEC_FP32 && p->dtype != COVSPEC_BF16 && p->dtype != COVSPEC_FP16) return COVSPEC_INVALID_ARG;
   if (p->n_pos > 64 || (long)p->n_seq * p->n_pos > 65535) return COVSPEC_UNSUPPORTED;
-  if (p->vocab % (p->dtype == COVSPEC_FP32 ? 4 : 8) != 0) return COVSPEC_UNSUPPORTED;
+  if (p->vocab % (p->dtype == COVSPEC_FP32 ? 4 : 8) != 0 || p->vocab >= 1 << 30) return COVSPEC_UNSUPPORTED;      // words and grids count in 32 bits
   if (!z || !history || !history_start || !penalties || !z_out) return COVSPEC_INVALID_ARG;
   if ((bias_start != nullptr) != (bias_word != nullptr) || (bias_start != nullptr) != (bias_value != nullptr)) return COVSPEC_INVALID_ARG;
   if (((uintptr_t)z | (uintptr_t)z_out) & 15) return COVSPEC_INVALID_ARG;

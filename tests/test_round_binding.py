@@ -1,6 +1,9 @@
 """Host-side checks of what the binding makes of tensors before the library sees them (no GPU work is launched)."""
+import ctypes
+
 import pytest
 
+import paper_2605_02218_amd as C
 from paper_2605_02218_amd import binding as Bd
 
 
@@ -41,3 +44,11 @@ def test_a_workspace_is_what_lies_behind_its_first_aligned_byte():
     for bad in (_OnDevice(x[:1].expand(4096)), _OnDevice(x[::2]), x):       # the last one is not on a device
         with pytest.raises(ValueError):
             Bd._ws_args(bad)
+
+
+@pytest.mark.parametrize("dtype", [C.FP32, C.BF16, C.FP16])
+def test_vocabularies_beyond_the_word_indexes_are_refused(dtype):
+    fake = 4096                 # never dereferenced
+    for vocab in ((1 << 31) - 8, 1 << 30):
+        cs = C.LogitsParams(1, 1, vocab, dtype).c_struct()
+        assert C.load_library().covspec_adjust_logits(ctypes.byref(cs), *[fake] * 11, None) == Bd.UNSUPPORTED
