@@ -64,7 +64,7 @@ __global__ __launch_bounds__(AT) void adjust_kernel(Adjust a, int L, int V) {
     mask[t] = 0;
     fetch(t, t);
   }
-  const int lane = tid & 63, word_of = a.drafted && lane < L ? a.drafted[row0 + lane] : -1;
+  const int lane = tid & 63, word_of = a.drafted && lane < L - 1 ? a.drafted[row0 + lane] : -1;      // no row lies behind the last
 #pragma unroll
   for (int e = 0; e < N; e += 4) *(u32x4_t*)(seen + tid * N + e) = (u32x4_t){};
   if (a.bias_start) {

@@ -67,3 +67,27 @@ def test_a_prompt_longer_than_the_history_is_all_of_it(most):
     assert torch.equal(C.adjust_logits(p, z, words, starts, pen, prompt_len=asked(most)), want)
     # and one below zero is none
     assert torch.equal(C.adjust_logits(p, z, words, starts, pen, prompt_len=asked(-most)), C.adjust_logits(p, z, words, starts, pen))
+
+
+@pytest.mark.parametrize("L", [1, 5, 64])
+def test_the_last_drafted_column_has_no_effect(L):
+    """The library is given an array that ends in front of its last element."""
+    import ctypes
+    import torch
+    import paper_2605_02218_amd as C
+    S, V = 2, 2048
+    z = torch.linspace(-3, 3, S * L * V, device="cuda").reshape(S, L, V).to(torch.bfloat16)
+    none = torch.zeros(S + 1, dtype=torch.int32, device="cuda")
+    pen = torch.tensor([[1.5, 0.5, 0.25, 1.0]] * S, device="cuda")
+    drafted = torch.randint(0, 9, (S, L), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    p = C.LogitsParams(S, L, V)
+    want = C.adjust_logits(p, z, none[:0], none, pen, drafted=drafted)
+    for other in (0, 5, V - 1, -1, V):
+        d = drafted.clone()
+        d[:, -1] = other
+        assert torch.equal(C.adjust_logits(p, z, none[:0], none, pen, drafted=d), want)
+    short, out, cs = drafted.reshape(-1)[:-1].clone(), torch.empty_like(z), p.c_struct()
+    st = C.load_library().covspec_adjust_logits(ctypes.byref(cs), z.data_ptr(), none.data_ptr(), none.data_ptr(), None, short.data_ptr(), pen.data_ptr(), None, None,
+                                                None, None, out.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert st == 0 and torch.equal(out, want)
