@@ -574,10 +574,11 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
     early();                                                           // what is loaded while the exponentials are taken
     float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
     if (__builtin_expect(far, 0)) {
+      const float from = m == -INFINITY ? 0.f : m;                     // then all scores are -infinity or NaN: zeros or NaN
 #pragma unroll
       for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[x][e] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((z[x][e] - m) * c2);
+        for (int e = 0; e < 8; ++e) z[x][e] = __builtin_amdgcn_exp2f((z[x][e] - from) * c2);
     } else {
 #pragma unroll
       for (int x = 0; x < NX; ++x)

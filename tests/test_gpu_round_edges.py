@@ -91,3 +91,26 @@ def test_the_last_drafted_column_has_no_effect(L):
                                                 None, None, out.data_ptr(), torch.cuda.current_stream().cuda_stream)
     torch.cuda.synchronize()
     assert st == 0 and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("kept", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 12, 30, 70, 600])
+def test_a_query_of_nan_beside_scores_of_the_largest_numbers(new, kept):
+    """Scores of 2^127 lie beyond the range of their own base-2 exponents; a row of NaN among them is NaN, the others the mean of v."""
+    import torch
+    import paper_2605_02218_amd as C
+    b = Batch(np.random.default_rng(2), [new], [new + 90], 16)
+    p = b.params(1, 64, "bf16", kept)
+    k = torch.zeros(b.n_pages, 1, 16, 64)
+    k[..., 0] = 2.0 ** (63 if kept == "bf16" else 8)
+    scale = None if kept == "bf16" else torch.full(k.shape[:3], 2.0 ** 55, device="cuda")
+    v, one = torch.full_like(k, 0.75), None if kept == "bf16" else torch.ones(k.shape[:3], device="cuda")
+    q = torch.zeros(new, 2, 64, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 2.0 ** 64
+    q[0, 0, 5] = float("nan")
+    t = torch_dtype(kept)
+    out, lse = C.attend(C.AttendParams(cache=p, n_heads=2, max_len=new + 90, scale=1.0), q, *b.device(), (k.to(t).cuda(), v.to(t).cuda(), scale, one), want_lse=True)
+    assert bool(torch.isnan(out[0, 0]).all()) and bool(torch.isnan(lse[0, 0]))
+    rest = torch.ones(new, 2, dtype=torch.bool, device="cuda")
+    rest[0, 0] = False
+    assert bool((out[rest] == 0.75).all()) and bool((lse[rest] == 2.0 ** 127).all())
