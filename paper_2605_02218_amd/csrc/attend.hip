@@ -234,6 +234,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
   typedef Form<DT, WIDE ? DT : KEPT, D> W;               // of the tiles that are multiplied
   constexpr bool RAW = CODES && !WIDE;
   constexpr bool TURNS = RW == 8;                        // see the loop over the tiles
+  constexpr bool AGAIN = KEPT != DT_I8 && RW > 1, CLEAR = KEPT != DT_I8 && RW == 1;      // v that is not finite: see in front of sums
   static_assert(!TURNS || (KW == 1 && KT == 64 && !CODES), "");
   typedef Operand<DT, M> P1;
   typedef Operand<VDT, M> P2;
@@ -447,7 +448,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       const int y = i * 64 * RW + me, row = y / F::CH, piece = y % F::CH;
       if (F::PIECES == F::CH || piece < F::PIECES) {
         const int from = row * F::ROWB + (piece ^ F::turn(row)) * 16, to = row * W::ROWB + ((2 * piece) ^ W::turn(row)) * 16;
-        const u32x4_t kk = *(const __attribute__((address_space(3))) u32x4_t*)(raw + from), vv = *(const __attribute__((address_space(3))) u32x4_t*)(raw + TILE + from);
+        const u32x4_t kk = *(const __attribute__((address_space(3))) u32x4_t*)(raw + from);
+        const u32x4_t vv = *(const __attribute__((address_space(3))) u32x4_t*)(raw + TILE + from);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = h == 0 ? to : to ^ 16;                        // the next piece
@@ -518,6 +520,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       }
     }
   };
+  bool partial = false;                                                // some row of the wave does not see all of the tile
+  bool again = false, left = false;                                    // AGAIN: second pass over the tiles; the products of the last one with v are left out
+  auto seen_in_part = [&](int j0, unsigned ok) { return j0 + KT > min(khi_min, hi) || j0 < klo_max || ok != (1u << KT / 16) - 1; };
   auto probabilities = [&](int t, unsigned ok, int stage, auto early) {
     const int j0 = lo + t * KT;
     const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(base + stage * STAGE + 2 * TILE);
@@ -531,7 +536,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
           for (int e = 0; e < 4; ++e) z[x][4 * f + e] *= w[e];
         }
     }
-    const bool partial = j0 + KT > min(khi_min, hi) || j0 < klo_max || ok != (1u << KT / 16) - 1;
+    partial = seen_in_part(j0, ok);
+    if constexpr (AGAIN) left = partial && again;
     if (partial) {
       // bit x: the lane's row sees position j0 + x
       auto below = [](int x) { return x <= 0 ? 0ull : x >= 64 ? ~0ull : (1ull << x) - 1; };
@@ -621,12 +627,143 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       if constexpr (SPLIT_P) o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, rest[x]), o[d]);
     }
   };
-  auto sums = [&](int stage) {                                         // the first step is on its way
+  // A position that a row does not see has p = 0 for it, but 0 * v is NaN if that v is not finite (of codes only e4m3 has such: its NaN).
+  //   CLEAR, waves with tiles of their own: in tiles that are not seen whole such numbers are replaced by zeros in front of the products, in the
+  //     registers of the operand, and added afterwards to the rows that see them (infinity times any p > 0 is infinity, NaN is NaN).
+  //   AGAIN, waves that share tiles and that the test costs more: a workgroup whose sums have come out NaN goes over its tiles again, without the products
+  //     with v of those that are not seen whole, and adds these term by term.  us, without either / with the test in the operands or while a tile is
+  //     widened / so: prompts of 4 x 3008 tokens 731, 782, 751; 88 rows behind 8192 positions 384, 396, 386; 2048 tokens behind 14336 of an e4m3 cache
+  //     1459, 1527, 1468.
+  constexpr uint32_t TOP = CODES ? 0x7F7F7F7Fu : VDT == DT_BF16 ? 0x7F807F80u : 0x7C007C00u, ONE = CODES ? 0x01010101u : VDT == DT_BF16 ? 0x00800080u : 0x04000400u;
+  constexpr uint32_t SIGN = CODES ? 0x80808080u : 0x80008000u;
+  constexpr int FIELD = CODES ? 8 : 16;
+  auto infinite_in = [](uint32_t w) { return ((w & TOP) + ONE) & SIGN; };                  // the sign bits of those fields
+  auto cleared = [](uint32_t w, uint32_t hit) { return w & ~(hit | (hit - (hit >> (FIELD - 1)))); };
+  auto clear_infinite = [&](int i) __attribute__((always_inline)) {                        // of the operand vf[i]: any in the wave?
+    uint32_t hit = 0;
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int w = 0; w < (RAW ? 2 : 4); ++w) hit |= infinite_in(vf[i][d][w]);
+    if (!__any(hit != 0)) return false;
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int w = 0; w < (RAW ? 2 : 4); ++w) vf[i][d][w] = cleared(vf[i][d][w], infinite_in(vf[i][d][w]));
+    return true;
+  };
+  auto row_sees = [&](int t, unsigned ok, int x) __attribute__((always_inline)) {           // the lane's row, position x of tile t
+    const int j = lo + t * KT + x;
+    const bool see = a.visible && j >= old ? j - old < 64 && (bits >> (j - old) & 1) : j >= klo && j < khi;
+    return see && has && j < hi && (ok >> (x >> 4) & 1);
+  };
+  auto add_infinite = [&](int t, unsigned ok, int stage) __attribute__((always_inline)) {
+    const lds_char* const vt = (const lds_char*)(base + stage * STAGE + TILE);
+#pragma unroll 1
+    for (int x = 0; x < KT; ++x) {
+      const bool see = row_sees(t, ok, x);
+#pragma unroll
+      for (int d = 0; d < DM; ++d)
+#pragma unroll
+        for (int b = 0; b < CA / 4; ++b) {
+          const int col = M * d + 8 * b + 4 * grp, piece = CODES ? col >> 4 : col >> 3;       // the first of the lane's four columns
+          const lds_char* const from = vt + x * F::ROWB + (piece ^ F::turn(x)) * 16 + (CODES ? col & 15 : (col & 7) * 2);
+          f32x4_t v;
+          if constexpr (CODES) {
+            v = decode4<KEPT>(*(const __attribute__((address_space(3))) uint32_t*)from);
+          } else {
+            const u32x2_t w = *(const __attribute__((address_space(3))) u32x2_t*)from;
+            const f32x2_t f0 = Half<DT>::unpack(w[0]), f1 = Half<DT>::unpack(w[1]);
+            v = (f32x4_t){f0[0], f0[1], f1[0], f1[1]};
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[d][4 * b + e] += see && !(fabsf(v[e]) < INFINITY) ? v[e] : 0.f;
+        }
+    }
+  };
+  auto sums = [&](int t, unsigned ok, int stage) __attribute__((always_inline)) {          // the first step is on its way
+    bool infinite = false;
 #pragma unroll
     for (int x = 0; x < NX; ++x) {
       if (x + 1 < NX) load_v(stage, x + 1);
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (CLEAR)
+        if (partial) infinite |= clear_infinite(x & 1);
       multiply_v(x);
+    }
+    if constexpr (CLEAR)
+      if (__builtin_expect(infinite, 0)) add_infinite(t, ok, stage);
+  };
+
+  // AGAIN: behind the first pass, whether there is a second one; all waves of the workgroup together.
+  __attribute__((address_space(3))) int* const vote = (__attribute__((address_space(3))) int*)(lds_char*)(smem + KW * GROUP);
+  auto once_more = [&]() __attribute__((always_inline)) {
+    if (!AGAIN || again) return false;
+    bool nan = false;
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int e = 0; e < CA; ++e) nan |= o[d][e] != o[d][e];
+    if (nan && has) *vote = 1;
+    wait_lds();
+    meet();
+    again = __builtin_amdgcn_readfirstlane(*vote) != 0;
+    if (!again) return false;
+    wait_lds();                                                        // all have read it
+    meet();
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int e = 0; e < CA; ++e) o[d][e] = 0.f;
+    m = -INFINITY;
+    ref = sum = 0.f;
+    far = left = false;
+    return true;
+  };
+  auto add_left_out = [&]() __attribute__((always_inline)) {
+    if (!AGAIN || !again) return;
+    for (int t = kw; t < count; t += KW) {
+      const int j0 = lo + t * KT;
+      if (!seen(t) || !seen_in_part(j0, exist(look_up(t)))) continue;
+#pragma unroll 1
+      for (int j = j0; j < min(j0 + KT, hi); ++j) {
+        const long x = place_of(c, s, j, g);
+        const bool see = has && x >= 0 && (a.visible && j >= old ? j - old < 64 && (bits >> (j - old) & 1) : j >= klo && j < khi);
+        if (!__any(see)) continue;
+        float y = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const u32x4_t w = __builtin_bit_cast(u32x4_t, q[k]);
+          u32x4_t kk;
+          if constexpr (CODES) kk = widen8<DT, KEPT>(*(const u32x2_t*)((const char*)a.kc + x * D + KM * k + 8 * grp));
+          else kk = *(const u32x4_t*)((const char*)a.kc + (x * D + KM * k + 8 * grp) * 2);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const f32x2_t u = Half<DT>::unpack(w[e]), v = Half<DT>::unpack(kk[e]);
+            y += u[0] * v[0] + u[1] * v[1];
+          }
+        }
+        y = row_sum<M>(y);
+        if constexpr (CODES) y *= a.ks[x];
+        float p = __builtin_amdgcn_exp2f((y - m) * c2);
+        if constexpr (CODES) p *= a.vs[x];
+#pragma unroll
+        for (int d = 0; d < DM; ++d)
+#pragma unroll
+          for (int b = 0; b < CA / 4; ++b) {
+            const long from = x * D + M * d + 8 * b + 4 * grp;
+            f32x4_t v;
+            if constexpr (CODES) {
+              v = decode4<KEPT>(*(const uint32_t*)((const char*)a.vc + from));
+            } else {
+              const u32x2_t w = *(const u32x2_t*)((const char*)a.vc + from * 2);
+              const f32x2_t f0 = Half<DT>::unpack(w[0]), f1 = Half<DT>::unpack(w[1]);
+              v = (f32x4_t){f0[0], f0[1], f1[0], f1[1]};
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[d][4 * b + e] = see ? __builtin_fmaf(p, v[e], o[d][4 * b + e]) : o[d][4 * b + e];
+          }
+      }
     }
   };
 
@@ -655,7 +792,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       meet();
       __builtin_amdgcn_sched_barrier(0);
     };
-    if (count > 0) {
+    while (count > 0) {
+      if (tid == 0) *vote = 0;                                         // all meet behind it and in front of its use
+      ring = sent = 0;
       next = look_up(0);
       send();
       send();
@@ -669,9 +808,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
         if (!second) send();
         // the first half of K on its way before the products with V, the second before those with the first
         load_k(t & 3, 0);
-        if (t > 0 && seen(t - 1)) {
+        if (t > 0 && seen(t - 1) && !left) {
           load_v((t - 1) & 3, 0);
-          sums((t - 1) & 3);
+          sums(t - 1, 0, (t - 1) & 3);
         }
         load_k(t & 3, 1);
         __builtin_amdgcn_sched_barrier(0);
@@ -684,22 +823,24 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
         if (second) arrived(t + 1);
         slot();
         if (second) send();
-        if (seen(t)) {
-          probabilities(t, ring >> 4 * (t & 3) & 15, t & 3, [] {});
-        }
+        if (seen(t)) probabilities(t, ring >> 4 * (t & 3) & 15, t & 3, [] {});
         if (!second) arrived(t + 1);
         slot();
       }
       if (!second) slot();
-      if (seen(count - 1)) {
+      if (seen(count - 1) && !left) {
         load_v((count - 1) & 3, 0);
-        sums((count - 1) & 3);
+        sums(count - 1, 0, (count - 1) & 3);
       }
+      if (!once_more()) break;
     }
+    add_left_out();
   } else if (count > 0) {
     // tile t of the group's: fetched while the one before is computed.  All waves of a workgroup meet as often as the group with most tiles needs.
     const int mine = kw < count ? (count - kw + KW - 1) / KW : 0, most = (count + KW - 1) / KW;
+    do {
     Pages now, next;
+    if (AGAIN && tid == 0) *vote = 0;                                  // all meet behind it and in front of its use
     if (mine > 0) { now = look_up(kw); fetch(kw, now, 0); }
     if (mine > 1) next = look_up(kw + KW);
     for (int t = 0; t < most; ++t) {
@@ -731,68 +872,16 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
       if (work && seen(kw + t * KW)) {
         scores(t & 1);
         probabilities(kw + t * KW, ok, t & 1, [&] { load_v(t & 1, 0); });
-        sums(t & 1);
+        if (!left) sums(kw + t * KW, ok, t & 1);
       }
       __builtin_amdgcn_sched_barrier(0);
       wait_lds();                                                      // nothing reads the stage that is filled next
       if constexpr (RW > 1 && !WIDE) meet();
     }
+    } while (once_more());
+    add_left_out();
   }
 
-  // ---- NaN: 0 * v of a position that some row of the tile does not see may have made it, if that v is not finite.  The rows are summed again,
-  // term by term with the products left out.
-  bool nan = false;
-#pragma unroll
-  for (int d = 0; d < DM; ++d)
-#pragma unroll
-    for (int e = 0; e < CA; ++e) nan |= o[d][e] != o[d][e];
-  if (__any(nan)) {
-#pragma unroll
-    for (int d = 0; d < DM; ++d)
-#pragma unroll
-      for (int e = 0; e < CA; ++e) o[d][e] = 0.f;
-    for (int t = kw; t < count; t += KW)
-      for (int j = lo + t * KT; j < min(lo + t * KT + KT, hi); ++j) {
-        const long x = place_of(c, s, j, g);
-        bool see = has && x >= 0 && j >= klo && j < khi;
-        if (a.visible && j >= old) see = has && x >= 0 && j - old < 64 && (bits >> (j - old) & 1);
-        if (!__any(see)) continue;
-        float y = 0.f;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const u32x4_t w = __builtin_bit_cast(u32x4_t, q[k]);
-          u32x4_t kk;
-          if constexpr (CODES) kk = widen8<DT, KEPT>(*(const u32x2_t*)((const char*)a.kc + x * D + KM * k + 8 * grp));
-          else kk = *(const u32x4_t*)((const char*)a.kc + (x * D + KM * k + 8 * grp) * 2);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f32x2_t u = Half<DT>::unpack(w[e]), v = Half<DT>::unpack(kk[e]);
-            y += u[0] * v[0] + u[1] * v[1];
-          }
-        }
-        y = row_sum<M>(y);
-        if constexpr (CODES) y *= a.ks[x];
-        float p = __builtin_amdgcn_exp2f((y - m) * c2);
-        if constexpr (CODES) p *= a.vs[x];
-#pragma unroll
-        for (int d = 0; d < DM; ++d)
-#pragma unroll
-          for (int b = 0; b < CA / 4; ++b) {
-            const long from = x * D + M * d + 8 * b + 4 * grp;
-            float v[4];
-            if constexpr (CODES) {
-              const f32x4_t f = decode4<KEPT>(*(const uint32_t*)((const char*)a.vc + from));
-              v[0] = f[0]; v[1] = f[1]; v[2] = f[2]; v[3] = f[3];
-            } else {
-              const u32x2_t w = *(const u32x2_t*)((const char*)a.vc + from * 2);
-              const f32x2_t f0 = Half<DT>::unpack(w[0]), f1 = Half<DT>::unpack(w[1]);
-              v[0] = f0[0]; v[1] = f0[1]; v[2] = f1[0]; v[3] = f1[1];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[d][4 * b + e] = see ? __builtin_fmaf(p, v[e], o[d][4 * b + e]) : o[d][4 * b + e];
-          }
-      }
-  }
   sum = row_sum<M>(sum);
   m *= unit;                                             // in units of the scores
 
@@ -961,7 +1050,7 @@ template <int DT, int KEPT, int D, int M, int RW, int KW, int KT>
 hipError_t launch_form(const Paged& c, const Attend& a, const Plan& p, void* ws, hipStream_t stream) {
   typedef Form<DT, KEPT, D> F;
   constexpr size_t stage = 2 * KT * F::ROWB + (KEPT != DT ? 8 * KT : 0), wide = KEPT != DT && RW > 1 ? 2 * KT * Form<DT, DT, D>::ROWB : 0, slots = (size_t)(KW - 1) * RW * (D * M * 4 + 512);
-  constexpr size_t tiles = KW * ((RW == 8 ? 4 : 2) * stage + wide), lds = tiles > slots ? tiles : slots;
+  constexpr size_t tiles = KW * ((RW == 8 ? 4 : 2) * stage + wide) + (KEPT != DT_I8 && RW > 1 ? 16 : 0), lds = tiles > slots ? tiles : slots;
   static PerDeviceInt raised;
   hipError_t e = ensure_dynamic_lds(raised, (const void*)attend_kernel<DT, KEPT, D, M, RW, KW, KT>, lds);
   if (e != hipSuccess) return e;

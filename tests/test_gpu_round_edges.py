@@ -2,7 +2,8 @@
 import numpy as np
 import pytest
 
-from round_util import Batch, torch_dtype
+from oracle import round_oracle as RO
+from round_util import HALF_STEP, Batch, pool_of, rounded, torch_dtype
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +115,61 @@ def test_a_query_of_nan_beside_scores_of_the_largest_numbers(new, kept):
     rest = torch.ones(new, 2, dtype=torch.bool, device="cuda")
     rest[0, 0] = False
     assert bool((out[rest] == 0.75).all()) and bool((lse[rest] == 2.0 ** 127).all())
+
+
+@pytest.mark.parametrize("dtype,kept", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3"), ("fp16", "e4m3"), ("bf16", "int8"), ("fp16", "int8")])
+@pytest.mark.parametrize("D,new,window,tree", [(64, 1, 0, False), (128, 2, 60, False), (96, 6, 0, True), (128, 12, 0, False), (128, 30, 0, True), (96, 60, 33, False),
+                                               (64, 160, 0, False), (96, 300, 0, False), (128, 300, 100, False), (64, 290, 0, True)])
+def test_numbers_that_are_not_finite_reach_the_rows_that_see_them(dtype, kept, D, new, window, tree):
+    """Infinities and NaN in v, some seen by all rows, some by a few, some by none, one on a page that does not exist for the sequence: of a row, the columns
+    without any keep the tolerance of finite sums (tests of the attention itself), the others are what the formula gives.  Scores are within +-4 of each
+    other, so that no p vanishes."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(D + new)
+    H, heads, old = 2, 4, 150
+    length = old + new
+    b = Batch(rng, [new], [length], 16)
+    k = pool_of(rng.standard_normal((b.n_pages, H, 16, D)), kept, dtype)
+    v = pool_of(rng.standard_normal((b.n_pages, H, 16, D)) + 0.5, kept, dtype)
+    q, q64 = rounded(0.3 * rng.standard_normal((new, heads, D)), dtype)
+    b.pages[0, 4] = -1                                  # positions 64 .. 79; the first page of the pool is loaded in its place
+    spoilt = [(j, float(x)) for j, x in ((3, np.inf), (70, np.nan), (old - 2, -np.inf), (old, np.nan), (length - 1, np.inf), (length - 1 - new // 2, np.inf))]
+    codes, v64 = v[0].clone(), v[2].copy()
+    for i, (j, x) in enumerate(spoilt):
+        page, at = RO.place(j, b.pages[0], 16, b.n_pages) or (0, 5)
+        cols = slice(5 * i % D, 5 * i % D + 3)
+        if kept == dtype:
+            codes[page, :, at, cols], v64[page, :, at, cols] = x, x
+        elif kept == "e4m3" and i < 2:
+            codes[page, :, at, cols], v64[page, :, at, cols] = float("nan"), np.nan       # a code that is none
+        else:
+            v[1][page, :, at], v64[page, :, at] = float("nan"), np.nan                    # as an infinity is written in 8 bits
+    bits = None
+    if tree:
+        bits = [int(x) for x in rng.integers(-(1 << 63), 1 << 63, new, dtype=np.int64)]
+        bits[0] = 0
+    p = C.AttendParams(cache=b.params(H, D, dtype, kept), n_heads=heads, max_len=length, window=window, scale=D ** -0.5)
+    pool = tuple(None if t is None else t.cuda() for t in (k[0], codes, k[1], v[1]))
+    vis = None if bits is None else torch.tensor(bits, dtype=torch.int64, device="cuda")
+    out, lse = C.attend(p, q.cuda(), *b.device(), pool, visible=vis, want_lse=True)
+    out, lse, u = out.float().cpu().numpy().astype(np.float64), lse.cpu().numpy(), HALF_STEP[dtype]
+    for i in list(range(0, new, 17)) + [new - 1, new // 2, max(new - 2, 0)]:
+        seen = RO.seen_by(i, new, length, window, None if bits is None else bits[i] & ((1 << 64) - 1))
+        at = [x for x in (RO.place(j, b.pages[0], 16, b.n_pages) for j in seen) if x is not None]
+        pg, of = np.array([x[0] for x in at], dtype=int), np.array([x[1] for x in at], dtype=int)
+        for h in range(heads):
+            K, V = k[2][pg, h // 2, of], v64[pg, h // 2, of]
+            z = K @ q64[i, h].astype(np.float64) * D ** -0.5
+            w = np.exp(z - z.max())
+            terms = w[:, None] * V / w.sum()
+            with np.errstate(invalid="ignore"):
+                want, A = terms.sum(0), np.abs(terms).sum(0)
+            fine = np.isfinite(want)
+            size = float((np.abs(K) @ np.abs(q64[i, h])).max()) * D ** -0.5
+            rel = 2 * (D + 64) * 2.0 ** -24 * size
+            tol = u * np.abs(want) + (2 * u + rel + 2.0 ** -19) * A + 2.0 ** -25 * (1 + np.abs(np.where(np.isfinite(V), V, 0.0)).sum(0))
+            assert np.all(np.abs(out[i, h][fine] - want[fine]) <= tol[fine]), (i, h)
+            np.testing.assert_array_equal(out[i, h][~fine], want[~fine], err_msg="row %d head %d" % (i, h))
+            e = z.max() + np.log(w.sum())
+            assert abs(lse[i, h] - e) <= rel + 2.0 ** -20 * (1 + abs(e))
