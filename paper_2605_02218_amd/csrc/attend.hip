@@ -733,8 +733,11 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
         float y = 0.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          const u32x4_t w = __builtin_bit_cast(u32x4_t, q[k]);
-          u32x4_t kk;
+          u32x4_t w = __builtin_bit_cast(u32x4_t, q[k]), kk;
+          if constexpr (TURNS) {                                       // read again: with it kept to here prompts take 1 % longer
+            w = (u32x4_t){};
+            if (has) w = *(const u32x4_t*)((const uint16_t*)a.q + t_row * a.q_pitch + (long)head * D + KM * k + 8 * grp) ^ flip;
+          }
           if constexpr (CODES) kk = widen8<DT, KEPT>(*(const u32x2_t*)((const char*)a.kc + x * D + KM * k + 8 * grp));
           else kk = *(const u32x4_t*)((const char*)a.kc + (x * D + KM * k + 8 * grp) * 2);
 #pragma unroll
