@@ -1035,8 +1035,10 @@ Plan plan_of(const Paged& c, int heads, int max_len) {
   p.sp.unit = p.rw == 1 ? 128 : 64;                  // a tile for each wave that takes tiles of its own
   p.sp.least = 2;                                    // a share's own beginning and end cost some units' time
   p.sp.tiles = (int)(rows / TR + c.S);               // at most: a sequence begins a tile
-  // as many shares as are at work at once: one or two on each of 256 compute units, by the LDS and registers of the form
-  const bool alone = p.rw == 8 || (p.width == 16 && c.kept == c.dtype && c.D > 64);
+  // As many shares as are at work at once: one or two on each of 256 compute units, by the LDS of the form; four waves with two stages of 16-bit tiles of
+  // their own, in rows of 256 bytes, take 128 of its 160 KB, as do eight that take turns.  us for 8 tokens of 4 heads for each of 8 key heads of 128, 256 shares
+  // and 512: one sequence of 30000 positions 39 and 50, 8 of 900 to 6100 36 and 49, 16 71 and 79, 32 (no shares with the one, shares with the other) 105 and 118.
+  const bool alone = p.rw == 8 || (p.rw == 1 && c.kept == c.dtype && c.D > 64);
   const int slots = alone ? 256 : 512;
   const long items = (long)p.sp.tiles * c.H, units = (max_len + p.sp.unit - 1) / p.sp.unit;
   const bool share = 2 * about(TR) <= slots && (double)items * units < 2e9;       // units are counted in 32 bits

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import test_gpu_attend as TA
 from oracle import round_oracle as RO
 from round_util import HALF_STEP, Batch, pool_of, rounded, torch_dtype
 
@@ -173,3 +174,16 @@ def test_numbers_that_are_not_finite_reach_the_rows_that_see_them(dtype, kept, D
             np.testing.assert_array_equal(out[i, h][~fine], want[~fine], err_msg="row %d head %d" % (i, h))
             e = z.max() + np.log(w.sum())
             assert abs(lse[i, h] - e) <= rel + 2.0 ** -20 * (1 + abs(e))
+
+
+KINDS = [("bf16", "bf16"), ("bf16", "int8"), ("bf16", "e4m3"), ("fp16", "fp16"), ("fp16", "int8"), ("fp16", "e4m3")]
+
+
+@pytest.mark.parametrize("dtype,kept", KINDS)
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("new,H,window", [([8, 8, 8, 8], 2, 0), ([8] * 3 + [3, 0], 3, 90), ([8] * 150, 1, 0)])
+def test_segments_of_17_to_32_rows(dtype, kept, D, new, H, window):
+    """Eight tokens of four heads for each key head: a tile of 32 rows for each sequence, by shares and, with 150 of them, by items."""
+    rng = np.random.default_rng(20)
+    b = Batch(rng, new, [n + int(x) for n, x in zip(new, rng.integers(0, 700 if len(new) < 9 else 200, len(new)))], 32, pad=1)
+    TA.run(b, 4 * H, H, D, dtype, kept, window=window, rows=set(range(0, b.T, 1 if len(new) < 9 else 61)) | {0, b.T - 2})

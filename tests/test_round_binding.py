@@ -52,3 +52,14 @@ def test_vocabularies_beyond_the_word_indexes_are_refused(dtype):
     for vocab in ((1 << 31) - 8, 1 << 30):
         cs = C.LogitsParams(1, 1, vocab, dtype).c_struct()
         assert C.load_library().covspec_adjust_logits(ctypes.byref(cs), *[fake] * 11, None) == Bd.UNSUPPORTED
+
+
+@pytest.mark.parametrize("heads,tile", [(8, 16), (32, 32)])
+def test_shares_are_as_many_as_are_at_work_at_once(heads, tile):
+    """8 tokens, 8 key heads of 128, a 16-bit cache: four waves with 16-bit tiles of their own fill a compute unit's LDS, 256 shares; over codes two
+    workgroups fit.  A share keeps two tiles of partial sums and their statistics."""
+    for kept, shares in ((C.BF16, 256), (C.E4M3, 512)):
+        c = C.CacheParams(n_seq=1, n_tokens=8, n_kv_heads=8, head_dim=128, page_size=64, n_pages=100, max_pages=100, dtype=C.BF16, cache_dtype=kept)
+        need = C.attend_workspace_size(C.AttendParams(cache=c, n_heads=heads, max_len=6000, scale=0.1))
+        sums = 2 * shares * tile * (128 + 2) * 4
+        assert sums < need < sums + 4096
