@@ -438,7 +438,9 @@ int covspec_draft_gate(const covspec_draft_params* p, const void* z_draft, const
  *   to even (to the nearest representable value for E4M3).  amax < 2^-100: all codes and the scale are zero.  A row
  *   with an infinity or NaN gets the scale NaN and zero codes, so that it reads back as NaN.
  * With cache_dtype == dtype rows are copied bit for bit.
- * Two rows of one call for the same place: one of them is kept, which one is not said.
+ * Two rows of one call for the same place (sequences that share a page and both write there): rows that are alike leave
+ * that row; of rows that differ each element, and the scale, is one row's or the other's, not all of the same one, so
+ * a call may have such rows only where they are alike or the place is not used.
  * covspec_cache_read: code * scale (fp32, rounded once to `dtype`), or the bits, of the positions of the batch.
  *   k, v        [n_tokens, n_kv_heads, head_dim] dtype, rows `row_pitch` elements apart (0: dense), so that they may
  *               be columns of a wider tensor, e.g. of a fused projection; 16-byte aligned

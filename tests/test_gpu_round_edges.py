@@ -187,3 +187,42 @@ def test_segments_of_17_to_32_rows(dtype, kept, D, new, H, window):
     rng = np.random.default_rng(20)
     b = Batch(rng, new, [n + int(x) for n, x in zip(new, rng.integers(0, 700 if len(new) < 9 else 200, len(new)))], 32, pad=1)
     TA.run(b, 4 * H, H, D, dtype, kept, window=window, rows=set(range(0, b.T, 1 if len(new) < 9 else 61)) | {0, b.T - 2})
+
+
+@pytest.mark.parametrize("dtype,kept", KINDS)
+def test_two_rows_for_one_place(dtype, kept):
+    """Sequences that share their pages: what they write alike is there, where they differ every element is one's or the other's, other places are untouched."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(21)
+    S, n, H, D = 40, 24, 3, 96
+    b = Batch(rng, [n] * S, [n] * S, 16, spare=2)
+    b.pages[1::2] = b.pages[::2]                         # neighbours in pairs
+    x = [rounded(rng.standard_normal((S // 2, 2, n, H, D)), dtype) for _ in range(2)]
+    for t, f in x:
+        t[:, 1, :16], f[:, 1, :16] = t[:, 0, :16], f[:, 0, :16]
+    p = b.params(H, D, dtype, kept)
+    pool = C.cache_alloc(p)
+    for t in pool:
+        if t is not None:
+            t.view(torch.uint8).fill_(0x5A)
+    before = [None if t is None else t.cpu().clone() for t in pool]
+    C.cache_write(p, x[0][0].reshape(-1, H, D).cuda(), x[1][0].reshape(-1, H, D).cuda(), *b.device(), pool)
+    torch.cuda.synchronize()
+    for i in range(2):
+        got = pool[i].cpu().float().numpy()
+        scale = None if pool[2 + i] is None else pool[2 + i].cpu().numpy()
+        used = np.zeros((b.n_pages, 16), dtype=bool)
+        codes, scales = (x[i][1], None) if kept == dtype else RO.quantise(x[i][1], kept)
+        for s in range(S // 2):
+            for j in range(n):
+                page, at = RO.place(j, b.pages[2 * s], 16, b.n_pages)
+                used[page, at] = True
+                one, two = codes[s, :, j]
+                assert np.all((got[page, :, at] == one) | (got[page, :, at] == two))
+                if scale is not None:
+                    assert np.all((scale[page, :, at] == scales[s, 0, j]) | (scale[page, :, at] == scales[s, 1, j]))
+        for t, u in ((pool[i], before[i]), (pool[2 + i], before[2 + i])):
+            if t is not None:
+                rest = torch.from_numpy(~used)[:, None, :].expand(t.shape[:3])
+                assert torch.equal(t.cpu()[rest].contiguous().view(torch.uint8), u[rest].contiguous().view(torch.uint8))
