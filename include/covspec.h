@@ -319,7 +319,8 @@ int covspec_probe_launches(const covspec_params* p, int32_t* rows, int32_t* cols
  * distribution a correction is drawn from after the first rejection).  For each of n_seq sequences
  * with n_draft drafted positions tau = 0..n_draft-1 and vocabulary width vocab:
  *   p_t = softmax(z_target[s, tau, :]), p_d = softmax(z_draft[s, tau, :]);
- *   alpha[s, tau] = min(1, p_t(y) / p_d(y)) at the drafted token y = tokens[s, tau];
+ *   alpha[s, tau] = min(1, p_t(y) / p_d(y)) at the drafted token y = tokens[s, tau]; 1 where p_d(y) = 0, also if
+ *   p_t(y) = 0 (a word that the draft cannot have drawn: see the mask of covspec_adjust_logits);
  *   position tau is accepted iff u_accept[s, tau] < alpha[s, tau] (both fp32);
  *   n_accept[s] = number of accepted positions before the first rejection;
  *   if n_accept[s] < n_draft: correction[s] = the smallest word w whose cumulative residual mass
@@ -533,6 +534,9 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
  *   penalties [n_seq, 4] fp32
  *   bias_start [n_seq + 1], bias_word int32, bias_value fp32, or all three NULL
  *   allowed   [n_seq, n_pos, (vocab + 31) / 32] 32-bit words, bit w % 32 of word w / 32 set = w allowed; or NULL
+ * A segment that was drafted without the mask may hold a word that is not allowed.  With the mask on the target's logits
+ * alone covspec_verify rejects it (p_t = 0) and draws an allowed one; with the mask on both sides it has p_t = p_d = 0 and
+ * counts as accepted.  So mask the draft's logits too only if the words were drawn from logits with the same mask.
  * Words outside [0, vocab) are nobody's.  Limits as covspec_verify, with n_pos in the place of n_draft: n_pos <= 64,
  * n_seq * n_pos <= 65535, vocab a multiple of 8 (bf16, fp16) or 4 (fp32) and below 2^30.  No workspace; one launch on
  * `stream`, does not synchronise, allocates nothing.

@@ -226,3 +226,29 @@ def test_two_rows_for_one_place(dtype, kept):
             if t is not None:
                 rest = torch.from_numpy(~used)[:, None, :].expand(t.shape[:3])
                 assert torch.equal(t.cpu()[rest].contiguous().view(torch.uint8), u[rest].contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_a_drafted_word_that_is_not_allowed(dtype):
+    """With the mask on the target alone it is rejected and an allowed word drawn; with the mask on both sides, which is for words drawn under it, it
+    counts as accepted."""
+    import torch
+    import paper_2605_02218_amd as C
+    S, L, V = 4, 3, 2048
+    g = torch.Generator(device="cuda").manual_seed(3)
+    DT = {"bf16": C.BF16, "fp16": C.FP16, "fp32": C.FP32}[dtype]
+    zt = torch.randn(S, L, V, device="cuda", generator=g).to(torch_dtype(dtype))
+    zd = zt.clone()                                     # alpha = 1 but for the mask
+    drafted = torch.randint(64, V, (S, L), device="cuda", dtype=torch.int32, generator=g)
+    drafted[:, 1] = torch.tensor([0, 31, 32, 63], device="cuda", dtype=torch.int32)
+    allowed = torch.full((S, L, V // 32), -1, dtype=torch.int32, device="cuda")
+    allowed[:, :, :2] = 0                               # words 0 .. 63 are not allowed
+    none = torch.zeros(S + 1, dtype=torch.int32, device="cuda")
+    pen = torch.tensor([[1.0, 0, 0, 1]] * S, device="cuda")
+    masked = [C.adjust_logits(C.LogitsParams(S, L, V, DT), z, none[:0], none, pen, allowed=allowed) for z in (zt, zd)]
+    ua, ur = torch.full((S, L), 0.5, device="cuda"), torch.rand(S, device="cuda", generator=g)
+    vp = C.VerifyParams(S, L, V, DT)
+    n, word, alpha = C.verify(vp, masked[0], zd, drafted, ua, ur)
+    assert n.tolist() == [1] * S and alpha[:, 1].tolist() == [0.0] * S and bool((alpha[:, [0, 2]] == 1).all()) and bool((word >= 64).all())
+    n, word, alpha = C.verify(vp, *masked, drafted, ua, ur)
+    assert n.tolist() == [L] * S and bool((alpha == 1).all())
