@@ -1,8 +1,11 @@
 """Edges of the entry points around a verification round that the tests of each of them leave out: calls that the documentation allows or refuses."""
+import ctypes
+
 import numpy as np
 import pytest
 
 import test_gpu_attend as TA
+import test_round_tolerances as TT
 from oracle import round_oracle as RO
 from round_util import HALF_STEP, Batch, pool_of, rounded, torch_dtype
 
@@ -74,7 +77,6 @@ def test_a_prompt_longer_than_the_history_is_all_of_it(most):
 @pytest.mark.parametrize("L", [1, 5, 64])
 def test_the_last_drafted_column_has_no_effect(L):
     """The library is given an array that ends in front of its last element."""
-    import ctypes
     import torch
     import paper_2605_02218_amd as C
     S, V = 2, 2048
@@ -252,3 +254,127 @@ def test_a_drafted_word_that_is_not_allowed(dtype):
     assert n.tolist() == [1] * S and alpha[:, 1].tolist() == [0.0] * S and bool((alpha[:, [0, 2]] == 1).all()) and bool((word >= 64).all())
     n, word, alpha = C.verify(vp, *masked, drafted, ua, ur)
     assert n.tolist() == [L] * S and bool((alpha == 1).all())
+
+
+class _Guarded:
+    """Tensors inside a larger allocation each, with marked bytes in front of and behind them that have to stay."""
+
+    def __init__(self):
+        self.all = []
+
+    def __call__(self, t=None, shape=None, dtype=None):
+        import torch
+        shape, dtype = (t.shape, t.dtype) if t is not None else (shape, dtype)
+        n = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        room = torch.full((n + 2 * 4096 + 256,), 0x5A, dtype=torch.uint8, device="cuda")
+        inside = room[4096:4096 + n].view(dtype).reshape(shape)
+        if t is not None:
+            inside.copy_(t)
+        self.all.append((room, n))
+        return inside
+
+    def check(self):
+        import torch
+        torch.cuda.synchronize()
+        for room, n in self.all:
+            assert bool((room[:4096] == 0x5A).all()) and bool((room[4096 + n:] == 0x5A).all())
+
+
+@pytest.mark.parametrize("dtype,kept,heads,new", [("bf16", "bf16", 4, 8), ("fp16", "e4m3", 64, 8), ("bf16", "int8", 16, 1), ("fp16", "fp16", 8, 300), ("bf16", "e4m3", 8, 90),
+                                                  ("bf16", "bf16", 16, 4)])
+def test_arrays_that_describe_nothing_sensible_write_nowhere_else(dtype, kept, heads, new):
+    """Starts that do not ascend, lengths and pages out of range (every index formed from them is checked by the kernels): marked bytes around every array that
+    a call is given stay, and of the pool only places that the arrays lead to change."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(22)
+    H, D, S = 2, 64, 3
+    b = Batch(rng, [new] * S, [new + 82, new + 32, new + 56], 16)
+    T = S * new
+    t = torch_dtype(dtype)
+    k, v = (pool_of(rng.standard_normal((b.n_pages, H, 16, D)), kept, dtype) for _ in range(2))
+    p = C.AttendParams(cache=b.params(H, D, dtype, kept), n_heads=heads, max_len=b.width * 16, scale=0.1)
+    q = rounded(rng.standard_normal((T, heads, D)), dtype)[0]
+    x = rounded(rng.standard_normal((T, H, D)), dtype)[0]
+    top = (1 << 31) - 1
+    for start, length in (([5, 0, T, 3], [90, 40, 64]), ([-9, 400, -1, 7], [1 << 30, -5, 77]), ([T, T, 0, T], [-top - 1, top, 0]), ([0, T, T, 0], [3, 0, 9]),
+                          ([top, -top, 0, T], [top, top, top]), ([-top, top, -top, top], [40, -40, 1]), ([0, 0, 0, top], [60, 60, 60])):
+        guard = _Guarded()
+        pool = tuple(None if y is None else guard(y) for y in (k[0], v[0], k[1], v[1]))
+        batch = [guard(torch.tensor(y, dtype=torch.int32)) for y in (start, length)] + [
+            guard(torch.from_numpy(rng.integers(-3, b.n_pages + 3, b.pages.shape).astype(np.int32)))]
+        need = C.attend_workspace_size(p)
+        ws, out, gq, gx = guard(shape=(need,), dtype=torch.uint8), guard(shape=(T, heads, D), dtype=t), guard(q), guard(x)
+        outs = [guard(shape=(T, H, D), dtype=t) for _ in range(2)]
+        ws.fill_(0x7F)
+        assert ws.data_ptr() % 256 == 0
+        lse, cs = guard(shape=(T, heads), dtype=torch.float32), p.c_struct()
+        at = [None if y is None else y.data_ptr() for y in (gq, *batch, *pool, None, out, lse, ws)]
+        assert C.load_library().covspec_attend(ctypes.byref(cs), *at, need, torch.cuda.current_stream().cuda_stream) == 0
+        C.cache_read(p.cache, pool, *batch, k_out=outs[0], v_out=outs[1])
+        guard.check()
+        for given, here in ((q, gq), (x, gx), (k[0], pool[0]), (v[0], pool[1])):
+            assert torch.equal(given.view(torch.uint8), here.cpu().view(torch.uint8))
+        C.cache_write(p.cache, gx, gx, *batch, pool)
+        guard.check()
+        # places on pages of the table, of heads as they were: all others keep their bytes
+        table = batch[2].cpu().numpy()
+        other = np.array([pg for pg in range(b.n_pages) if pg not in table], dtype=int)
+        for given, here in ((k[0], pool[0]), (v[0], pool[1])):
+            assert torch.equal(given[other].view(torch.uint8), here.cpu()[other].view(torch.uint8))
+
+
+def test_only_the_places_of_the_rows_change():
+    """A round's rows into a pool that is full: every other byte of codes and scales is what it was."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(23)
+    for dtype, kept, D in (("bf16", "int8", 128), ("fp16", "e4m3", 96), ("bf16", "bf16", 64)):
+        H, guard = 5, _Guarded()
+        b = Batch(rng, [9, 0, 3, 17], [70, 12, 3, 300], 32, pad=4)
+        k, v = (pool_of(rng.standard_normal((b.n_pages, H, 32, D)), kept, dtype) for _ in range(2))
+        pool = tuple(None if y is None else guard(y) for y in (k[0], v[0], k[1], v[1]))
+        x = rounded(rng.standard_normal((b.T, H, D)), dtype)[0]
+        p = b.params(H, D, dtype, kept)
+        C.cache_write(p, x.cuda(), x.cuda(), *b.device(), pool)
+        guard.check()
+        mine = np.zeros((b.n_pages, 32), dtype=bool)
+        for at in b.places():
+            if at not in (None, "padding"):
+                mine[at] = True
+        for given, here in zip((k[0], v[0], k[1], v[1]), pool):
+            if given is not None:
+                rest = torch.from_numpy(~mine)[:, None, :].expand(given.shape[:3])
+                assert torch.equal(given[rest].contiguous().view(torch.uint8), here.cpu()[rest].contiguous().view(torch.uint8))
+        outs = [guard(torch.full((b.T, H, D), 7.0, dtype=torch_dtype(dtype))) for _ in range(2)]
+        C.cache_read(p, pool, *b.device(), k_out=outs[0], v_out=outs[1])
+        guard.check()
+        for o in outs:
+            assert bool((o[int(b.start[-1]):] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,kept", [k for k in KINDS if k[0] != k[1]])
+@pytest.mark.parametrize("D,new", [(64, 1), (128, 1), (96, 6), (128, 6), (128, 14), (64, 30), (96, 30), (128, 30)])
+def test_products_with_codes_keep_their_bits(dtype, kept, D, new):
+    """Few positions whose scores are exact (small whole numbers), so that the roundings of p v_scale show: derived in test_round_tolerances."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(D + new)
+    H, heads = 2, 8
+    b = Batch(rng, [new] * 3, [new + 1, new + 34, new + 9], 16)
+    codes = torch.from_numpy(rng.integers(-4, 5, (b.n_pages, H, 16, D)).astype(np.float32))
+    k_scale = torch.full(codes.shape[:3], 2.0 ** -4)
+    v = pool_of(rng.standard_normal(codes.shape) * np.exp(0.5 * rng.standard_normal(codes.shape[:3] + (1,))), kept, dtype)
+    q = rng.integers(-1, 2, (b.T, heads, D)).astype(np.float64)
+    p = C.AttendParams(cache=b.params(H, D, dtype, kept), n_heads=heads, max_len=max(b.length), scale=1.0)
+    pool = (codes.to(torch_dtype(kept)).cuda(), v[0].cuda(), k_scale.cuda(), v[1].cuda())
+    out, _ = C.attend(p, torch.from_numpy(q).to(torch_dtype(dtype)).cuda(), *b.device(), pool)
+    out, k64 = out.float().cpu().numpy().astype(np.float64), codes.double().numpy() * 2.0 ** -4
+    for s in range(3):
+        for i in range(new):
+            t = int(b.start[s]) + i
+            at = np.array([RO.place(j, b.pages[s], 16, b.n_pages) for j in RO.seen_by(i, new, b.length[s])])
+            assert len(at) <= 64
+            for h in range(heads):
+                o, _, A, _ = RO.attend_row(q[t, h], k64[at[:, 0], h // 4, at[:, 1]], v[2][at[:, 0], h // 4, at[:, 1]], 1.0)
+                assert np.all(np.abs(out[t, h] - o) <= TT.allowed(dtype, o, A)), (s, i, h)
