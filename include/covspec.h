@@ -489,8 +489,9 @@ int covspec_cache_read(const covspec_cache_params* p, const void* k_cache, const
  *   lse_out [n_tokens, n_heads] fp32 log sum_j exp(scale * q . k_j), or NULL
  * max_len (HOST) bounds the lengths: it sizes the grid and the workspace; positions at or beyond it are not seen.
  * Products are taken of 16-bit values with fp32 sums (8-bit codes are exact in 16 bits; their scales enter in fp32),
- * softmax statistics are fp32, p (of an fp16 batch over codes: p times the scale, to 16 bits of
- * significand) is rounded to 16 bits for its product with v.  The same call gives the same bits.
+ * softmax statistics are fp32.  p (over codes p times their scale) keeps 16 bits of significand in its product with v
+ * in an fp16 batch over codes, and in a bf16 batch with up to 32 rows for a key head of a sequence (tokens x heads, in the
+ * mean of the batch; 64 over a bf16 cache); else it is rounded to dtype.  The same call gives the same bits.
  * Limits: those of the cache (its row_pitch is not used); n_heads a multiple of n_kv_heads, at most 64 times it;
  * n_tokens * n_heads and n_seq * n_kv_heads below 2^30 (and a grid of less than 2^32 threads); max_len from 1 to max_pages * page_size; window >= 0; scale finite.  Workspace:
  * covspec_attend_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on `stream`,

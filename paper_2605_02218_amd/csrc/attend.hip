@@ -230,7 +230,11 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
   // of 88 rows behind 120001 tokens took 74 us instead of 83).
   constexpr bool CODES = KEPT != DT, WIDE = CODES && RW > 1;
   constexpr int VDT = CODES ? DT_BF16 : DT;              // type of the products with v
-  constexpr bool SPLIT_P = CODES && DT == DT_F16;
+  // In bf16, p (v_scale) goes into its products in two parts as well, 16 bits of significand, wherever that costs 3 % or less: where a wave has tiles of its own,
+  // and in 16-bit caches up to 64 rows.  Error against 64 bits with one part 1.45 times the rounding of the output for 64 single tokens over e4m3, 1.37 for 32
+  // segments, with two 1.00.  us with one and two: 64 single tokens over e4m3 124 and 126, over bf16 behind 8192 positions each 352 to 358 and 358 to 363, segments of 64
+  // rows 392 and 399; but those over e4m3 299 and 344, 88 rows 400 and 468, prompts of 4 x 3008 tokens 750 and 943.  fp16 caches have p's 11 bits.
+  constexpr bool SPLIT_P = CODES ? DT == DT_F16 || RW == 1 : DT == DT_BF16 && RW <= 2;
   typedef Form<DT, WIDE ? DT : KEPT, D> W;               // of the tiles that are multiplied
   constexpr bool RAW = CODES && !WIDE;
   constexpr bool TURNS = RW == 8;                        // see the loop over the tiles
@@ -614,8 +618,16 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float a0 = z[x][2 * e], a1 = z[x][2 * e + 1];
-        prob[x][e] = Half<VDT>::pack(a0, a1);
-        if constexpr (SPLIT_P) rest[x][e] = Half<VDT>::pack(a0 - bf16lo_to_f32(prob[x][e]), a1 - bf16hi_to_f32(prob[x][e]));
+        if constexpr (SPLIT_P && !CODES) {
+          // cut, not rounded, and the second part a little larger: both are above zero, and an infinity in v times them is one
+          constexpr float more = 1.f + 0x1p-20f;
+          const uint32_t f0 = __float_as_uint(a0) & 0xFFFF0000u, f1 = __float_as_uint(a1) & 0xFFFF0000u;
+          prob[x][e] = f0 >> 16 | f1;
+          rest[x][e] = Half<VDT>::pack(__builtin_fmaf(a0, more, -__uint_as_float(f0)), __builtin_fmaf(a1, more, -__uint_as_float(f1)));
+        } else {
+          prob[x][e] = Half<VDT>::pack(a0, a1);
+          if constexpr (SPLIT_P) rest[x][e] = Half<VDT>::pack(a0 - bf16lo_to_f32(prob[x][e]), a1 - bf16hi_to_f32(prob[x][e]));
+        }
       }
   };
   auto multiply_v = [&](int x) {
