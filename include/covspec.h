@@ -482,7 +482,8 @@ int covspec_cache_read(const covspec_cache_params* p, const void* k_cache, const
  *   j <= pos, and j > pos - window if window > 0; or, with `visible`, every position in front of the chunk and
  *   of the chunk itself those rows b whose bit b of visible[row] is set (a tree of drafted tokens, paper Sec. III-C: row
  *   0 is bit 0; rows from the 65th on are then seen by none; a row sees itself only if its own bit says so).
- *   A row that sees nothing gives zeros and the log-sum -infinity.  What unseen positions hold, NaN included, has no effect.
+ *   A row that sees nothing, or only scores of -infinity, gives zeros and the log-sum -infinity.  What unseen positions
+ *   hold, NaN included, has no effect.  (p is kept below 2^8: v of up to 2^100 in magnitude cannot overflow the sums.)
  *   q     [n_tokens, n_heads, head_dim] dtype, rows q_pitch elements apart (0: dense), 16-byte aligned
  *   visible [n_tokens] int64 bits, or NULL (with window == 0 only)
  *   out   [n_tokens, n_heads, head_dim] dtype, rows out_pitch elements apart (0: dense); padding rows stay as they were
@@ -525,7 +526,8 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
  *   4. x = x / T;
  *   5. w not allowed: x = -infinity;
  * with (r, c, f, T) = penalties[s] = repetition, presence, frequency, temperature; (1, 0, 0, 1) changes no bit of a number
- * (zeros keep their sign; a NaN stays one).  A T that is not > 0 counts as 1.  Steps 1 to 4 are one fp32 multiplication
+ * (zeros keep their sign; a NaN stays one).  A T that is not > 0 counts as 1; r and T are not
+ * subnormal (their reciprocals are taken).  Steps 1 to 4 are one fp32 multiplication
  * and addition with a factor and a summand per word, themselves formed in fp32: off by at most eight roundings of 2^-24
  * of the largest magnitude that occurs in them; then one rounding to dtype.
  * DEVICE pointers:
@@ -538,6 +540,8 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
  * A segment that was drafted without the mask may hold a word that is not allowed.  With the mask on the target's logits
  * alone covspec_verify rejects it (p_t = 0) and draws an allowed one; with the mask on both sides it has p_t = p_d = 0 and
  * counts as accepted.  So mask the draft's logits too only if the words were drawn from logits with the same mask.
+ * A position at which nothing is allowed has no distribution: do not verify it (n_accept and correction stay in their
+ * ranges, but mean nothing from there on).
  * Words outside [0, vocab) are nobody's.  Limits as covspec_verify, with n_pos in the place of n_draft: n_pos <= 64,
  * n_seq * n_pos <= 65535, vocab a multiple of 8 (bf16, fp16) or 4 (fp32) and below 2^30.  No workspace; one launch on
  * `stream`, does not synchronise, allocates nothing.

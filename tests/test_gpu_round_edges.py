@@ -381,3 +381,33 @@ def test_products_with_v_keep_their_bits(dtype, kept, D, new):
             for h in range(heads):
                 o, _, A, _ = RO.attend_row(q[t, h], k64[at[:, 0], h // 4, at[:, 1]], v[2][at[:, 0], h // 4, at[:, 1]], 1.0)
                 assert np.all(np.abs(out[t, h] - o) <= TT.allowed(dtype, o, A, TT.parts(dtype, kept, new * heads // H))), (s, i, h)
+
+
+@pytest.mark.parametrize("dtype,kept", [k for k in KINDS if k[0] != k[1]])
+def test_rows_over_the_whole_range_of_their_type(dtype, kept):
+    """A row's largest magnitude from the smallest number of the type to its largest, the border of 2^-100 among them: codes and scales to the bit, and what
+    is read back."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(24)
+    D, top = 64, {"bf16": range(-133, 128), "fp16": range(-24, 16)}[dtype]
+    b = Batch(rng, [len(top)], [len(top) + 7], 64)
+    x = np.stack([rng.uniform(-1, 1, (1, D)) for _ in top]) * 2.0 ** (np.array(top, dtype=float)[:, None, None] + 1)
+    x[:, 0, 3] = (2.0 - 2.0 ** -7) * 2.0 ** np.array(top, dtype=float)             # below 2^(k + 1) in both types
+    x[::5, 0, 3] = 2.0 ** np.array(top, dtype=float)[::5]
+    x[::5, 0] = np.clip(x[::5, 0], -x[::5, :1, 3], x[::5, :1, 3])
+    x = np.clip(x, -np.abs(x[:, :, 3:4]), np.abs(x[:, :, 3:4]))
+    t, v32 = rounded(x, dtype)
+    assert np.isfinite(v32).all()
+    p = b.params(1, D, dtype, kept)
+    pool, batch = C.cache_alloc(p), b.device()
+    C.cache_write(p, t.cuda(), t.cuda(), *batch, pool)
+    k, v = C.cache_read(p, pool, *batch)
+    torch.cuda.synchronize()
+    at = np.array(b.places())
+    codes, scale = RO.quantise(v32, kept)
+    for i, back in ((0, k), (1, v)):
+        np.testing.assert_array_equal(pool[i].cpu().float().numpy()[at[:, 0], 0, at[:, 1]], codes[:, 0])
+        np.testing.assert_array_equal(pool[2 + i].cpu().numpy()[at[:, 0], 0, at[:, 1]], scale[:, 0])
+        want = torch.from_numpy(codes * scale[..., None]).to(t.dtype)
+        np.testing.assert_array_equal(back.cpu().float().numpy(), want.float().numpy())
