@@ -526,10 +526,10 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
  *   4. x = x / T;
  *   5. w not allowed: x = -infinity;
  * with (r, c, f, T) = penalties[s] = repetition, presence, frequency, temperature; (1, 0, 0, 1) changes no bit of a number
- * (zeros keep their sign; a NaN stays one).  A T that is not > 0 counts as 1; r and T are not
- * subnormal (their reciprocals are taken).  Steps 1 to 4 are one fp32 multiplication
- * and addition with a factor and a summand per word, themselves formed in fp32: off by at most eight roundings of 2^-24
- * of the largest magnitude that occurs in them; then one rounding to dtype.
+ * (zeros keep their sign; a NaN stays one).  A T that is not > 0 counts as 1; r and T are not subnormal (their
+ * reciprocals are taken).  Steps 1 to 4 are one fp32 multiplication and addition with a factor and a summand per word,
+ * themselves formed in fp32: off by at most eight roundings of 2^-24 of the largest magnitude that occurs in them; then
+ * one rounding to dtype.
  * DEVICE pointers:
  *   z, z_out  [n_seq, n_pos, vocab] dtype, 16-byte aligned; z_out may be z (not overlap it otherwise)
  *   history   packed words, int32; history_start [n_seq + 1] int32 ascending; prompt_len [n_seq] int32 or NULL (0)

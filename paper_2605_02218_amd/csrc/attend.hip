@@ -644,7 +644,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void attend_kernel(Paged c, Attend
   //     registers of the operand, and added afterwards to the rows that see them (infinity times any p > 0 is infinity, NaN is NaN).
   //   AGAIN, waves that share tiles and that the test costs more: a workgroup whose sums have come out NaN goes over its tiles again, without the products
   //     with v of those that are not seen whole, and adds these term by term.  us, without either / with the test in the operands or while a tile is
-  //     widened / so: prompts of 4 x 3008 tokens 731, 782, 751; 88 rows behind 8192 positions 384, 396, 386; 2048 tokens behind 14336 of an e4m3 cache
+  //     widened / so: prompts of 4 x 3008 tokens 731, 782, 745; 88 rows behind 8192 positions 384, 396, 386; 2048 tokens behind 14336 of an e4m3 cache
   //     1459, 1527, 1468.
   constexpr uint32_t TOP = CODES ? 0x7F7F7F7Fu : VDT == DT_BF16 ? 0x7F807F80u : 0x7C007C00u, ONE = CODES ? 0x01010101u : VDT == DT_BF16 ? 0x00800080u : 0x04000400u;
   constexpr uint32_t SIGN = CODES ? 0x80808080u : 0x80008000u;
@@ -1026,8 +1026,10 @@ __global__ __launch_bounds__(JT) void attend_join_kernel(Attend a, int T, int G,
 // Tiles of 16 rows up to 16, of 32 (64, 128) up to 32 (64, any more); us for 64 x 8192 positions of a 16-bit cache, 8 key heads: 4 rows for each in
 // 16-row tiles 352, in 32-row tiles 372; 64 rows 357, 88 rows 397, all near the 370 that the bytes take at 5.8 TB/s.
 // 256 rows whose waves take turns (16-bit caches) from 512 on, where the workgroups, one on a compute unit, are shares or many: 512 tokens behind 32256
-// 587 instead of 658 with 128 rows, 1024 behind 15360 565 instead of 626, prompts of 4 x 3008 741 instead of 752; but 376 items, one prompt of
-// 3000, 113 instead of 107.
+// 587 instead of 658 with 128 rows, 1024 behind 15360 565 instead of 626, prompts of 6000 (1500 items) 668 and 686, of 4096 (1024) 329 and 334.  Between 257 and
+// 1023 items, of the larger size, it goes by how the last round of 256 is filled, which lengths decide that the host does not know: prompts of 272 items 53 and 46,
+// 376 113 and 107, 512 100 and 106, 640 160 and 151, 768 202 and 197 (1090 and 1167 with 9000 positions in front), 896 262 and 263; 128 rows there.
+// The rows are the mean over the sequences, padding and empty ones included: one long chunk among single tokens gives each token a tile of its size.
 // Shares where a workgroup per item would leave half of the device idle: 256 tokens behind 32512 (128 items of 128 rows) 361 instead of 909, single tokens
 // of 8 sequences 40 instead of 70, 8 drafted tokens of 4 sequences 37 instead of 128, a tree behind 120001 positions 84 instead of 5450; 32 segments
 // behind 900 to 6100 (256 items) 119.5 and 121.5.  With more items there is nothing to gain, as those that still run have the memory to themselves: 64
