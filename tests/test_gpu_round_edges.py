@@ -411,3 +411,28 @@ def test_rows_over_the_whole_range_of_their_type(dtype, kept):
         np.testing.assert_array_equal(pool[2 + i].cpu().numpy()[at[:, 0], 0, at[:, 1]], scale[:, 0])
         want = torch.from_numpy(codes * scale[..., None]).to(t.dtype)
         np.testing.assert_array_equal(back.cpu().float().numpy(), want.float().numpy())
+
+
+@pytest.mark.parametrize("dtype,kept,new,heads", [("bf16", "bf16", 3, 2), ("bf16", "e4m3", 8, 4), ("bf16", "bf16", 12, 8), ("fp16", "e4m3", 12, 8), ("fp16", "fp16", 25, 8),
+                                                  ("bf16", "e4m3", 25, 8), ("bf16", "int8", 25, 8)])
+def test_many_sequences_whose_last_token_is_not_finite(dtype, kept, new, heads):
+    """A workgroup for each item: every other sequence has NaN in its last row's v, which that row alone sees."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(25)
+    S, H, D = 300, 1, 64
+    b = Batch(rng, [new] * S, [new + int(x) for x in rng.integers(0, 150, S)], 16)
+    k, v, q, q64 = TA.setup(rng, b, heads, H, D, dtype, kept)
+    pool = TA.upload(k, v)
+    last = [int(b.start[s + 1]) - 1 for s in range(0, S, 2)]
+    for s in range(0, S, 2):
+        page, at = RO.place(b.length[s] - 1, b.pages[s], 16, b.n_pages)
+        (pool[1] if kept == dtype else pool[3])[page, :, at] = float("nan")
+    p = C.AttendParams(cache=b.params(H, D, dtype, kept), n_heads=heads, max_len=max(b.length), scale=D ** -0.5)
+    out, lse = C.attend(p, q.cuda(), *b.device(), pool, want_lse=True)
+    torch.cuda.synchronize()
+    spoilt = torch.zeros(b.T, dtype=torch.bool)
+    spoilt[last] = True
+    assert bool(torch.isnan(out[spoilt.cuda()]).all()) and not bool(torch.isnan(out[~spoilt.cuda()]).any()) and not bool(torch.isnan(lse).any())
+    rows = (set(range(0, b.T, 53)) | {t - 1 for t in last[::9]}) - set(last)
+    TA.check(b, heads, H, D, dtype, kept, k[2], v[2], q64, out, lse, D ** -0.5, rows=rows)
