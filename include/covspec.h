@@ -558,6 +558,150 @@ int covspec_adjust_logits(const covspec_logits_params* p, const void* z, const i
                           const float* penalties, const int32_t* bias_start, const int32_t* bias_word,
                           const float* bias_value, const uint32_t* allowed, void* z_out, covspec_stream_t stream);
 
+/*
+ * Page tables on the device: which pages every sequence holds, from the lengths they are to have.  NOT in the paper; the paged calls above take `start`,
+ * `length` and `pages`, and the lengths of the next round follow from n_accept of covspec_verify, which is on the device.
+ *
+ * covspec_pages_step moves all sequences to their next lengths.  State (DEVICE, int32, read and written):
+ *   pages [n_seq, max_pages]; held [n_seq] pages that a sequence has; borrowed [n_seq] of which the first so many belong to somebody else (a shared
+ *   prefix) and are never given back; free_pages [n_pages] a stack, of which the first n_free[0] entries are free pages
+ * For each sequence want[s] tokens, of which the last rows[s] are the rows of the next call (DEVICE, int32; below zero counts as zero, rows beyond
+ * want as want); want = 0 ends a sequence.  With need = ceil(want / page_size):
+ *   1. a sequence with held > need gives back its pages from max(need, borrowed) on and holds need.  The stack takes them, the last page of the last
+ *      sequence first, so that growing and shrinking by the same pages leaves it as it was.  What falls off its end (more pages than n_pages) is lost.
+ *   2. sequences with held < need get all the pages they lack or none, from the top of the stack, in their order, none overtaking another: once one
+ *      goes empty-handed all later ones that ask do.  A sequence that asks for more than max_pages gets nothing and stops nobody.
+ *   3. borrowed = min(borrowed, held).  Entries of `pages` at and beyond held are unspecified but for those that were not touched.
+ *   4. outcome [n_seq]: 0 as wanted; 1 no pages: it holds what it held; 2 pages, but its rows and those in front of it are more than n_tokens (once one
+ *      is left out all later ones with rows are).  1 and 2: no rows, and a length of want - rows, or of all it holds if that is less.
+ *   5. start [n_seq + 1] and length [n_seq] as the calls above take them; for every row, padding included, slots [n_tokens] int64, its place
+ *      page * page_size + position % page_size, and positions [n_tokens]: -1 for padding rows, the slot also where the page is none of the pool's.
+ *      slots and positions may be NULL.
+ * held, borrowed and n_free outside their ranges count as the nearest value inside; nothing outside the arrays is touched whatever they hold.
+ * Limits: n_seq <= 65536, n_seq * max_pages and n_tokens below 2^30, page_size as above: else COVSPEC_UNSUPPORTED.  n_tokens may be 0 (then
+ * without slots and positions).  Workspace: covspec_pages_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on
+ * `stream`, does not synchronise, allocates nothing; the launches depend on the parameters alone.
+ */
+typedef struct covspec_pages_params {
+  int32_t n_seq;        /* S                                                     */
+  int32_t n_tokens;     /* T: rows that a call has room for                      */
+  int32_t page_size;    /* tokens per page: a power of two from 16 to 1024       */
+  int32_t n_pages;      /* pages of the pool                                     */
+  int32_t max_pages;    /* width of the page table                               */
+} covspec_pages_params;
+
+size_t covspec_pages_workspace_size(const covspec_pages_params* p);
+int covspec_pages_step(const covspec_pages_params* p, const int32_t* want, const int32_t* rows, int32_t* pages, int32_t* held,
+                       int32_t* borrowed, int32_t* free_pages, int32_t* n_free, int32_t* start, int32_t* length, int32_t* outcome,
+                       int64_t* slots, int32_t* positions, void* workspace, size_t workspace_bytes, covspec_stream_t stream);
+
+/*
+ * Rotary positions.  NOT in the paper, whose models have them.  The first rotary_dim elements of a head are pairs, (i, i + rotary_dim / 2), or with
+ * `interleaved` (2i, 2i + 1); pair i of a row at position pos is turned by pos * f_i:
+ *   y1 = magnitude (x1 cos - x2 sin),  y2 = magnitude (x2 cos + x1 sin);  the other elements stay as they are.
+ * f_i is given as steps[i], the part of a turn from one position to the next as a 64-bit binary fraction, so that pos * steps[i] mod 2^64 is the angle
+ * of any position without a rounding.  Cosine and sine are off by at most 2^-22, products and sums are fp32, then one rounding to dtype.
+ * Negative positions turn the other way: with positions negated the call undoes a rotation, and is its gradient.
+ *
+ * covspec_rotary_steps (HOST) writes steps[rotary_dim / 2] from f_i = base^(-2i / rotary_dim) and a way to scale it for longer contexts:
+ *   LINEAR  f / factor
+ *   BASE    base * factor^(rotary_dim / (rotary_dim - 2)) in the place of base
+ *   BANDS   f (keep + (1 - keep) / factor), keep = (turns - low) / (high - low) within [0, 1], turns = original_len f / 2 pi
+ *   RAMP    the same with keep = 1 - (i - a) / (b - a) within [0, 1]: a = floor of the index at which `high` turns are made over original_len, at least 0,
+ *           b = ceiling of that for `low`, at most rotary_dim - 1 (b - a at least 0.001)
+ *   PLAIN   f.  Fields that a kind does not use are not looked at.
+ */
+enum { COVSPEC_ROTARY_PLAIN = 0, COVSPEC_ROTARY_LINEAR = 1, COVSPEC_ROTARY_BASE = 2, COVSPEC_ROTARY_BANDS = 3, COVSPEC_ROTARY_RAMP = 4 };
+
+typedef struct covspec_rotary_scaling {
+  int32_t kind;          /* COVSPEC_ROTARY_*                                      */
+  int32_t original_len;  /* BANDS, RAMP: >= 1                                     */
+  double base;           /* > 0; RAMP: > 1                                        */
+  double factor;         /* > 0                                                   */
+  double low, high;      /* BANDS: low < high; RAMP: 0 < low < high               */
+} covspec_rotary_scaling;
+
+int covspec_rotary_steps(const covspec_rotary_scaling* s, int32_t rotary_dim, uint64_t* steps_out);
+
+/*
+ * covspec_rotate: rows of q and k (either may be NULL, with its output) to q_out and k_out, which may be the inputs (not overlap them otherwise).
+ * covspec_rotate_write: the same for q, while k, rotated, and v go straight into the paged cache (covspec_cache_write): with cache_dtype == dtype what
+ * covspec_rotate and then covspec_cache_write leave, to the bit; 8-bit codes are made of the rotated values in fp32, without a rounding to dtype between.
+ *   q, q_out [n_tokens, n_heads, head_dim], k, k_out, v [n_tokens, n_kv_heads, head_dim] dtype (COVSPEC_BF16, COVSPEC_FP16), rows q_pitch, q_out_pitch,
+ *   k_pitch (k and v) and k_out_pitch elements apart (0: dense), 16-byte aligned
+ *   steps     [rotary_dim / 2] 64-bit, DEVICE
+ *   positions [n_axes, n_tokens] int32, or NULL: a row's position in its sequence, by start and length, for every axis
+ *   axis      [rotary_dim / 2] int32, which of the positions turns a pair; a value outside counts as the nearest axis; NULL: the first, for all
+ *   start, length: the batch, as above; padding rows are left as they were.  covspec_rotate with positions may have both NULL: all rows are rotated.
+ * Limits: head_dim 64, 96 or 128; rotary_dim a multiple of 16 up to head_dim; n_axes from 1 to 4; n_tokens * (n_heads + n_kv_heads) below 2^30, n_seq
+ * below 2^30; pitches multiples of 8, not below a row; for covspec_rotate_write those of the cache as well (its row_pitch is not used), whose n_seq,
+ * n_tokens, n_kv_heads, head_dim and dtype have to be the same.  No workspace; one launch on `stream`, does not synchronise, allocates nothing.
+ */
+typedef struct covspec_rotary_params {
+  int32_t n_seq;        /* S                                                     */
+  int32_t n_tokens;     /* T: rows, padding included                             */
+  int32_t n_heads;      /* of q                                                  */
+  int32_t n_kv_heads;   /* of k and v                                            */
+  int32_t head_dim;     /* D                                                     */
+  int32_t rotary_dim;   /* R                                                     */
+  int32_t interleaved;  /* 0: pairs (i, i + R / 2); 1: (2i, 2i + 1)              */
+  int32_t n_axes;
+  int32_t dtype;
+  float magnitude;      /* finite; 1 unless a scaling asks for another           */
+  int64_t q_pitch, k_pitch, q_out_pitch, k_out_pitch;
+} covspec_rotary_params;
+
+int covspec_rotate(const covspec_rotary_params* p, const void* q, const void* k, const uint64_t* steps, const int32_t* positions,
+                   const int32_t* axis, const int32_t* start, const int32_t* length, void* q_out, void* k_out, covspec_stream_t stream);
+int covspec_rotate_write(const covspec_rotary_params* p, const covspec_cache_params* c, const void* q, const void* k, const void* v,
+                         const uint64_t* steps, const int32_t* positions, const int32_t* axis, const int32_t* start, const int32_t* length,
+                         const int32_t* pages, void* q_out, void* k_cache, void* v_cache, float* k_scale, float* v_scale, covspec_stream_t stream);
+
+/*
+ * Attention over the pages that a cheap score selects for each row, for contexts so long that reading the whole cache bounds the call.  NOT in the paper.
+ * A block is a page of a sequence: block b holds the positions b * page_size .. (b + 1) * page_size - 1.
+ *
+ * covspec_block_summary: summaries of the pages that hold rows of the batch, over the positions of each that are below length[s]; called behind
+ * covspec_cache_write (covspec_rotate_write), whose rejected tokens are gone from a summary as soon as the next rows overwrite them.
+ *   summary [n_pages, n_kv_heads, 2, head_dim] int8, summary_scale [n_pages, n_kv_heads] fp32 (DEVICE, the caller's, beside the pool)
+ *   channel by channel the largest, then the smallest key of the page (8-bit caches: code * scale in fp32), as codes: with amax = the largest magnitude
+ *   of all of them, scale = amax / 127, code = x * ((1 / amax) * 127) to the nearest, ties to even, each operation rounded to fp32 on its own.
+ *   amax < 2^-100: codes and scale zero; a key that is not finite: codes zero, scale NaN.  16-byte aligned; 2^40 bytes at most.  Two sequences of a
+ *   call that share a page of which they see different positions leave one's summary or the other's, so share whole pages.
+ *
+ * covspec_sparse_attend: for row t and key head g, q_h the group's queries, quantised each like a row of an INT8 cache (codes c_h, scale s_h):
+ *   score of block b = max over h of (sum_d max(c_hd largest_d, c_hd smallest_d)) * summary_scale * s_h, the sum of integers exact, then two fp32
+ *   products in this order; it bounds what q_h . k can be in the block but for the roundings of the codes.  (For attend.scale > 0, as it should be.)
+ *   Of the blocks 0 .. nb - 1 that begin below the end of what the row sees (position + 1; with `visible` that of its chunk's first 64 rows) it takes the
+ *   first `first`, the last `recent`, and of the others those with the largest scores, `top` in all: a NaN counts as the largest, ties go to the
+ *   lower block, one on a page that does not exist is not taken.
+ *   blocks [n_tokens, n_kv_heads, top] int32 the blocks taken, ascending, then -1; with given != 0 they are the caller's instead (those of another
+ *   layer, say) and summary, summary_scale are not read: any order, entries that are no block of the sequence take no part, a block that is
+ *   listed twice counts twice.  Written for the rows of the batch; padding rows stay as they were.
+ *   out, lse_out: covspec_attend over the positions of these blocks that the row sees (visible, padding, rows that see nothing, positions that do not exist
+ *   as there); probabilities keep 16 bits of significand in their product with v in every form but fp16 over an fp16 cache, 11 there.
+ * Limits: those of covspec_attend, with window == 0; top from 1 to 1024, first, recent >= 0, first + recent <= top; at most 32768 blocks, as
+ * ceil(max_len / page_size) counts them; n_tokens * n_kv_heads * 32768 below 2^40: else COVSPEC_INVALID_ARG (top, first, recent, window) or COVSPEC_UNSUPPORTED.  Workspace:
+ * covspec_sparse_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on `stream`, does not synchronise, allocates
+ * nothing; the launches depend on the parameters alone.  The same call gives the same bits.
+ */
+int covspec_block_summary(const covspec_cache_params* p, const int32_t* start, const int32_t* length, const int32_t* pages, const void* k_cache,
+                          const float* k_scale, void* summary, float* summary_scale, covspec_stream_t stream);
+
+typedef struct covspec_sparse_params {
+  covspec_attend_params attend;
+  int32_t top;          /* blocks of a row and key head                          */
+  int32_t first;        /* of them the first ones of the sequence                */
+  int32_t recent;       /* and the last ones that the row sees                   */
+  int32_t given;        /* != 0: `blocks` is read                                */
+} covspec_sparse_params;
+
+size_t covspec_sparse_workspace_size(const covspec_sparse_params* p);
+int covspec_sparse_attend(const covspec_sparse_params* p, const void* q, const int32_t* start, const int32_t* length, const int32_t* pages,
+                          const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, const void* summary,
+                          const float* summary_scale, const int64_t* visible, int32_t* blocks, void* out, float* lse_out, void* workspace,
+                          size_t workspace_bytes, covspec_stream_t stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* covspec_status_string(int status);
 

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcovspec.so")
@@ -20,6 +20,7 @@ FP16 = 2          # logits, cached tokens and their attention
 INT8, E4M3 = 3, 4  # what a cache holds only
 REL_COSINE_MAX, REL_ATTN_SOFTMAX = 0, 1
 LR_ENERGY_TOPK, LR_GREEDY_RESIDUAL, LR_SCORE_TOPK, LR_RANDOM = 0, 1, 2, 3
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = 0, 1, 2, 3, 4
 OK, INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED, HIP_ERROR = 0, 1, 2, 3, 4
 
 EXPORTS = ("covspec_workspace_size", "covspec_resolve", "covspec_score", "covspec_select",
@@ -27,7 +28,9 @@ EXPORTS = ("covspec_workspace_size", "covspec_resolve", "covspec_score", "covspe
            "covspec_verify_workspace_size", "covspec_verify", "covspec_verify_static", "covspec_draft_fanout", "covspec_draft_workspace_size",
            "covspec_draft_gate", "covspec_last_error", "covspec_ragged_resolve", "covspec_ragged_workspace_size",
            "covspec_reduce_ragged", "covspec_lowrank_path", "covspec_image_status", "covspec_set_wait_limit_us", "covspec_stream_workspace_size", "covspec_stream_step",
-           "covspec_cache_write", "covspec_cache_read", "covspec_attend_workspace_size", "covspec_attend", "covspec_adjust_logits")
+           "covspec_cache_write", "covspec_cache_read", "covspec_attend_workspace_size", "covspec_attend", "covspec_adjust_logits",
+           "covspec_pages_workspace_size", "covspec_pages_step", "covspec_rotary_steps", "covspec_rotate", "covspec_rotate_write", "covspec_block_summary",
+           "covspec_sparse_workspace_size", "covspec_sparse_attend")
 
 
 class CovspecParams(ctypes.Structure):
@@ -67,6 +70,23 @@ class CovspecAttendParams(ctypes.Structure):
 
 class CovspecLogitsParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "n_pos", "vocab", "dtype")]
+
+
+class CovspecPagesParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "n_tokens", "page_size", "n_pages", "max_pages")]
+
+
+class CovspecRotaryScaling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("kind", "original_len")] + [(n, ctypes.c_double) for n in ("base", "factor", "low", "high")]
+
+
+class CovspecRotaryParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "n_tokens", "n_heads", "n_kv_heads", "head_dim", "rotary_dim", "interleaved", "n_axes", "dtype")] + [
+        ("magnitude", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("q_pitch", "k_pitch", "q_out_pitch", "k_out_pitch")]
+
+
+class CovspecSparseParams(ctypes.Structure):
+    _fields_ = [("attend", CovspecAttendParams)] + [(n, ctypes.c_int32) for n in ("top", "first", "recent", "given")]
 
 
 class CovspecError(RuntimeError):
@@ -153,6 +173,23 @@ def load_library() -> ctypes.CDLL:
     lib.covspec_attend.argtypes = [app] + [vp] * 12 + [ctypes.c_size_t, vp]
     lib.covspec_adjust_logits.restype = ctypes.c_int
     lib.covspec_adjust_logits.argtypes = [lpp] + [vp] * 12
+    gpp, scp, rpp, bpp = (ctypes.POINTER(t) for t in (CovspecPagesParams, CovspecRotaryScaling, CovspecRotaryParams, CovspecSparseParams))
+    lib.covspec_pages_workspace_size.restype = ctypes.c_size_t
+    lib.covspec_pages_workspace_size.argtypes = [gpp]
+    lib.covspec_pages_step.restype = ctypes.c_int
+    lib.covspec_pages_step.argtypes = [gpp] + [vp] * 13 + [ctypes.c_size_t, vp]
+    lib.covspec_rotary_steps.restype = ctypes.c_int
+    lib.covspec_rotary_steps.argtypes = [scp, ctypes.c_int32, ctypes.POINTER(ctypes.c_uint64)]
+    lib.covspec_rotate.restype = ctypes.c_int
+    lib.covspec_rotate.argtypes = [rpp] + [vp] * 10
+    lib.covspec_rotate_write.restype = ctypes.c_int
+    lib.covspec_rotate_write.argtypes = [rpp, cpp] + [vp] * 15
+    lib.covspec_block_summary.restype = ctypes.c_int
+    lib.covspec_block_summary.argtypes = [cpp] + [vp] * 8
+    lib.covspec_sparse_workspace_size.restype = ctypes.c_size_t
+    lib.covspec_sparse_workspace_size.argtypes = [bpp]
+    lib.covspec_sparse_attend.restype = ctypes.c_int
+    lib.covspec_sparse_attend.argtypes = [bpp] + [vp] * 15 + [ctypes.c_size_t, vp]
     lib.covspec_last_error.restype = ctypes.c_char_p
     lib.covspec_last_error.argtypes = []
     _lib = lib
@@ -787,3 +824,219 @@ def adjust_logits(p: LogitsParams, z, history, history_start, penalties, prompt_
     if st != OK:
         raise CovspecError(st, "covspec_adjust_logits")
     return out
+
+
+# ---------------------------------------------------------------- page tables, rotary positions, attention over selected pages
+@dataclass
+class PagesParams:
+    n_seq: int
+    n_tokens: int
+    page_size: int
+    n_pages: int
+    max_pages: int
+
+    def c_struct(self) -> CovspecPagesParams:
+        return CovspecPagesParams(self.n_seq, self.n_tokens, self.page_size, self.n_pages, self.max_pages)
+
+
+class PagesStep(NamedTuple):
+    """What covspec_pages_step returns: start [S + 1], length [S], outcome [S] int32, slots [T] int64, positions [T] int32."""
+    start: object
+    length: object
+    outcome: object
+    slots: object
+    positions: object
+
+
+def pages_workspace_size(p: PagesParams) -> int:
+    cs = p.c_struct()
+    return int(load_library().covspec_pages_workspace_size(ctypes.byref(cs)))
+
+
+def pages_alloc(p: PagesParams, device="cuda"):
+    """The state when nobody holds anything: (pages [S, max_pages], held [S], borrowed [S], free_pages [n_pages], n_free [1]), int32; page 0 goes out first."""
+    import torch
+    i32 = torch.int32
+    return (torch.zeros(p.n_seq, p.max_pages, dtype=i32, device=device), torch.zeros(p.n_seq, dtype=i32, device=device), torch.zeros(p.n_seq, dtype=i32, device=device),
+            torch.arange(p.n_pages - 1, -1, -1, dtype=i32, device=device), torch.full((1,), p.n_pages, dtype=i32, device=device))
+
+
+def pages_step(p: PagesParams, state, want, rows, workspace=None, want_slots=True) -> PagesStep:
+    """covspec_pages_step on `state` (of pages_alloc), which it changes; slots and positions are None without `want_slots`."""
+    import torch
+    pages, held, borrowed, free, n_free = state
+    dev = _same_device(want, rows, workspace, *state)
+    i32, S, T = torch.int32, p.n_seq, p.n_tokens
+    args = [_expect(want, "want", (S,), i32), _expect(rows, "rows", (S,), i32), _expect(pages, "pages", (S, p.max_pages), i32), _expect(held, "held", (S,), i32),
+            _expect(borrowed, "borrowed", (S,), i32), _expect(free, "free_pages", (p.n_pages,), i32), _expect(n_free, "n_free", (1,), i32)]
+    if workspace is None:
+        n = pages_workspace_size(p)
+        if n == 0:
+            raise CovspecError(INVALID_ARG, "covspec_pages_workspace_size")
+        workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
+    slots = want_slots and T > 0
+    r = PagesStep(torch.empty(S + 1, dtype=i32, device=dev), torch.empty(S, dtype=i32, device=dev), torch.empty(S, dtype=i32, device=dev),
+                  torch.empty(T, dtype=torch.int64, device=dev) if slots else None, torch.empty(T, dtype=i32, device=dev) if slots else None)
+    wp, wb = _ws_args(workspace)
+    cs = p.c_struct()
+    st = _call_on(dev, load_library().covspec_pages_step, ctypes.byref(cs), *args, *[_ptr(t) for t in r], wp, wb)
+    if st != OK:
+        raise CovspecError(st, "covspec_pages_step")
+    return r
+
+
+def rotary_steps(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, original: int = 0, low: float = 0.0, high: float = 0.0,
+                 device="cuda"):
+    """covspec_rotary_steps: the parts of a turn from one position to the next, as 64-bit patterns in an int64 tensor [rotary_dim / 2]."""
+    import torch
+    n = max(rotary_dim // 2, 1)
+    out = (ctypes.c_uint64 * n)()
+    cs = CovspecRotaryScaling(scaling, original, base, factor, low, high)
+    st = load_library().covspec_rotary_steps(ctypes.byref(cs), rotary_dim, out)
+    if st != OK:
+        raise CovspecError(st, "covspec_rotary_steps")
+    return torch.tensor([v - (1 << 64) if v >> 63 else v for v in out], dtype=torch.int64, device=device)
+
+
+@dataclass
+class RotaryParams:
+    n_seq: int
+    n_tokens: int
+    n_heads: int
+    n_kv_heads: int
+    head_dim: int
+    rotary_dim: int = 0          # 0: the whole head
+    interleaved: bool = False
+    n_axes: int = 1
+    dtype: int = BF16
+    magnitude: float = 1.0
+
+    def c_struct(self, q_pitch: int = 0, k_pitch: int = 0, q_out_pitch: int = 0, k_out_pitch: int = 0) -> CovspecRotaryParams:
+        return CovspecRotaryParams(self.n_seq, self.n_tokens, self.n_heads, self.n_kv_heads, self.head_dim, self.rotary_dim or self.head_dim, int(self.interleaved),
+                                   self.n_axes, self.dtype, self.magnitude, q_pitch, k_pitch, q_out_pitch, k_out_pitch)
+
+
+def _rotary_ptrs(p: RotaryParams, steps, positions, axis, start, length):
+    types = _types()
+    i32, half = types["i32"], (p.rotary_dim or p.head_dim) // 2
+    return [_expect(steps, "steps", (half,), types["i64"]), _expect(positions, "positions", (p.n_axes, p.n_tokens), i32), _expect(axis, "axis", (half,), i32),
+            _expect(start, "start", (p.n_seq + 1,), i32), _expect(length, "length", (p.n_seq,), i32)]
+
+
+def rotate(p: RotaryParams, q, k, steps, start=None, length=None, positions=None, axis=None, q_out=None, k_out=None):
+    """covspec_rotate: (q, k) turned, in q_out and k_out (which may be q and k) or new tensors; q or k may be None.  Padding rows of outputs allocated here
+    are unspecified."""
+    import torch
+    dev = _same_device(q, k, steps, start, length, positions, axis, q_out, k_out)
+    dt = _types()[p.dtype]
+    got, pitch = [], {}
+    for name, x, out, heads in (("q", q, q_out, p.n_heads), ("k", k, k_out, p.n_kv_heads)):
+        if x is None:
+            if out is not None:
+                raise ValueError("%s_out without %s" % (name, name))
+            got += [None, None, None]
+            continue
+        out = torch.empty(p.n_tokens, heads, p.head_dim, dtype=dt, device=dev) if out is None else out
+        xp, pitch[name + "_pitch"] = _rows(x, name, p.n_tokens, heads, p.head_dim, dt)
+        op, pitch[name + "_out_pitch"] = _rows(out, name + "_out", p.n_tokens, heads, p.head_dim, dt)
+        got += [xp, op, out]
+    cs = p.c_struct(**pitch)
+    st = _call_on(dev, load_library().covspec_rotate, ctypes.byref(cs), got[0], got[3], *_rotary_ptrs(p, steps, positions, axis, start, length), got[1], got[4])
+    if st != OK:
+        raise CovspecError(st, "covspec_rotate")
+    return got[2], got[5]
+
+
+def rotate_write(p: RotaryParams, c: CacheParams, q, k, v, steps, start, length, pages, cache, positions=None, axis=None, q_out=None):
+    """covspec_rotate_write: q turned, in q_out (which may be q) or a new tensor; k, turned, and v into `cache` (of cache_alloc)."""
+    import torch
+    dev = _same_device(q, k, v, steps, start, length, pages, positions, axis, q_out, *cache)
+    dt = _types()[p.dtype]
+    qp, q_pitch = _rows(q, "q", p.n_tokens, p.n_heads, p.head_dim, dt)
+    q_out = torch.empty(p.n_tokens, p.n_heads, p.head_dim, dtype=dt, device=dev) if q_out is None else q_out
+    op, q_out_pitch = _rows(q_out, "q_out", p.n_tokens, p.n_heads, p.head_dim, dt)
+    kp, pitch = _rows(k, "k", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
+    vp, pitch_v = _rows(v, "v", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
+    if pitch != pitch_v:
+        raise ValueError("k and v must have the same distance between rows")
+    batch, pool = _cache_ptrs(c, start, length, pages, cache)
+    cs, cc = p.c_struct(q_pitch, pitch, q_out_pitch), c.c_struct()
+    st = _call_on(dev, load_library().covspec_rotate_write, ctypes.byref(cs), ctypes.byref(cc), qp, kp, vp, *_rotary_ptrs(p, steps, positions, axis, start, length),
+                  batch[2], op, *pool)
+    if st != OK:
+        raise CovspecError(st, "covspec_rotate_write")
+    return q_out
+
+
+def block_alloc(p: CacheParams, device="cuda"):
+    """Summaries of a pool's pages, of nothing yet: (codes [n_pages, n_kv_heads, 2, head_dim] int8, scale [n_pages, n_kv_heads] fp32)."""
+    import torch
+    return (torch.zeros(p.n_pages, p.n_kv_heads, 2, p.head_dim, dtype=torch.int8, device=device),
+            torch.zeros(p.n_pages, p.n_kv_heads, dtype=torch.float32, device=device))
+
+
+def _summary_ptrs(p: CacheParams, summary):
+    types = _types()
+    return [_expect(summary[0], "summary", (p.n_pages, p.n_kv_heads, 2, p.head_dim), types[INT8]), _expect(summary[1], "summary scales", (p.n_pages, p.n_kv_heads), types["f32"])]
+
+
+def block_summary(p: CacheParams, start, length, pages, cache, summary):
+    """covspec_block_summary: the pages that hold rows of the batch, summarised in `summary` (of block_alloc)."""
+    dev = _same_device(start, length, pages, *cache, *summary)
+    batch, pool = _cache_ptrs(p, start, length, pages, cache)
+    cs = p.c_struct()
+    st = _call_on(dev, load_library().covspec_block_summary, ctypes.byref(cs), *batch, pool[0], pool[2], *_summary_ptrs(p, summary))
+    if st != OK:
+        raise CovspecError(st, "covspec_block_summary")
+    return summary
+
+
+@dataclass
+class SparseParams:
+    attend: AttendParams
+    top: int
+    first: int = 1
+    recent: int = 1
+
+    def c_struct(self, q_pitch: int = 0, out_pitch: int = 0, given: bool = False) -> CovspecSparseParams:
+        return CovspecSparseParams(self.attend.c_struct(q_pitch, out_pitch), self.top, self.first, self.recent, int(given))
+
+
+def sparse_workspace_size(p: SparseParams, given: bool = False) -> int:
+    cs = p.c_struct(given=given)
+    return int(load_library().covspec_sparse_workspace_size(ctypes.byref(cs)))
+
+
+def sparse_attend(p: SparseParams, q, start, length, pages, cache, summary, visible=None, blocks=None, workspace=None, out=None, want_lse=False, blocks_out=None):
+    """covspec_sparse_attend: (out [T, heads, D], lse [T, heads] fp32 or None, blocks [T, Hkv, top] int32).  With `blocks` these are attended to and
+    `summary` may be None; else the choice goes to blocks_out or a new tensor.  Padding rows of outputs allocated here are unspecified."""
+    import torch
+    c, a = p.attend.cache, p.attend
+    given = blocks is not None
+    if given and blocks_out is not None:
+        raise ValueError("blocks are either given or chosen")
+    if not given and summary is None:
+        raise ValueError("blocks are chosen by their summaries")
+    dev = _same_device(q, start, length, pages, visible, workspace, out, blocks, blocks_out, *cache, *(summary or ()))
+    dt = _types()[c.dtype]
+    qp, q_pitch = _rows(q, "q", c.n_tokens, a.n_heads, c.head_dim, dt)
+    out = torch.empty(c.n_tokens, a.n_heads, c.head_dim, dtype=dt, device=dev) if out is None else out
+    op, out_pitch = _rows(out, "out", c.n_tokens, a.n_heads, c.head_dim, dt)
+    batch, pool = _cache_ptrs(c, start, length, pages, cache)
+    bits = _expect(visible, "visible", (c.n_tokens,), _types()["i64"])
+    if not given:
+        blocks = torch.empty(c.n_tokens, c.n_kv_heads, p.top, dtype=torch.int32, device=dev) if blocks_out is None else blocks_out
+    bp = _expect(blocks, "blocks", (c.n_tokens, c.n_kv_heads, p.top), _types()["i32"])
+    sp = [None, None] if summary is None else _summary_ptrs(c, summary)
+    if workspace is None:
+        n = sparse_workspace_size(p, given)
+        if n == 0:
+            raise CovspecError(INVALID_ARG, "covspec_sparse_workspace_size")
+        workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
+    lse = torch.empty(c.n_tokens, a.n_heads, dtype=torch.float32, device=dev) if want_lse else None
+    wp, wb = _ws_args(workspace)
+    cs = p.c_struct(q_pitch, out_pitch, given)
+    st = _call_on(dev, load_library().covspec_sparse_attend, ctypes.byref(cs), qp, *batch, *pool, *sp, bits, bp, op, _ptr(lse), wp, wb)
+    if st != OK:
+        raise CovspecError(st, "covspec_sparse_attend")
+    return out, lse, blocks

@@ -20,23 +20,6 @@ constexpr int HEADS = 2;
 
 // lanes of a row: a power of two, so that exchanges stay inside; head dimension 96 leaves a quarter of them without work
 constexpr int row_lanes(int D) { return D == 64 ? 8 : 16; }
-constexpr float kTiny = 0x1p-100f;              // smaller maxima: (1 / amax) Q and the products with it would leave the range of fp32
-
-template <int KEPT> constexpr float kTop = KEPT == DT_I8 ? 127.f : 448.f;
-
-template <int KEPT>
-__device__ __forceinline__ uint32_t encode4(const float (&y)[4]) {
-  if constexpr (KEPT == DT_I8) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w |= ((uint32_t)(int)rintf(y[e]) & 0xFFu) << (8 * e);
-    return w;
-  } else {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
-  }
-}
-
 // Codes of the row that LANES neighbouring lanes hold eight values of each; the scale is the same in all of them.
 template <int DT, int KEPT, int LANES>
 __device__ __forceinline__ u32x2_t quantise(const u32x4_t& raw, float& scale) {
@@ -51,19 +34,11 @@ __device__ __forceinline__ u32x2_t quantise(const u32x4_t& raw, float& scale) {
   }
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  const float amax = __uint_as_float(top);
-  const bool finite = top < 0x7F800000u;
-  const float inv = finite && amax >= kTiny ? (1.f / amax) * kTop<KEPT> : 0.f;
-  scale = !finite ? __uint_as_float(0x7FC00000u) : amax >= kTiny ? amax / kTop<KEPT> : 0.f;
+  float inv;
+  const bool finite = code_step<KEPT>(top, inv, scale);
   u32x2_t out;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float y[4];
-#pragma unroll
-    // three roundings: the largest may come out some parts in 2^23 above Q
-    for (int e = 0; e < 4; ++e) y[e] = finite ? __builtin_amdgcn_fmed3f(x[4 * h + e] * inv, -kTop<KEPT>, kTop<KEPT>) : 0.f;
-    out[h] = encode4<KEPT>(y);
-  }
+  for (int h = 0; h < 2; ++h) out[h] = encode_row4<KEPT>(x + 4 * h, inv, finite);
   return out;
 }
 

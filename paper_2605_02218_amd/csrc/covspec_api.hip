@@ -840,6 +840,18 @@ static int attend_check(const covspec_attend_params* p, Paged* c) {
   return COVSPEC_OK;
 }
 
+static Attend attend_of(const Paged& c, const covspec_attend_params& p, const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                        const float* v_scale, const int64_t* visible, void* out, float* lse_out) {
+  Attend a;
+  a.q = q; a.q_pitch = p.q_pitch ? p.q_pitch : (long)p.n_heads * c.D;
+  a.heads = p.n_heads; a.max_len = p.max_len; a.window = p.window < 1 << 30 ? p.window : 1 << 30; a.scale = p.scale;
+  a.kc = k_cache; a.vc = v_cache; a.ks = k_scale; a.vs = v_scale;
+  a.visible = (const long long*)visible;
+  a.out = out; a.out_pitch = p.out_pitch ? p.out_pitch : (long)p.n_heads * c.D;
+  a.lse = lse_out;
+  return a;
+}
+
 size_t covspec_attend_workspace_size(const covspec_attend_params* p) {
   Paged c;
   if (attend_check(p, &c) != COVSPEC_OK) return 0;
@@ -856,15 +868,199 @@ int covspec_attend(const covspec_attend_params* p, const void* q, const int32_t*
   if (!workspace || ((uintptr_t)workspace & 255) || ((uintptr_t)visible & 7) || ((uintptr_t)lse_out & 3)) return COVSPEC_INVALID_ARG;
   if (visible && p->window != 0) return COVSPEC_INVALID_ARG;      // a tree's rows are not its positions
   if (workspace_bytes < attend_workspace_bytes(c, p->n_heads, p->max_len)) return COVSPEC_WORKSPACE_TOO_SMALL;
-  Attend a;
-  a.q = q; a.q_pitch = p->q_pitch ? p->q_pitch : (long)p->n_heads * c.D;
-  a.heads = p->n_heads; a.max_len = p->max_len; a.window = p->window < 1 << 30 ? p->window : 1 << 30; a.scale = p->scale;
-  a.kc = k_cache; a.vc = v_cache; a.ks = k_scale; a.vs = v_scale;
-  a.visible = (const long long*)visible;
-  a.out = out; a.out_pitch = p->out_pitch ? p->out_pitch : (long)p->n_heads * c.D;
-  a.lse = lse_out;
+  const Attend a = attend_of(c, *p, q, k_cache, v_cache, k_scale, v_scale, visible, out, lse_out);
   discard_pending_error();
   return launched("launch_attend", launch_attend(c, a, workspace, (hipStream_t)stream));
+}
+
+// ---- page tables, rotary positions, attention over selected pages (around the same cache)
+static int pages_check(const covspec_pages_params* p, Pages* g) {
+  if (!p) return COVSPEC_INVALID_ARG;
+  if (p->n_seq < 1 || p->n_tokens < 0 || p->page_size < 1 || p->n_pages < 1 || p->max_pages < 1) return COVSPEC_INVALID_ARG;
+  if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)) != 0) return COVSPEC_UNSUPPORTED;
+  const int64_t most = 1 << 30;
+  if (p->n_seq > 65536 || (int64_t)p->n_seq * p->max_pages >= most || p->n_tokens >= most || p->n_pages >= most ||
+      (int64_t)p->max_pages * p->page_size >= most) return COVSPEC_UNSUPPORTED;
+  *g = Pages{};
+  g->S = p->n_seq; g->T = p->n_tokens; g->n_pages = p->n_pages; g->max_pages = p->max_pages;
+  while ((1 << g->page_shift) < p->page_size) ++g->page_shift;
+  return COVSPEC_OK;
+}
+
+size_t covspec_pages_workspace_size(const covspec_pages_params* p) {
+  Pages g;
+  return pages_check(p, &g) == COVSPEC_OK ? pages_workspace_bytes(g.S) : 0;
+}
+
+int covspec_pages_step(const covspec_pages_params* p, const int32_t* want, const int32_t* rows, int32_t* pages, int32_t* held,
+                       int32_t* borrowed, int32_t* free_pages, int32_t* n_free, int32_t* start, int32_t* length, int32_t* outcome,
+                       int64_t* slots, int32_t* positions, void* workspace, size_t workspace_bytes, covspec_stream_t stream) {
+  Pages g;
+  const int st = pages_check(p, &g);
+  if (st != COVSPEC_OK) return st;
+  if (!want || !rows || !pages || !held || !borrowed || !free_pages || !n_free || !start || !length || !outcome || !workspace) return COVSPEC_INVALID_ARG;
+  if (((uintptr_t)want | (uintptr_t)rows | (uintptr_t)pages | (uintptr_t)held | (uintptr_t)borrowed | (uintptr_t)free_pages | (uintptr_t)n_free | (uintptr_t)start |
+       (uintptr_t)length | (uintptr_t)outcome | (uintptr_t)positions) & 3) return COVSPEC_INVALID_ARG;
+  if (((uintptr_t)slots & 7) || ((uintptr_t)workspace & 255)) return COVSPEC_INVALID_ARG;
+  if (workspace_bytes < pages_workspace_bytes(g.S)) return COVSPEC_WORKSPACE_TOO_SMALL;
+  g.want = want; g.rows = rows; g.pages = pages; g.held = held; g.borrowed = borrowed; g.free_pages = free_pages; g.n_free = n_free;
+  g.start = start; g.length = length; g.outcome = outcome; g.slots = slots; g.positions = positions;
+  discard_pending_error();
+  return launched("launch_pages", launch_pages(g, workspace, (hipStream_t)stream));
+}
+
+int covspec_rotary_steps(const covspec_rotary_scaling* s, int32_t rotary_dim, uint64_t* steps_out) {
+  if (!s || !steps_out || rotary_dim < 2 || rotary_dim % 2 != 0) return COVSPEC_INVALID_ARG;
+  if (rotary_dim > 1 << 20) return COVSPEC_UNSUPPORTED;
+  const int kind = s->kind, R = rotary_dim;
+  auto positive = [](double x) { return x > 0.0 && x < INFINITY; };
+  if (kind < COVSPEC_ROTARY_PLAIN || kind > COVSPEC_ROTARY_RAMP || !positive(s->base)) return COVSPEC_INVALID_ARG;
+  if (kind != COVSPEC_ROTARY_PLAIN && !positive(s->factor)) return COVSPEC_INVALID_ARG;
+  if (kind == COVSPEC_ROTARY_BASE && R < 4) return COVSPEC_INVALID_ARG;
+  if (kind == COVSPEC_ROTARY_BANDS || kind == COVSPEC_ROTARY_RAMP) {
+    if (s->original_len < 1 || !(s->low < s->high) || !(fabs(s->low) < INFINITY) || !(fabs(s->high) < INFINITY)) return COVSPEC_INVALID_ARG;
+    if (kind == COVSPEC_ROTARY_RAMP && (!(s->low > 0.0) || !(s->base > 1.0))) return COVSPEC_INVALID_ARG;
+  }
+  // 64 bits of significand throughout, as many as a step has
+  const long double two_pi = 6.283185307179586476925286766559L, factor = s->factor;
+  long double base = s->base;
+  if (kind == COVSPEC_ROTARY_BASE) base *= powl(factor, (long double)R / (R - 2));
+  long double a = 0, b = 1;
+  if (kind == COVSPEC_ROTARY_RAMP) {
+    auto index = [&](double turns) { return R * logl(s->original_len / (turns * two_pi)) / (2 * logl(base)); };
+    a = fmaxl(floorl(index(s->high)), 0);
+    b = a + fmaxl(fminl(ceill(index(s->low)), R - 1) - a, 0.001L);
+  }
+  for (int i = 0; i < R / 2; ++i) {
+    long double f = powl(base, -2.0L * i / R), keep = 1;
+    if (kind == COVSPEC_ROTARY_LINEAR) f /= factor;
+    if (kind == COVSPEC_ROTARY_BANDS) keep = (s->original_len * f / two_pi - s->low) / ((long double)s->high - s->low);
+    if (kind == COVSPEC_ROTARY_RAMP) keep = 1 - (i - a) / (b - a);
+    if (kind == COVSPEC_ROTARY_BANDS || kind == COVSPEC_ROTARY_RAMP) {
+      keep = fminl(fmaxl(keep, 0), 1);
+      f *= keep + (1 - keep) / factor;
+    }
+    long double turns = f / two_pi;
+    if (!(turns < INFINITY)) return COVSPEC_INVALID_ARG;
+    turns -= floorl(turns);                               // whole turns turn nothing
+    const long double step = rintl(turns * 18446744073709551616.0L);
+    steps_out[i] = step >= 18446744073709551616.0L ? 0 : (uint64_t)step;
+  }
+  return COVSPEC_OK;
+}
+
+static int rotary_check(const covspec_rotary_params* p, Paged* c, Rotate* r) {
+  if (!p) return COVSPEC_INVALID_ARG;
+  if (p->n_seq < 1 || p->n_tokens < 1 || p->n_heads < 1 || p->n_kv_heads < 1 || p->head_dim < 1 || p->rotary_dim < 1 || p->n_axes < 1) return COVSPEC_INVALID_ARG;
+  if (p->dtype != COVSPEC_BF16 && p->dtype != COVSPEC_FP16) return COVSPEC_INVALID_ARG;
+  if (p->rotary_dim > p->head_dim || !(fabsf(p->magnitude) < INFINITY) || (p->interleaved != 0 && p->interleaved != 1)) return COVSPEC_INVALID_ARG;
+  const int64_t dq = (int64_t)p->n_heads * p->head_dim, dk = (int64_t)p->n_kv_heads * p->head_dim, far = (int64_t)1 << 32;
+  const int64_t pitch[4] = {p->q_pitch, p->q_out_pitch, p->k_pitch, p->k_out_pitch};
+  for (int i = 0; i < 4; ++i)
+    if (pitch[i] != 0 && (pitch[i] < (i < 2 ? dq : dk) || pitch[i] % 8 != 0)) return COVSPEC_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 96 && p->head_dim != 128) return COVSPEC_UNSUPPORTED;
+  if (p->rotary_dim % 16 != 0 || p->n_axes > 4 || p->n_seq >= 1 << 30) return COVSPEC_UNSUPPORTED;
+  if ((int64_t)p->n_tokens * ((int64_t)p->n_heads + p->n_kv_heads) >= 1 << 30) return COVSPEC_UNSUPPORTED;
+  for (const int64_t x : pitch)
+    if (x > far) return COVSPEC_UNSUPPORTED;
+  *c = Paged{};
+  c->S = p->n_seq; c->T = p->n_tokens; c->H = p->n_kv_heads; c->D = p->head_dim; c->dtype = p->dtype;
+  *r = Rotate{};
+  r->heads = p->n_heads; r->R = p->rotary_dim; r->interleaved = p->interleaved; r->n_axes = p->n_axes; r->magnitude = p->magnitude;
+  r->q_pitch = p->q_pitch ? p->q_pitch : dq;
+  r->q_out_pitch = p->q_out_pitch ? p->q_out_pitch : dq;
+  r->k_pitch = p->k_pitch ? p->k_pitch : dk;
+  r->k_out_pitch = p->k_out_pitch ? p->k_out_pitch : dk;
+  return COVSPEC_OK;
+}
+
+static bool rotary_arrays(Rotate* r, const uint64_t* steps, const int32_t* positions, const int32_t* axis, const int32_t* start, const int32_t* length) {
+  r->steps = steps; r->positions = positions; r->axis = axis;
+  return steps && !((uintptr_t)steps & 7) && !(((uintptr_t)positions | (uintptr_t)axis | (uintptr_t)start | (uintptr_t)length) & 3);
+}
+
+int covspec_rotate(const covspec_rotary_params* p, const void* q, const void* k, const uint64_t* steps, const int32_t* positions,
+                   const int32_t* axis, const int32_t* start, const int32_t* length, void* q_out, void* k_out, covspec_stream_t stream) {
+  Paged c;
+  Rotate r;
+  const int st = rotary_check(p, &c, &r);
+  if (st != COVSPEC_OK) return st;
+  if ((!q && !k) || !q != !q_out || !k != !k_out || !rotary_arrays(&r, steps, positions, axis, start, length)) return COVSPEC_INVALID_ARG;
+  if (!start != !length || (!start && !positions)) return COVSPEC_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out) & 15) return COVSPEC_INVALID_ARG;
+  if ((q && q == q_out && r.q_pitch != r.q_out_pitch) || (k && k == k_out && r.k_pitch != r.k_out_pitch)) return COVSPEC_INVALID_ARG;      // rows of one on rows of another
+  c.start = start; c.length = length;
+  r.q = (const uint16_t*)q; r.k = (const uint16_t*)k; r.q_out = (uint16_t*)q_out; r.k_out = (uint16_t*)k_out;
+  discard_pending_error();
+  return launched("launch_rotate", launch_rotate(c, r, (hipStream_t)stream));
+}
+
+int covspec_rotate_write(const covspec_rotary_params* p, const covspec_cache_params* cp, const void* q, const void* k, const void* v,
+                         const uint64_t* steps, const int32_t* positions, const int32_t* axis, const int32_t* start, const int32_t* length,
+                         const int32_t* pages, void* q_out, void* k_cache, void* v_cache, float* k_scale, float* v_scale, covspec_stream_t stream) {
+  Paged c;
+  Rotate r;
+  int st = rotary_check(p, &c, &r);
+  if (st != COVSPEC_OK) return st;
+  if (!cp || cp->n_seq != p->n_seq || cp->n_tokens != p->n_tokens || cp->n_kv_heads != p->n_kv_heads || cp->head_dim != p->head_dim || cp->dtype != p->dtype)
+    return COVSPEC_INVALID_ARG;
+  if ((st = cache_check(cp, &c)) != COVSPEC_OK) return st;
+  if ((st = cache_arrays(&c, k, v, start, length, pages, k_cache, v_cache, k_scale, v_scale)) != COVSPEC_OK) return st;
+  if (!q || !q_out || !rotary_arrays(&r, steps, positions, axis, start, length) || (((uintptr_t)q | (uintptr_t)q_out) & 15)) return COVSPEC_INVALID_ARG;
+  if (q == q_out && r.q_pitch != r.q_out_pitch) return COVSPEC_INVALID_ARG;
+  r.q = (const uint16_t*)q; r.k = (const uint16_t*)k; r.v = (const uint16_t*)v; r.q_out = (uint16_t*)q_out;
+  r.kc = k_cache; r.vc = v_cache; r.ks = k_scale; r.vs = v_scale;
+  discard_pending_error();
+  return launched("launch_rotate", launch_rotate(c, r, (hipStream_t)stream));
+}
+
+int covspec_block_summary(const covspec_cache_params* p, const int32_t* start, const int32_t* length, const int32_t* pages, const void* k_cache,
+                          const float* k_scale, void* summary, float* summary_scale, covspec_stream_t stream) {
+  Paged c;
+  int st = cache_check(p, &c);
+  if (st != COVSPEC_OK) return st;
+  // there is no second tensor, nor values
+  if ((st = cache_arrays(&c, k_cache, k_cache, start, length, pages, k_cache, k_cache, k_scale, k_scale)) != COVSPEC_OK) return st;
+  if (!summary || !summary_scale || ((uintptr_t)summary & 15) || ((uintptr_t)summary_scale & 3)) return COVSPEC_INVALID_ARG;
+  if (!summary_fits(c)) return COVSPEC_UNSUPPORTED;
+  discard_pending_error();
+  return launched("launch_summary", launch_summary(c, k_cache, k_scale, (int8_t*)summary, summary_scale, (hipStream_t)stream));
+}
+
+static int sparse_check(const covspec_sparse_params* p, Paged* c) {
+  if (!p) return COVSPEC_INVALID_ARG;
+  const int st = attend_check(&p->attend, c);
+  if (st != COVSPEC_OK) return st;
+  if (p->attend.window != 0 || p->top < 1 || p->first < 0 || p->recent < 0 || (int64_t)p->first + p->recent > p->top || (p->given != 0 && p->given != 1))
+    return COVSPEC_INVALID_ARG;
+  if (p->top > 1024 || !sparse_fits(*c, p->attend.n_heads, p->attend.max_len, p->top)) return COVSPEC_UNSUPPORTED;
+  return COVSPEC_OK;
+}
+
+size_t covspec_sparse_workspace_size(const covspec_sparse_params* p) {
+  Paged c;
+  if (sparse_check(p, &c) != COVSPEC_OK) return 0;
+  return sparse_workspace_bytes(c, p->attend.n_heads, p->attend.max_len, p->top, p->given != 0);
+}
+
+int covspec_sparse_attend(const covspec_sparse_params* p, const void* q, const int32_t* start, const int32_t* length, const int32_t* pages,
+                          const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, const void* summary,
+                          const float* summary_scale, const int64_t* visible, int32_t* blocks, void* out, float* lse_out, void* workspace,
+                          size_t workspace_bytes, covspec_stream_t stream) {
+  Paged c;
+  int st = sparse_check(p, &c);
+  if (st != COVSPEC_OK) return st;
+  if ((st = cache_arrays(&c, q, out, start, length, pages, k_cache, v_cache, k_scale, v_scale)) != COVSPEC_OK) return st;
+  if (!blocks || !workspace || ((uintptr_t)workspace & 255) || ((uintptr_t)visible & 7) || (((uintptr_t)lse_out | (uintptr_t)blocks) & 3)) return COVSPEC_INVALID_ARG;
+  if (!p->given && (!summary || !summary_scale || ((uintptr_t)summary & 15) || ((uintptr_t)summary_scale & 3))) return COVSPEC_INVALID_ARG;
+  const covspec_attend_params& t = p->attend;
+  if (workspace_bytes < sparse_workspace_bytes(c, t.n_heads, t.max_len, p->top, p->given != 0)) return COVSPEC_WORKSPACE_TOO_SMALL;
+  const Attend a = attend_of(c, t, q, k_cache, v_cache, k_scale, v_scale, visible, out, lse_out);
+  Sparse sp;
+  sp.top = p->top; sp.first = p->first; sp.recent = p->recent; sp.given = p->given != 0;
+  sp.summary = (const int8_t*)summary; sp.scales = summary_scale; sp.blocks = blocks;
+  discard_pending_error();
+  return launched("launch_sparse", launch_sparse(c, a, sp, workspace, (hipStream_t)stream));
 }
 
 int covspec_adjust_logits(const covspec_logits_params* p, const void* z, const int32_t* history, const int32_t* history_start,

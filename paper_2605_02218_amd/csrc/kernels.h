@@ -275,6 +275,46 @@ size_t attend_workspace_bytes(const Paged& c, int heads, int max_len);
 bool attend_fits(const Paged& c, int heads, int max_len);
 hipError_t launch_attend(const Paged& c, const Attend& a, void* ws, hipStream_t stream);
 
+// ---------------------------------------------------------------- pages.hip
+struct Pages {
+  int S, T, page_shift, n_pages, max_pages;
+  const int32_t *want, *rows;
+  int32_t *pages, *held, *borrowed, *free_pages, *n_free;        // the state
+  int32_t *start, *length, *outcome;
+  int64_t* slots;                      // or null
+  int32_t* positions;                  // or null
+};
+size_t pages_workspace_bytes(int S);
+hipError_t launch_pages(const Pages& p, void* ws, hipStream_t stream);
+
+// ---------------------------------------------------------------- rotate.hip
+struct Rotate {
+  const uint16_t *q, *k, *v;           // q or k may be null; v with a cache
+  uint16_t *q_out, *k_out;
+  long q_pitch, k_pitch, q_out_pitch, k_out_pitch;
+  int heads, R, interleaved, n_axes, step;
+  float magnitude;
+  const uint64_t* steps;
+  const int32_t *positions, *axis;     // or null
+  void *kc, *vc;                       // the cache, or null
+  float *ks, *vs;
+};
+hipError_t launch_rotate(const Paged& c, const Rotate& r, hipStream_t stream);
+
+// ---------------------------------------------------------------- sparse.hip
+struct Sparse {
+  int top, first, recent;
+  bool given;                          // the blocks are the caller's
+  const int8_t* summary;
+  const float* scales;
+  int32_t* blocks;
+};
+bool summary_fits(const Paged& c);
+hipError_t launch_summary(const Paged& c, const void* kc, const float* ks, int8_t* summary, float* scales, hipStream_t stream);
+size_t sparse_workspace_bytes(const Paged& c, int heads, int max_len, int top, bool given);
+bool sparse_fits(const Paged& c, int heads, int max_len, int top);
+hipError_t launch_sparse(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream);
+
 // ---------------------------------------------------------------- adjust.hip
 struct Adjust {
   const void* z;

@@ -71,4 +71,40 @@ __device__ __forceinline__ f32x4_t decode4(uint32_t w) {
   }
 }
 
+// Codes of a row: x ((1 / amax) Q) to the nearest, ties to even.
+constexpr float kTiny = 0x1p-100f;              // smaller maxima: (1 / amax) Q and the products with it would leave the range of fp32
+
+template <int KEPT> constexpr float kTop = KEPT == DT_I8 ? 127.f : 448.f;
+
+template <int KEPT>
+__device__ __forceinline__ uint32_t encode4(const float (&y)[4]) {
+  if constexpr (KEPT == DT_I8) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w |= ((uint32_t)(int)rintf(y[e]) & 0xFFu) << (8 * e);
+    return w;
+  } else {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  }
+}
+
+// 1 / step and step of a row's codes, from its largest magnitude as the bits of a float (NaN above infinity above the finite ones); false: not finite.
+template <int KEPT>
+__device__ __forceinline__ bool code_step(uint32_t top, float& inv, float& scale) {
+  const float amax = __uint_as_float(top);
+  const bool finite = top < 0x7F800000u;
+  inv = finite && amax >= kTiny ? (1.f / amax) * kTop<KEPT> : 0.f;
+  scale = !finite ? __uint_as_float(0x7FC00000u) : amax >= kTiny ? amax / kTop<KEPT> : 0.f;
+  return finite;
+}
+template <int KEPT>
+__device__ __forceinline__ uint32_t encode_row4(const float* x, float inv, bool finite) {
+  float y[4];
+#pragma unroll
+  // three roundings: the largest may come out some parts in 2^23 above Q
+  for (int e = 0; e < 4; ++e) y[e] = finite ? __builtin_amdgcn_fmed3f(x[e] * inv, -kTop<KEPT>, kTop<KEPT>) : 0.f;
+  return encode4<KEPT>(y);
+}
+
 }  // namespace covspec

@@ -1,0 +1,208 @@
+// Rotary positions: rows of q and k turned, to new rows, in place, or with v straight into the paged cache.
+//
+// Pair (x1, x2) number i of a row at position pos: y1 = x1 c - x2 s, y2 = x2 c + x1 s, (c, s) = magnitude (cos, sin)(2 pi u), u = frac(pos step_i).
+// step_i is a 64-bit binary fraction of a turn, so pos step_i mod 2^64 is u itself, exact but for the last bits of step_i (2^-33 of a turn at position 2^31).
+// Of u the upper 32 bits go on (1.5e-9 of an angle): an eighth of a turn to both sides of the nearest quarter, where short series are good to 2^-24.
+//
+// D / 16 lanes take a row, 16 elements each: eight pairs, two pieces of 16 bytes.  A lane's cosines and sines serve all rows of a token it takes, every
+// `step`-th of its heads; lanes of neighbouring groups take neighbouring heads.  Bound by memory; single tokens by latency: all heads at once.
+#include <type_traits>
+
+#include "paged.h"
+
+namespace covspec {
+
+namespace {
+
+constexpr int RT = 256;
+
+struct Turn { float c, s; };
+// Cosine and sine of a 64-bit fraction of a turn: series around the nearest quarter, |x| <= pi / 4, errors below 2^-28 of 1; the conversion to a
+// float and the product with 2 pi 2^-32 are off by 2^-24 of x each.
+__device__ __forceinline__ Turn turn_of(uint64_t u, float magnitude) {
+  const uint32_t hi = (uint32_t)(u >> 32), quarter = (hi + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(hi - (quarter << 30)) * (float)(6.283185307179586476925 / 4294967296.0), y = x * x;
+  float s = __builtin_fmaf(y, 1.f / 362880.f, -1.f / 5040.f);
+  s = __builtin_fmaf(y, s, 1.f / 120.f);
+  s = __builtin_fmaf(y, s, -1.f / 6.f);
+  s = __builtin_fmaf(x * y, s, x);
+  float c = __builtin_fmaf(y, -1.f / 3628800.f, 1.f / 40320.f);
+  c = __builtin_fmaf(y, c, -1.f / 720.f);
+  c = __builtin_fmaf(y, c, 1.f / 24.f);
+  c = __builtin_fmaf(y, c, -0.5f);
+  c = __builtin_fmaf(y, c, 1.f);
+  const bool odd = quarter & 1;
+  const float a = odd ? s : c, b = odd ? c : s;
+  return Turn{quarter == 1 || quarter == 2 ? -a * magnitude : a * magnitude, quarter >= 2 ? -b * magnitude : b * magnitude};
+}
+
+__device__ __forceinline__ void load16(const uint16_t* from, int a, int b, u32x4_t (&w)[2]) {
+  w[0] = *(const u32x4_t*)(from + a);
+  w[1] = *(const u32x4_t*)(from + b);
+}
+template <int DT>
+__device__ __forceinline__ void unpack16(const u32x4_t (&w)[2], float (&x)[16]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const f32x2_t p = Half<DT>::unpack(w[e / 4][e % 4]);
+    x[2 * e] = p[0];
+    x[2 * e + 1] = p[1];
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store16(uint16_t* to, int a, int b, const float (&x)[16]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    *(u32x4_t*)(to + (h == 0 ? a : b)) = (u32x4_t){Half<DT>::pack(x[8 * h], x[8 * h + 1]), Half<DT>::pack(x[8 * h + 2], x[8 * h + 3]),
+                                                   Half<DT>::pack(x[8 * h + 4], x[8 * h + 5]), Half<DT>::pack(x[8 * h + 6], x[8 * h + 7])};
+}
+
+// KEPT: what k and v are kept as in the cache; -1: rows, no cache.  FAR: pairs (i, i + R / 2), else (2i, 2i + 1).
+template <int DT, int KEPT, int D, bool FAR>
+__global__ __launch_bounds__(RT) void rotate_kernel(Paged c, Rotate r) {
+  constexpr bool CACHE = KEPT >= 0, CODES = CACHE && KEPT != DT;
+  constexpr int LANES = D == 64 ? 4 : 8;                               // head dimension 96 leaves two of eight without work
+  const long x = (long)blockIdx.x * (RT / LANES) + threadIdx.x / LANES;
+  const int lane = threadIdx.x & (LANES - 1), t = (int)(x / r.step), first = (int)(x % r.step);
+  const bool inside = t < c.T && lane * 16 < D;
+  bool mine = inside;
+  int pos = 0;
+  long place = -1;                                                     // of head 0
+  if (c.start) {
+    const int s = seq_of_wave<64 / LANES>(c.start, c.S, t < c.T ? t : 0x7FFFFFFF);
+    mine = inside && s >= 0 && s < c.S;
+    if (mine) {
+      const long at = (long)c.length[s] - c.start[s + 1] + t;
+      pos = (int)at;
+      if constexpr (CACHE) place = place_of(c, s, at, 0);
+    }
+  }
+  // which elements: eight pairs, or 16 neighbouring ones that are not turned
+  const bool turns = lane * 16 < r.R;
+  const int a = FAR && turns ? 8 * lane : 16 * lane, b = FAR && turns ? r.R / 2 + 8 * lane : 16 * lane + 8;
+  Turn w[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e] = Turn{1.f, 0.f};
+  if (turns && mine) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      int p = pos;
+      if (r.positions) {
+        const int axis = r.axis ? min(max(r.axis[8 * lane + e], 0), r.n_axes - 1) : 0;
+        p = r.positions[(long)axis * c.T + t];
+      }
+      w[e] = turn_of((uint64_t)(int64_t)p * r.steps[8 * lane + e], r.magnitude);
+    }
+  }
+  auto turned = [&](float (&y)[16]) {
+    if (!turns) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = FAR ? e : 2 * e, j = FAR ? e + 8 : 2 * e + 1;
+      const float x1 = y[i], x2 = y[j];
+      y[i] = __builtin_fmaf(x1, w[e].c, -(x2 * w[e].s));
+      y[j] = __builtin_fmaf(x2, w[e].c, x1 * w[e].s);
+    }
+  };
+  // a row of codes: the lanes of the row exchange their maxima, so all of them come here
+  auto keep = [&](const float (&y)[16], bool has, long to, void* codes, float* scales) {
+    if constexpr (CODES) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(y[e]) & 0x7FFFFFFFu);
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+      float inv, scale;
+      const bool finite = code_step<KEPT>(top, inv, scale);
+      if (has) {
+        uint8_t* const row = (uint8_t*)codes + to * D;
+        *(u32x2_t*)(row + a) = (u32x2_t){encode_row4<KEPT>(y, inv, finite), encode_row4<KEPT>(y + 4, inv, finite)};
+        *(u32x2_t*)(row + b) = (u32x2_t){encode_row4<KEPT>(y + 8, inv, finite), encode_row4<KEPT>(y + 12, inv, finite)};
+        if (lane == 0) scales[to] = scale;
+      }
+    } else {
+      if (has) store16<DT>((uint16_t*)codes + to * D, a, b, y);
+    }
+  };
+  const int rows_q = r.q ? r.heads : 0, rows = rows_q + (r.k ? c.H : 0);
+  // all lanes of a wave stay to the end of the loop where rows exchange their maxima
+  for (int h0 = 0; h0 < rows; h0 += r.step) {
+    const int h = h0 + first;
+    const bool has = mine && h < rows;
+    if (h < rows_q) {
+      if (has) {
+        u32x4_t raw[2];
+        float y[16];
+        load16(r.q + t * r.q_pitch + (long)h * D, a, b, raw);
+        unpack16<DT>(raw, y);
+        turned(y);
+        store16<DT>(r.q_out + t * r.q_out_pitch + (long)h * D, a, b, y);
+      }
+    } else {
+      const int g = h - rows_q;
+      u32x4_t raw[2] = {}, raw_v[2] = {};
+      float y[16];
+      const bool goes = CACHE ? has && place >= 0 : has;
+      if (goes) {
+        load16(r.k + t * r.k_pitch + (long)g * D, a, b, raw);
+        if constexpr (CACHE) load16(r.v + t * r.k_pitch + (long)g * D, a, b, raw_v);
+      }
+      unpack16<DT>(raw, y);
+      turned(y);
+      if constexpr (CACHE) {
+        const long to = place + ((long)g << c.page_shift);
+        keep(y, goes, to, r.kc, r.ks);
+        if constexpr (CODES) {
+          unpack16<DT>(raw_v, y);
+          keep(y, goes, to, r.vc, r.vs);
+        } else if (goes) {
+          *(u32x4_t*)((uint16_t*)r.vc + to * D + a) = raw_v[0];
+          *(u32x4_t*)((uint16_t*)r.vc + to * D + b) = raw_v[1];
+        }
+      } else if (goes) {
+        store16<DT>(r.k_out + t * r.k_out_pitch + (long)g * D, a, b, y);
+      }
+    }
+  }
+}
+
+template <int DT, int KEPT, int D>
+hipError_t launch_dim(const Paged& c, Rotate r, hipStream_t stream) {
+  constexpr int LANES = D == 64 ? 4 : 8;
+  const int rows = (r.q ? r.heads : 0) + (r.k ? c.H : 0);
+  r.step = rows;
+  while (r.step > 4 && (long)c.T * r.step * LANES > 256l * 2048) r.step = (r.step + 1) / 2;
+  const unsigned grid = (unsigned)(((long)c.T * r.step * LANES + RT - 1) / RT);
+  if (r.interleaved)
+    hipLaunchKernelGGL((rotate_kernel<DT, KEPT, D, false>), dim3(grid), dim3(RT), 0, stream, c, r);
+  else
+    hipLaunchKernelGGL((rotate_kernel<DT, KEPT, D, true>), dim3(grid), dim3(RT), 0, stream, c, r);
+  return hipGetLastError();
+}
+
+template <int DT, int KEPT>
+hipError_t launch_kept(const Paged& c, const Rotate& r, hipStream_t stream) {
+  if (c.D == 64) return launch_dim<DT, KEPT, 64>(c, r, stream);
+  if (c.D == 96) return launch_dim<DT, KEPT, 96>(c, r, stream);
+  if (c.D == 128) return launch_dim<DT, KEPT, 128>(c, r, stream);
+  return hipErrorInvalidValue;
+}
+
+template <int DT>
+hipError_t launch_type(const Paged& c, const Rotate& r, hipStream_t stream) {
+  if (!r.kc) return launch_kept<DT, -1>(c, r, stream);
+  if (c.kept == DT) return launch_kept<DT, DT>(c, r, stream);
+  if (c.kept == DT_I8) return launch_kept<DT, DT_I8>(c, r, stream);
+  if (c.kept == DT_E4M3) return launch_kept<DT, DT_E4M3>(c, r, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const Paged& c, const Rotate& r, hipStream_t stream) {
+  if (c.dtype == DT_BF16) return launch_type<DT_BF16>(c, r, stream);
+  if (c.dtype == DT_F16) return launch_type<DT_F16>(c, r, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace covspec

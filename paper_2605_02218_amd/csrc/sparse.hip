@@ -1,0 +1,955 @@
+// Attention over the pages that a cheap score selects for each row: summaries of pages, scores, the choice, attention over it.
+//
+// A page's summary is, channel by channel, the largest and the smallest of its keys as int8 codes with one scale.  For codes c of a query, which are those of
+// an 8-bit row, sum_d max(c_d largest_d, c_d smallest_d) = sum_d max(c_d, 0) largest_d + min(c_d, 0) smallest_d is a product over 2 D terms, exact in
+// int32 whatever its order, and fewer than 2^24; two fp32 products with the scales follow.  So the scores are defined to the bit, and with them
+// the choice, on any machine.  A block costs 2 D + 4 bytes to score and page_size 2 D e to attend to.
+#include <algorithm>
+#include <type_traits>
+
+#include "host_cache.h"
+#include "tiles.h"
+
+namespace covspec {
+
+namespace {
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+// Rows and lengths as covspec_attend takes them.  t uniform in the wave; false: a padding row.
+struct Row { int s, row0, n, old; };
+__device__ __forceinline__ bool row_of(const Paged& c, int t, Row& r) {
+  r.s = seq_of_wave<1>(c.start, c.S, t);
+  if (t >= c.T || r.s < 0 || r.s >= c.S) return false;
+  r.s = __builtin_amdgcn_readfirstlane(r.s);
+  r.row0 = min(max(c.start[r.s], 0), c.T);
+  r.n = max(min(c.start[r.s + 1], c.T), r.row0) - r.row0;
+  r.old = (int)max((long)c.length[r.s] - r.n, -(1l << 30));
+  return true;
+}
+// End of what row i of the chunk sees.
+__device__ __forceinline__ int seen_end(const Paged& c, const Row& r, int i, int max_len, bool tree) {
+  const long cap = min((long)max_len, (long)c.max_pages << c.page_shift), hi = (long)r.old + (tree ? min(r.n, 64) : i + 1);
+  return (int)max(min(hi, cap), 0l);
+}
+__device__ __forceinline__ int blocks_up_to(const Paged& c, int end) { return (int)(((long)end + (1 << c.page_shift) - 1) >> c.page_shift); }
+
+// ---- summaries
+
+template <int DT, int KEPT, int D> struct Piece {
+  static constexpr bool CODES = KEPT != DT;
+  static constexpr int N = CODES ? 16 : 8;             // channels of a lane: 16 bytes
+  static constexpr int LANES = D / N <= 4 ? 4 : D / N <= 8 ? 8 : 16;       // of a row; head dimension 96 leaves a quarter without work
+};
+
+// A wave takes a page of a key head, or (WAVES = 4) a workgroup a large one.  BY_ROW: an item is a row, the first of its sequence's on the page does the work;
+// else items are the pages that each sequence's rows touch, one sequence behind the other.
+template <int DT, int KEPT, int D, int WAVES, bool BY_ROW>
+__global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const void* __restrict__ kc, const float* __restrict__ ks, int8_t* __restrict__ summary,
+                                                      float* __restrict__ scales) {
+  typedef Piece<DT, KEPT, D> P;
+  constexpr int N = P::N, LANES = P::LANES, ROWS = 64 / LANES;
+  __shared__ float shared[WAVES > 1 ? WAVES : 1][WAVES > 1 ? 2 * D + 1 : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long item = WAVES > 1 ? blockIdx.x : (long)blockIdx.x * 4 + wave;
+  if (item >= items) return;
+  const int x = (int)(item / c.H), g = (int)(item % c.H);
+  const int shift = c.page_shift, cap = c.max_pages << shift;
+  int s = -1, block = 0;
+  if constexpr (BY_ROW) {
+    Row r;
+    if (!row_of(c, x, r)) return;
+    const long pos = (long)c.length[r.s] - c.start[r.s + 1] + x;
+    if (pos < 0 || pos >= cap || (x != c.start[r.s] && (pos & ((1 << shift) - 1)) != 0)) return;
+    s = r.s;
+    block = (int)(pos >> shift);
+  } else {
+    int left = x;
+    for (int s0 = 0; s0 < c.S && s < 0; s0 += 64) {
+      const int mine = min(s0 + lane, c.S - 1), row0 = min(max(c.start[mine], 0), c.T), n = max(min(c.start[mine + 1], c.T), row0) - row0, len = c.length[mine];
+      const int lo = max(len - n, 0), hi = min(len, cap);
+      const int own = s0 + lane < c.S && n > 0 && lo < hi ? ((hi - 1) >> shift) - (lo >> shift) + 1 : 0, upto = wave_inscan(own);
+      const unsigned long long over = __ballot(upto > left);
+      if (over) {
+        const int at = __ffsll((long long)over) - 1;
+        s = s0 + at;
+        block = (__builtin_amdgcn_readlane(lo, at) >> shift) + left - __builtin_amdgcn_readlane(upto, at) + __builtin_amdgcn_readlane(own, at);
+      }
+      left -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (s < 0) return;
+  }
+  const int page = c.pages[(long)s * c.max_pages + block];
+  if (page < 0 || page >= c.n_pages) return;
+  const int count = min(min(c.length[s], cap) - (block << shift), 1 << shift);          // positions of the page: at least one, if `start` ascends
+  if (count < 1) return;
+  const long first = ((long)page * c.H + g) << shift;
+  const int piece = lane % LANES, row = lane / LANES;
+  float top[N], low[N];
+  uint32_t size = 0;                              // largest magnitude, as bits
+#pragma unroll
+  for (int e = 0; e < N; ++e) { top[e] = -INFINITY; low[e] = INFINITY; }
+  if (piece * N < D) {
+    constexpr int AHEAD = 8;
+    for (int j0 = (WAVES > 1 ? wave * ROWS : 0); j0 < count; j0 += AHEAD * ROWS * WAVES) {
+      u32x4_t raw[AHEAD];
+      float scale[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const long at = first + min(j0 + i * ROWS * WAVES + row, count - 1);           // the last row again behind it
+        raw[i] = *(const u32x4_t*)((const char*)kc + (at * D + piece * N) * (P::CODES ? 1 : 2));
+        if constexpr (P::CODES) scale[i] = ks[at];
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        float v[N];
+        if constexpr (P::CODES) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const f32x4_t f = decode4<KEPT>(raw[i][w]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * w + e] = f[e] * scale[i];
+          }
+        } else {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const f32x2_t f = Half<DT>::unpack(raw[i][w]);
+            v[2 * w] = f[0];
+            v[2 * w + 1] = f[1];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          top[e] = fmaxf(top[e], v[e]);
+          low[e] = fminf(low[e], v[e]);
+          size = max(size, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int o = LANES; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      top[e] = fmaxf(top[e], __shfl_xor(top[e], o, 64));
+      low[e] = fminf(low[e], __shfl_xor(low[e], o, 64));
+    }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) size = max(size, (uint32_t)__shfl_xor((int)size, o, 64));
+  if constexpr (WAVES > 1) {
+    if (row == 0 && piece * N < D) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        shared[wave][piece * N + e] = top[e];
+        shared[wave][D + piece * N + e] = low[e];
+      }
+    }
+    if (lane == 0) shared[wave][2 * D] = __uint_as_float(size);
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      size = max(size, __float_as_uint(shared[w][2 * D]));
+      if (piece * N < D) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          top[e] = fmaxf(top[e], shared[w][piece * N + e]);
+          low[e] = fminf(low[e], shared[w][D + piece * N + e]);
+        }
+      }
+    }
+  }
+  float inv, scale;
+  const bool finite = code_step<DT_I8>(size, inv, scale);
+  const long to = (long)page * c.H + g;
+  if (row == 0 && piece * N < D) {
+#pragma unroll
+    for (int w = 0; w < N / 4; ++w) {
+      *(uint32_t*)(summary + to * 2 * D + piece * N + 4 * w) = encode_row4<DT_I8>(top + 4 * w, inv, finite);
+      *(uint32_t*)(summary + to * 2 * D + D + piece * N + 4 * w) = encode_row4<DT_I8>(low + 4 * w, inv, finite);
+    }
+  }
+  if (lane == 0) scales[to] = scale;
+}
+
+// ---- scores
+
+// A score as an integer of the same order; NaN above all others; 0 is left for blocks that are not there.
+__device__ __forceinline__ uint32_t score_key(float f) { return f != f ? 0xFFFFFFFFu : float_order_key(f); }
+
+// Largest over runs of GP lanes, GP a power of two up to 16.
+__device__ __forceinline__ uint32_t run_max(uint32_t v, int gp) {
+  if (gp >= 2) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));        // quad_perm 1 0 3 2
+  if (gp >= 4) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));        // quad_perm 2 3 0 1
+  if (gp >= 8) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));       // row_half_mirror
+  if (gp >= 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));      // row_mirror
+  return v;
+}
+
+// Blocks are rows of the product, 16 at a time, (token, query head) its columns, 16 NT for a wave: gp columns a token, its heads and then none.
+// A wave takes 64 blocks, all their summaries on their way before the first product.
+constexpr int SCORED = 256;                       // blocks of a workgroup
+template <int DT, int D, int NT>
+__global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, int chunks, int pitch, const int8_t* __restrict__ summary,
+                                                    const float* __restrict__ scales, uint32_t* __restrict__ keys) {
+  constexpr int STEPS = 2 * D / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+  const int G = a.heads / c.H, tokens = 16 * NT / gp;
+  const long item = blockIdx.x / c.H;
+  const int g = blockIdx.x % c.H, t0 = (int)(item / chunks), chunk = (int)(item % chunks);
+  Row r;
+  if (!row_of(c, t0, r)) return;
+  const int i0 = t0 - r.row0;
+  if (i0 % tokens != 0) return;                   // the first row of `tokens` does the work
+  const int i1 = min(i0 + tokens, r.n);
+  const int nb = blocks_up_to(c, seen_end(c, r, i1 - 1, a.max_len, a.visible != nullptr));
+  const int b0 = chunk * SCORED + wave * 64;
+  if (b0 >= nb) return;
+  const int b = b0 + lane;
+  int id = b < nb ? c.pages[(long)r.s * c.max_pages + b] : -1;
+  const bool there = id >= 0 && id < c.n_pages;
+  id = there ? id : 0;
+  const float scale = scales[(long)id * c.H + g];
+  const unsigned long long exists = __ballot(there);
+  i32x4_t m[4][STEPS];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const long from = ((long)__shfl(id, 16 * j + col, 64) * c.H + g) * 2 * D + 16 * quad;
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) m[j][k] = *(const i32x4_t*)(summary + from + 64 * k);
+  }
+  // the queries' codes
+  i32x4_t q[NT][STEPS];
+  float qs[NT];
+  bool real[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int x = 16 * n + col, i = i0 + x / gp, h = x % gp;
+    real[n] = i < i1 && h < G;
+    u32x4_t raw[STEPS][2];
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      const int k0 = 64 * k + 16 * quad, d = k0 >= D ? k0 - D : k0;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        raw[k][p] = (u32x4_t){};
+        if (real[n]) raw[k][p] = *(const u32x4_t*)((const uint16_t*)a.q + (long)(r.row0 + i) * a.q_pitch + (long)(g * G + h) * D + d + 8 * p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x2_t f = Half<DT>::unpack(raw[k][p][e]);
+          top = max(top, max(__float_as_uint(f[0]) & 0x7FFFFFFFu, __float_as_uint(f[1]) & 0x7FFFFFFFu));
+        }
+      }
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    float inv;
+    const bool finite = code_step<DT_I8>(top, inv, qs[n]);
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      const bool neg = 64 * k + 16 * quad >= D;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const f32x2_t f = Half<DT>::unpack(raw[k][w / 2][2 * (w & 1) + e]);
+          y[2 * e] = neg ? fminf(f[0], 0.f) : fmaxf(f[0], 0.f);
+          y[2 * e + 1] = neg ? fminf(f[1], 0.f) : fmaxf(f[1], 0.f);
+        }
+        q[n][k][w] = (int)encode_row4<DT_I8>(y, inv, finite);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float ksc[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ksc[e] = __shfl(scale, 16 * j + 4 * quad + e, 64);
+    uint32_t best[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      i32x4_t acc = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(m[j][k], q[n][k], acc, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool ok = real[n] && (exists >> (16 * j + 4 * quad + e) & 1);
+        best[n][e] = run_max(ok ? score_key(__fmul_rn(__fmul_rn((float)acc[e], ksc[e]), qs[n])) : 0u, min(gp, 16));
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (gp > 16) {                              // a token's heads are in several products; its first one collects them
+        const int parts = gp / 16;
+        if (n % parts != 0) continue;
+#pragma unroll
+        for (int o = 1; o < NT; ++o)
+          if (o < parts && n + o < NT)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) best[n][e] = max(best[n][e], best[n + o][e]);
+      }
+      const int x = 16 * n + col, i = i0 + x / gp;
+      if (x % gp == 0 && i < i1)
+        *(u32x4_t*)(keys + ((long)(r.row0 + i) * c.H + g) * pitch + b0 + 16 * j + 4 * quad) = (u32x4_t){best[n][0], best[n][1], best[n][2], best[n][3]};
+    }
+  }
+}
+
+// ---- the choice
+
+// One workgroup for a row and key head, KPT blocks a thread in registers: the top-th largest key by halving its range, two bits at a time, then the blocks above
+// it and the first ones at it, in order.
+template <int WAVES, int KPT>
+__global__ __launch_bounds__(64 * WAVES) void choose_kernel(Paged c, int max_len, bool tree, int top, int first, int recent, int pitch,
+                                                            const uint32_t* __restrict__ keys, int32_t* __restrict__ blocks) {
+  constexpr int WORDS = WAVES * KPT;
+  __shared__ unsigned long long above[WORDS], equal[WORDS];
+  __shared__ int offset[WORDS], counts[2][3][WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int t = blockIdx.x / c.H;
+  Row r;
+  if (!row_of(c, t, r)) return;
+  const int nb = blocks_up_to(c, seen_end(c, r, t - r.row0, max_len, tree));
+  const uint32_t* const mine = keys + (long)blockIdx.x * pitch;
+  int32_t* const out = blocks + (long)blockIdx.x * top;
+  uint32_t key[KPT];
+#pragma unroll
+  for (int i = 0; i < KPT; ++i) {
+    const int b = i * 64 * WAVES + tid;
+    key[i] = 0;
+    if (b < nb) key[i] = b < first || b >= nb - recent ? 0xFFFFFFFFu : min(mine[b], 0xFFFFFFFEu);
+  }
+  int turn = 0;
+  // how many keys are at least x[0], x[1], x[2]
+  auto count3 = [&](const uint32_t (&x)[3], int (&n)[3]) {
+#pragma unroll
+    for (int w = 0; w < 3; ++w) n[w] = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i)
+#pragma unroll
+      for (int w = 0; w < 3; ++w) n[w] += __popcll(__ballot(key[i] >= x[w]));
+    if constexpr (WAVES > 1) {
+      if (lane < 3) counts[turn][lane][wave] = lane == 0 ? n[0] : lane == 1 ? n[1] : n[2];
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < 3; ++w) {
+        n[w] = 0;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) n[w] += counts[turn][w][k];
+      }
+      turn ^= 1;
+    }
+  };
+  uint32_t at = 1;                                // the key of the last one taken
+  int n[3], taken, more;                          // taken: blocks in all; more: of them at `at` itself
+  {
+    const uint32_t x[3] = {1u, 1u, 1u};
+    count3(x, n);
+  }
+  taken = min(n[0], top);
+  if (n[0] > top) {
+    at = 0;
+    for (int shift = 30; shift >= 0; shift -= 2) {
+      const uint32_t x[3] = {at | 1u << shift, at | 2u << shift, at | 3u << shift};
+      count3(x, n);
+      at = n[2] >= top ? x[2] : n[1] >= top ? x[1] : n[0] >= top ? x[0] : at;
+    }
+    const uint32_t x[3] = {at == 0xFFFFFFFFu ? at : at + 1, 0xFFFFFFFFu, 0xFFFFFFFFu};
+    count3(x, n);
+    more = top - (at == 0xFFFFFFFFu ? 0 : n[0]);
+  } else {
+    more = 0;
+    at = 0;
+  }
+  // in order: word i WAVES + wave holds 64 neighbouring blocks
+#pragma unroll
+  for (int i = 0; i < KPT; ++i) {
+    const unsigned long long up = __ballot(key[i] > at), eq = __ballot(at != 0 && key[i] == at);
+    if (lane == 0) { above[i * WAVES + wave] = up; equal[i * WAVES + wave] = eq; }
+  }
+  __syncthreads();
+  if (wave == 0) {
+    int eq_before = 0, before = 0;
+    for (int w0 = 0; w0 < WORDS; w0 += 64) {
+      const int w = w0 + lane;
+      unsigned long long up = w < WORDS ? above[w] : 0, eq = w < WORDS ? equal[w] : 0;
+      const int eqs = __popcll(eq), eq_upto = wave_inscan(eqs);
+      int room = min(max(more - (eq_before + eq_upto - eqs), 0), eqs);
+      for (int k = eqs; k > room; --k) eq &= ~(1ull << (63 - __builtin_clzll(eq)));
+      up |= eq;
+      const int own = __popcll(up), upto = wave_inscan(own);
+      if (w < WORDS) { above[w] = up; offset[w] = before + upto - own; }
+      eq_before += __builtin_amdgcn_readlane(eq_upto, 63);
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < KPT; ++i) {
+    const unsigned long long w = above[i * WAVES + wave];
+    if (w >> lane & 1) out[offset[i * WAVES + wave] + __popcll(w & ((1ull << lane) - 1))] = i * 64 * WAVES + tid;
+  }
+  for (int e = taken + tid; e < top; e += 64 * WAVES) out[e] = -1;
+}
+
+// ---- attention over the choice
+
+// An item is the query heads of one key head of one row, M of them, over its blocks one behind the other: positions v = 0 .. top page_size - 1 of a list.  They all
+// see the same.  Four waves take every fourth tile of 32; `pieces` workgroups share a long list, sparse_join_kernel adds them up.  Forms of tiles, products and
+// softmax as in the attention over whole caches (attend.hip); what the row does not see is -infinity among the scores and zeros in V.
+constexpr int KT = 32, KW = 4;
+struct Listed { int top, pieces, span; const int32_t* blocks; };        // span: positions of a piece, a multiple of 128
+
+template <int DT, int KEPT, int D, int M> struct Sizes {
+  typedef Form<DT, KEPT, D> F;
+  static constexpr bool CODES = KEPT != DT;
+  static constexpr int TILE = KT * F::ROWB, STAGE = 2 * TILE + (CODES ? 8 * KT : 0), SLOT = D * M * 4 + 512;
+  static constexpr int TILES = KW * 2 * STAGE, JOIN = (KW - 1) * SLOT;
+  static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
+};
+
+template <int DT, int KEPT, int D, int M>
+__global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Attend a, Listed ls, float* __restrict__ part, f32x2_t* __restrict__ stat) {
+  typedef Sizes<DT, KEPT, D, M> Z;
+  typedef Form<DT, KEPT, D> F;
+  constexpr bool CODES = KEPT != DT;
+  constexpr int VDT = CODES ? DT_BF16 : DT;
+  // p (v_scale) in two 16-bit parts, as single tokens of the whole cache have it
+  constexpr bool SPLIT_P = CODES || DT == DT_BF16;
+  typedef Operand<DT, M> P1;
+  typedef Operand<VDT, M> P2;
+  typedef typename P1::vec vec;
+  typedef typename P2::vec vvec;
+  typedef typename P1::acc acc;
+  constexpr int NG = 64 / M, KM = 8 * NG, CA = M * M / 64;
+  constexpr int DM = D / M, KS = D / KM, ST = KT / M, NX = KT / KM;
+  constexpr int TILE = Z::TILE, STAGE = Z::STAGE, LOADS = KT / F::RPI;
+  extern __shared__ __align__(1024) char smem[];
+  __shared__ int list_page[1024], list_block[1024], list_end;
+  const int tid = threadIdx.x, lane = tid & 63, kw = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane / M;
+  const int G = a.heads / c.H, shift = c.page_shift, page_mask = (1 << shift) - 1;
+  const int g = blockIdx.x % c.H, x = blockIdx.x / c.H, t = x % c.T, piece = x / c.T, h0 = blockIdx.y * M;
+  Row row;
+  if (!row_of(c, t, row)) return;
+  const int hi = seen_end(c, row, t - row.row0, a.max_len, a.visible != nullptr);
+  const int always = a.visible ? min(row.old, hi) : hi;                // below this every position is seen
+  const unsigned long long bits = a.visible ? (unsigned long long)a.visible[t] : 0;
+
+  // ---- the piece's blocks
+  const int begin = piece * ls.span, end = min(begin + ls.span, ls.top << shift);
+  const int e0 = begin >> shift, entries = ((end - 1) >> shift) - e0 + 1;
+  if (tid == 0) list_end = 0;
+  __syncthreads();
+  for (int e = tid; e < entries; e += 64 * KW) {
+    const int b = ls.blocks[((long)t * c.H + g) * ls.top + e0 + e];
+    int page = -1;
+    if (b >= 0 && b < c.max_pages && ((long)b << shift) < hi) page = c.pages[(long)row.s * c.max_pages + b];
+    if (page >= c.n_pages) page = -1;
+    list_page[e] = page;
+    list_block[e] = b;
+    if (page >= 0) atomicMax(&list_end, e + 1);
+  }
+  __syncthreads();
+  const int stop = min(end, (e0 + __builtin_amdgcn_readfirstlane(list_end)) << shift);
+  const int count = max(stop - begin + KT - 1, 0) / KT, mine = kw < count ? (count - kw + KW - 1) / KW : 0;
+
+  const int in_tile = lane % M, rg = h0 + in_tile, head = g * G + rg;
+  const bool has = rg < G;
+  const float unit = fmaxf(fabsf(a.scale), 1.2e-38f), c2 = unit * kLog2E;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;             // a negative scale negates the query
+  vec q[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    u32x4_t w = {};
+    if (has) w = *(const u32x4_t*)((const uint16_t*)a.q + t * a.q_pitch + (long)head * D + KM * k + 8 * grp) ^ flip;
+    q[k] = __builtin_bit_cast(vec, w);
+  }
+
+  // ---- tiles into LDS
+  const unsigned base = (unsigned)(uintptr_t)(lds_char*)smem + kw * 2 * STAGE;
+  // 16 positions of the list from v on: their page (-1: nothing there) and block
+  struct Groups { int page[2], block[2]; };
+  auto look_up = [&](int tile) {
+    Groups r;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int v = begin + tile * KT + 16 * u, e = min(v >> shift, (stop - 1) >> shift) - e0;
+      r.page[u] = __builtin_amdgcn_readfirstlane(v < stop ? list_page[e] : -1);
+      r.block[u] = __builtin_amdgcn_readfirstlane(list_block[e]);
+    }
+    return r;
+  };
+  auto fetch = [&](int tile, const Groups& w, int stage) {
+    const unsigned to = base + stage * STAGE;
+    long at[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) at[u] = (((long)max(w.page[u], 0) * c.H + g) << shift) + ((begin + tile * KT + 16 * u) & page_mask);
+    if constexpr (CODES) {
+      const int y = lane & 31;
+      load4_lds(to + 2 * TILE, (lane < 32 ? a.ks : a.vs) + (y < 16 ? at[0] : at[1]) + (y & 15));
+    }
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int x0 = i * F::RPI, xr = (x0 & 15) + lane / F::CH, part_of = (lane % F::CH) ^ F::turn(xr);
+      if (F::PIECES == F::CH || part_of < F::PIECES) {
+        const long where = uniform(at[x0 / 16]);
+        const unsigned off = (unsigned)xr * (D * F::ESZ) + part_of * 16;
+        load16_lds(to + x0 * F::ROWB, (const char*)a.kc + where * (D * F::ESZ), off);
+        load16_lds(to + TILE + x0 * F::ROWB, (const char*)a.vc + where * (D * F::ESZ), off);
+      }
+    }
+  };
+  // bit x: the row sees position x of the tile
+  auto seen_in = [&](int tile, const Groups& w) {
+    uint32_t see = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const long j0 = ((long)w.block[u] << shift) + ((begin + tile * KT + 16 * u) & page_mask);
+      auto below = [](long k) { return k <= 0 ? 0ull : k >= 64 ? ~0ull : (1ull << k) - 1; };
+      unsigned long long m = below(always - j0);
+      if (a.visible && j0 + 16 > row.old) {
+        const long by = row.old - j0;
+        m |= (by >= 64 || by <= -64 ? 0ull : by >= 0 ? bits << by : bits >> -by) & below(hi - j0);
+      }
+      see |= (w.page[u] >= 0 ? (uint32_t)m & 0xFFFFu : 0u) << (16 * u);
+    }
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)see);
+  };
+
+  acc o[DM];
+#pragma unroll
+  for (int d = 0; d < DM; ++d)
+#pragma unroll
+    for (int e = 0; e < CA; ++e) o[d][e] = 0.f;
+  float m = -INFINITY, ref = 0.f, sum = 0.f;
+  bool far = false;
+
+  int kbase[M == 16 ? 2 : 1];
+#pragma unroll
+  for (int b = 0; b < (M == 16 ? 2 : 1); ++b) {
+    const int y = M == 16 ? (lane & 3) | (lane & 12) << 1 | b << 2 : (lane & 3) | (lane & 8) >> 1 | (lane & 4) << 1 | (lane & 16);
+    kbase[b] = y * F::ROWB + (CODES ? ((grp >> 1) ^ F::turn(y)) * 16 + 8 * (grp & 1) : (grp ^ F::turn(y)) * 16);
+  }
+  const int vcol = M == 16 ? 0 : lane >> 4 & 1, vj = lane & 15;
+  int vbase[CODES ? 1 : 2];
+  if constexpr (CODES) {
+    const int y = 8 * grp + vj / 2;
+    vbase[0] = y * F::ROWB + (vcol ^ F::turn(y)) * 16 + 8 * (vj & 1);
+  } else {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int y = 8 * grp + 4 * b + vj / 4;
+      vbase[b] = y * F::ROWB + ((2 * vcol + (vj >> 1 & 1)) ^ F::turn(y)) * 16 + 8 * (vj & 1);
+    }
+  }
+  typedef std::conditional_t<CODES, u32x2_t, u32x4_t> raw_t;
+
+  auto work = [&](uint32_t see, int stage) __attribute__((always_inline)) {
+    const lds_char* const kt = (const lds_char*)(base + stage * STAGE);
+    lds_char* const vt = (lds_char*)(base + stage * STAGE + TILE);
+    const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(base + stage * STAGE + 2 * TILE);
+    const bool partial = see != ~0u;
+    if (partial) {                                                     // 0 * v is NaN where v is not finite
+#pragma unroll
+      for (int i = 0; i < KT * F::CH / 64; ++i) {
+        const int y = (i * 64 + lane) / F::CH;
+        if (!(see >> y & 1)) *(__attribute__((address_space(3))) u32x4_t*)(vt + (i * 64 + lane) * 16) = (u32x4_t){};
+      }
+    }
+    raw_t kf[ST][KS];
+#pragma unroll
+    for (int st = 0; st < ST; ++st)
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        kf[st][k] = *(const __attribute__((address_space(3))) raw_t*)(kt + (M == 16 ? st / 2 : st) * 32 * F::ROWB + (kbase[M == 16 ? st & 1 : 0] ^ k * KM * F::ESZ));
+    __builtin_amdgcn_sched_barrier(0);
+    acc sc[ST];
+#pragma unroll
+    for (int st = 0; st < ST; ++st)
+#pragma unroll
+      for (int e = 0; e < CA; ++e) sc[st][e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int st = 0; st < ST; ++st) {
+        u32x4_t w;
+        if constexpr (CODES) w = widen8<DT, KEPT>(kf[st][k]); else w = kf[st][k];
+        sc[st] = P1::mfma(__builtin_bit_cast(vec, w), q[k], sc[st]);
+      }
+    float z[NX][8];                                                    // position KM x + 8 group + e
+#pragma unroll
+    for (int y = 0; y < NX; ++y)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[y][e] = M == 16 ? sc[2 * y + e / 4][e % 4] : sc[y / 2][8 * (y & 1) + e];
+    if constexpr (CODES) {
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const f32x4_t w = *(const __attribute__((address_space(3))) f32x4_t*)(scales + KM * y + 8 * grp + 4 * f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[y][4 * f + e] *= w[e];
+        }
+    }
+    if (partial) {
+#pragma unroll
+      for (int y = 0; y < NX; ++y) {
+        const uint32_t w = see >> (8 * grp) >> (KM * y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[y][e] = w & (1u << e) ? z[y][e] : -INFINITY;
+      }
+    }
+    float top = z[0][0];
+#pragma unroll
+    for (int y = 0; y < NX; ++y)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, z[y][e]);
+    top = row_max<M>(top);
+    const bool grow = (top - m) * c2 > kSlack;                         // m = -infinity: whenever something is seen
+    if (__any(grow)) {
+      const float next = grow ? top : m;
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - next) * c2);
+      sum *= keep;
+#pragma unroll
+      for (int d = 0; d < DM; ++d)
+#pragma unroll
+        for (int e = 0; e < CA; ++e) o[d][e] *= keep;
+      m = next;
+      ref = m == -INFINITY ? 0.f : m * c2;
+      far = __any(fabsf(ref) > 1e38f);
+    }
+    raw_t vf[2][DM];
+    auto load_v = [&](int y) {
+#pragma unroll
+      for (int d = 0; d < DM; ++d) {
+        if constexpr (CODES) {
+          typedef __attribute__((address_space(3))) i32x2_t L;
+          vf[y & 1][d] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((L*)(vt + y * KM * F::ROWB + (vbase[0] ^ d * M))));
+        } else {
+          typedef __attribute__((address_space(3))) s16x4_t L;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const u32x2_t raw = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(vt + y * KM * F::ROWB + (vbase[b] ^ d * 2 * M))));
+            vf[y & 1][d][2 * b] = raw[0];
+            vf[y & 1][d][2 * b + 1] = raw[1];
+          }
+        }
+      }
+    };
+    load_v(0);
+    if (__builtin_expect(far, 0)) {
+      const float from = m == -INFINITY ? 0.f : m;                     // then all scores are -infinity or NaN: zeros or NaN
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[y][e] = __builtin_amdgcn_exp2f((z[y][e] - from) * c2);
+    } else {
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[y][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[y][e], c2, -ref));
+    }
+    float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int y = 0; y < NX; ++y)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) part_sum[e & 3] += z[y][e];
+    sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+    if constexpr (CODES) {
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const f32x4_t w = *(const __attribute__((address_space(3))) f32x4_t*)(scales + KT + KM * y + 8 * grp + 4 * f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {                                // the scale of a row that is not seen may be anything
+            const bool unseen = partial && !(see >> (8 * grp) >> (KM * y + 4 * f + e) & 1);
+            z[y][4 * f + e] = unseen ? 0.f : z[y][4 * f + e] * w[e];
+          }
+        }
+    }
+    u32x4_t prob[NX], rest[SPLIT_P ? NX : 1];
+#pragma unroll
+    for (int y = 0; y < NX; ++y)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a0 = z[y][2 * e], a1 = z[y][2 * e + 1];
+        if constexpr (SPLIT_P && !CODES) {
+          // cut, not rounded, and the second part a little larger: both are above zero, and an infinity in v times them is one
+          constexpr float more = 1.f + 0x1p-20f;
+          const uint32_t f0 = __float_as_uint(a0) & 0xFFFF0000u, f1 = __float_as_uint(a1) & 0xFFFF0000u;
+          prob[y][e] = f0 >> 16 | f1;
+          rest[y][e] = Half<VDT>::pack(__builtin_fmaf(a0, more, -__uint_as_float(f0)), __builtin_fmaf(a1, more, -__uint_as_float(f1)));
+        } else {
+          prob[y][e] = Half<VDT>::pack(a0, a1);
+          if constexpr (SPLIT_P) rest[y][e] = Half<VDT>::pack(a0 - bf16lo_to_f32(prob[y][e]), a1 - bf16hi_to_f32(prob[y][e]));
+        }
+      }
+#pragma unroll
+    for (int y = 0; y < NX; ++y) {
+      if (y + 1 < NX) load_v(y + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < DM; ++d) {
+        u32x4_t w;
+        if constexpr (CODES) w = widen8<VDT, KEPT>(vf[y & 1][d]); else w = vf[y & 1][d];
+        o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, prob[y]), o[d]);
+        if constexpr (SPLIT_P) o[d] = P2::mfma(__builtin_bit_cast(vvec, w), __builtin_bit_cast(vvec, rest[y]), o[d]);
+      }
+    }
+  };
+
+  if (mine > 0) {
+    Groups now = look_up(kw), next = {};
+    fetch(kw, now, 0);
+    if (mine > 1) next = look_up(kw + KW);
+    for (int i = 0; i < mine; ++i) {
+      const Groups here = now;
+      if (i + 1 < mine) {
+        fetch(kw + (i + 1) * KW, next, (i + 1) & 1);
+        now = next;
+        if (i + 2 < mine) next = look_up(kw + (i + 2) * KW);
+        wait_loads<2 * LOADS + (CODES ? 1 : 0)>();
+      } else {
+        wait_loads<0>();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const uint32_t see = seen_in(kw + i * KW, here);
+      if (see != 0) work(see, i & 1);
+      __builtin_amdgcn_sched_barrier(0);
+      wait_lds();                                                      // nothing reads the stage that is filled next
+    }
+  }
+  sum = row_sum<M>(sum);
+  m *= unit;                                                           // in units of the scores
+
+  // ---- the four waves
+  __syncthreads();
+  if (kw > 0) {
+    char* const to = smem + (kw - 1) * Z::SLOT;
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int b = 0; b < CA / 4; ++b) *(f32x4_t*)(to + (d * (CA / 4) + b) * 1024 + lane * 16) = (f32x4_t){o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+    *(float*)(to + D * M * 4 + lane * 4) = m;
+    *(float*)(to + D * M * 4 + 256 + lane * 4) = sum;
+  }
+  __syncthreads();
+  if (kw > 0) return;
+#pragma unroll
+  for (int w = 0; w < KW - 1; ++w) {
+    const char* const other = smem + w * Z::SLOT;
+    const float m2 = *(const float*)(other + D * M * 4 + lane * 4), s2 = *(const float*)(other + D * M * 4 + 256 + lane * 4);
+    const float top = fmaxf(m, m2), zero = top == -INFINITY ? 0.f : top;
+    const float f1 = __builtin_amdgcn_exp2f((m - zero) * kLog2E), f2 = __builtin_amdgcn_exp2f((m2 - zero) * kLog2E);
+    sum = sum * f1 + s2 * f2;
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int b = 0; b < CA / 4; ++b) {
+        const f32x4_t v = *(const f32x4_t*)(other + (d * (CA / 4) + b) * 1024 + lane * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[d][4 * b + e] = o[d][4 * b + e] * f1 + v[e] * f2;
+      }
+    m = top;
+  }
+  if (!has) return;
+  if (ls.pieces == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t* const out = (uint16_t*)a.out + t * a.out_pitch + (long)head * D;
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int b = 0; b < CA / 4; ++b)
+        *(u32x2_t*)(out + M * d + 8 * b + 4 * grp) = (u32x2_t){Half<DT>::pack(o[d][4 * b] * inv, o[d][4 * b + 1] * inv), Half<DT>::pack(o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv)};
+    if (a.lse && grp == 0) a.lse[(long)t * a.heads + head] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
+  } else {
+    const long to = ((long)t * a.heads + head) * ls.pieces + piece;
+#pragma unroll
+    for (int d = 0; d < DM; ++d)
+#pragma unroll
+      for (int b = 0; b < CA / 4; ++b) *(f32x4_t*)(part + to * D + M * d + 8 * b + 4 * grp) = (f32x4_t){o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+    if (grp == 0) stat[to] = (f32x2_t){m, sum};
+  }
+}
+
+// Adds up the pieces of a row and head, 32 lanes a row, eight pieces on their way at once.
+constexpr int JT = 256;
+template <int DT, int D>
+__global__ __launch_bounds__(JT) void sparse_join_kernel(Paged c, Attend a, int pieces, const float* __restrict__ part, const f32x2_t* __restrict__ stat) {
+  const long row = (long)blockIdx.x * (JT / 32) + threadIdx.x / 32;
+  const int at = threadIdx.x & 31;
+  if (row >= (long)c.T * a.heads) return;
+  const int t = (int)(row / a.heads), head = (int)(row % a.heads);
+  if (t < c.start[0] || t >= c.start[c.S]) return;
+  float m = -INFINITY;
+  for (int k = at; k < pieces; k += 32) m = fmaxf(m, stat[row * pieces + k][0]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float zero = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < pieces; k0 += 8) {
+    f32x2_t st[8];
+    f32x4_t v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const long from = row * pieces + min(k0 + k, pieces - 1);
+      st[k] = stat[from];
+      v[k] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      if (at * 4 < D) v[k] = *(const f32x4_t*)(part + from * D + at * 4);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool has = k0 + k < pieces;
+      const float f = has ? __builtin_amdgcn_exp2f((st[k][0] - zero) * kLog2E) : 0.f;
+      sum += has ? st[k][1] * f : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += has ? v[k][e] * f : 0.f;
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (at * 4 < D)
+    *(u32x2_t*)((uint16_t*)a.out + t * a.out_pitch + (long)head * D + at * 4) = (u32x2_t){Half<DT>::pack(o[0] * inv, o[1] * inv), Half<DT>::pack(o[2] * inv, o[3] * inv)};
+  if (a.lse && at == 0) a.lse[(long)t * a.heads + head] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
+}
+
+// ---- launches
+
+int blocks_of(const Paged& c, int max_len) { return (int)(((long)max_len + (1 << c.page_shift) - 1) >> c.page_shift); }
+int key_pitch(const Paged& c, int max_len) { return (blocks_of(c, max_len) + 63) / 64 * 64; }
+int run_of(int G) {
+  int gp = 1;
+  while (gp < G) gp *= 2;
+  return gp;
+}
+
+struct Pieces { int pieces, span; };
+Pieces pieces_of(const Paged& c, int heads, int top) {
+  const int G = heads / c.H, M = G <= 16 ? 16 : 32;
+  const long items = (long)c.T * c.H * ((G + M - 1) / M), positions = (long)top << c.page_shift;
+  const int slots = c.kept == c.dtype && c.D > 64 ? 256 : 512;        // workgroups at work at once, by their LDS
+  long pieces = 2 * items > slots ? 1 : std::min<long>(slots / items, (positions + 255) / 256);
+  long span = ((positions + pieces - 1) / pieces + 127) / 128 * 128;
+  pieces = (positions + span - 1) / span;
+  return Pieces{(int)pieces, (int)span};
+}
+
+size_t key_bytes(const Paged& c, int max_len, bool given) { return given ? 0 : ((size_t)c.T * c.H * key_pitch(c, max_len) * sizeof(uint32_t) + 255) / 256 * 256; }
+
+template <int DT, int D>
+hipError_t launch_choice(const Paged& c, const Attend& a, const Sparse& sp, uint32_t* keys, hipStream_t stream) {
+  const int nb = blocks_of(c, a.max_len), pitch = key_pitch(c, a.max_len), gp = run_of(a.heads / c.H), chunks = (nb + SCORED - 1) / SCORED;
+  const bool one = gp <= 16 && (long)c.T * gp <= 16l * c.S;            // 16 columns hold the rows of a sequence, in the mean
+  const dim3 grid((unsigned)((long)c.T * c.H * chunks));
+  if (one)
+    hipLaunchKernelGGL((score_kernel<DT, D, 1>), grid, dim3(256), 0, stream, c, a, gp, chunks, pitch, sp.summary, sp.scales, keys);
+  else
+    hipLaunchKernelGGL((score_kernel<DT, D, 4>), grid, dim3(256), 0, stream, c, a, gp, chunks, pitch, sp.summary, sp.scales, keys);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 rows((unsigned)((long)c.T * c.H));
+  const bool tree = a.visible != nullptr;
+  if (nb <= 1024)
+    hipLaunchKernelGGL((choose_kernel<1, 16>), rows, dim3(64), 0, stream, c, a.max_len, tree, sp.top, sp.first, sp.recent, pitch, (const uint32_t*)keys, sp.blocks);
+  else if (nb <= 4096)
+    hipLaunchKernelGGL((choose_kernel<4, 16>), rows, dim3(256), 0, stream, c, a.max_len, tree, sp.top, sp.first, sp.recent, pitch, (const uint32_t*)keys, sp.blocks);
+  else
+    hipLaunchKernelGGL((choose_kernel<16, 32>), rows, dim3(1024), 0, stream, c, a.max_len, tree, sp.top, sp.first, sp.recent, pitch, (const uint32_t*)keys, sp.blocks);
+  return hipGetLastError();
+}
+
+template <int DT, int KEPT, int D, int M>
+hipError_t launch_form(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream) {
+  const Pieces pc = pieces_of(c, a.heads, sp.top);
+  constexpr size_t lds = Sizes<DT, KEPT, D, M>::LDS;
+  static PerDeviceInt raised;
+  hipError_t e = ensure_dynamic_lds(raised, (const void*)sparse_attend_kernel<DT, KEPT, D, M>, lds);
+  if (e != hipSuccess) return e;
+  if (!sp.given && (e = launch_choice<DT, D>(c, a, sp, (uint32_t*)ws, stream)) != hipSuccess) return e;
+  float* part = (float*)((char*)ws + key_bytes(c, a.max_len, sp.given));
+  f32x2_t* stat = (f32x2_t*)(part + (size_t)c.T * a.heads * pc.pieces * D);
+  const Listed ls{sp.top, pc.pieces, pc.span, sp.blocks};
+  const int G = a.heads / c.H;
+  hipLaunchKernelGGL((sparse_attend_kernel<DT, KEPT, D, M>), dim3((unsigned)((long)c.T * c.H * pc.pieces), (G + M - 1) / M), dim3(64 * KW), lds, stream, c, a, ls, part, stat);
+  if ((e = hipGetLastError()) != hipSuccess || pc.pieces == 1) return e;
+  const long rows = (long)c.T * a.heads;
+  hipLaunchKernelGGL((sparse_join_kernel<DT, D>), dim3((unsigned)((rows + JT / 32 - 1) / (JT / 32))), dim3(JT), 0, stream, c, a, pc.pieces, (const float*)part, (const f32x2_t*)stat);
+  return hipGetLastError();
+}
+
+// f(16-bit type, kind of cache, head dimension) with the three as constants
+template <typename F>
+hipError_t with_forms(const Paged& c, F f) {
+  auto dims = [&](auto dt, auto kept) {
+    if (c.D == 64) return f(dt, kept, std::integral_constant<int, 64>{});
+    if (c.D == 96) return f(dt, kept, std::integral_constant<int, 96>{});
+    if (c.D == 128) return f(dt, kept, std::integral_constant<int, 128>{});
+    return hipErrorInvalidValue;
+  };
+  auto kinds = [&](auto dt) {
+    if (c.kept == dt.value) return dims(dt, dt);
+    if (c.kept == DT_I8) return dims(dt, std::integral_constant<int, DT_I8>{});
+    if (c.kept == DT_E4M3) return dims(dt, std::integral_constant<int, DT_E4M3>{});
+    return hipErrorInvalidValue;
+  };
+  if (c.dtype == DT_BF16) return kinds(std::integral_constant<int, DT_BF16>{});
+  if (c.dtype == DT_F16) return kinds(std::integral_constant<int, DT_F16>{});
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t sparse_workspace_bytes(const Paged& c, int heads, int max_len, int top, bool given) {
+  const Pieces pc = pieces_of(c, heads, top);
+  const size_t parts = pc.pieces == 1 ? 0 : (size_t)c.T * heads * pc.pieces * (c.D + 2) * sizeof(float);
+  return std::max<size_t>(key_bytes(c, max_len, given) + parts, 256);
+}
+
+// A launch has fewer than 2^32 threads.
+bool sparse_fits(const Paged& c, int heads, int max_len, int top) {
+  const long nb = blocks_of(c, max_len);
+  if (nb > 32768) return false;
+  const double rows = (double)c.T * c.H;
+  const Pieces pc = pieces_of(c, heads, top);
+  return rows * ((nb + SCORED - 1) / SCORED) * 256 < 4e9 && rows * pc.pieces * 256 < 4e9 && rows * 1024 < 4e9 && (double)c.T * heads * 32 < 4e9;
+}
+
+// Pages that the rows of a call touch, at most, and whether its rows are fewer.
+static long touched_pages(const Paged& c, bool* by_row) {
+  const long touched = ((long)c.T >> c.page_shift) + 2l * c.S;
+  *by_row = c.T <= touched;
+  return std::min<long>(c.T, touched);
+}
+
+bool summary_fits(const Paged& c) {
+  bool by_row;
+  return (double)touched_pages(c, &by_row) * c.H * (c.page_shift >= 8 ? 256 : 64) < 4e9;
+}
+
+hipError_t launch_summary(const Paged& c, const void* kc, const float* ks, int8_t* summary, float* scales, hipStream_t stream) {
+  return with_forms(c, [&](auto dt, auto kept, auto dim) {
+    bool by_row;
+    const long items = touched_pages(c, &by_row) * c.H;
+    const bool large = c.page_shift >= 8;
+    auto go = [&](auto kernel, int per) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, stream, c, items, kc, ks, summary, scales);
+      return hipGetLastError();
+    };
+    if (large && by_row) return go((summary_kernel<dt.value, kept.value, dim.value, 4, true>), 1);
+    if (large) return go((summary_kernel<dt.value, kept.value, dim.value, 4, false>), 1);
+    if (by_row) return go((summary_kernel<dt.value, kept.value, dim.value, 1, true>), 4);
+    return go((summary_kernel<dt.value, kept.value, dim.value, 1, false>), 4);
+  });
+}
+
+hipError_t launch_sparse(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream) {
+  return with_forms(c, [&](auto dt, auto kept, auto dim) {
+    if (a.heads / c.H <= 16) return launch_form<dt.value, kept.value, dim.value, 16>(c, a, sp, ws, stream);
+    return launch_form<dt.value, kept.value, dim.value, 32>(c, a, sp, ws, stream);
+  });
+}
+
+}  // namespace covspec
