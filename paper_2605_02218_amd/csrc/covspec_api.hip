@@ -1037,10 +1037,16 @@ static int sparse_check(const covspec_sparse_params* p, Paged* c) {
   return COVSPEC_OK;
 }
 
+static Sparse sparse_of(const covspec_sparse_params& p) {
+  Sparse sp = {};
+  sp.top = p.top; sp.first = p.first; sp.recent = p.recent; sp.given = p.given != 0;
+  return sp;
+}
+
 size_t covspec_sparse_workspace_size(const covspec_sparse_params* p) {
   Paged c;
   if (sparse_check(p, &c) != COVSPEC_OK) return 0;
-  return sparse_workspace_bytes(c, p->attend.n_heads, p->attend.max_len, p->top, p->given != 0);
+  return sparse_workspace_bytes(c, p->attend.n_heads, p->attend.max_len, sparse_of(*p));
 }
 
 int covspec_sparse_attend(const covspec_sparse_params* p, const void* q, const int32_t* start, const int32_t* length, const int32_t* pages,
@@ -1054,10 +1060,9 @@ int covspec_sparse_attend(const covspec_sparse_params* p, const void* q, const i
   if (!blocks || !workspace || ((uintptr_t)workspace & 255) || ((uintptr_t)visible & 7) || (((uintptr_t)lse_out | (uintptr_t)blocks) & 3)) return COVSPEC_INVALID_ARG;
   if (!p->given && (!summary || !summary_scale || ((uintptr_t)summary & 15) || ((uintptr_t)summary_scale & 3))) return COVSPEC_INVALID_ARG;
   const covspec_attend_params& t = p->attend;
-  if (workspace_bytes < sparse_workspace_bytes(c, t.n_heads, t.max_len, p->top, p->given != 0)) return COVSPEC_WORKSPACE_TOO_SMALL;
+  Sparse sp = sparse_of(*p);
+  if (workspace_bytes < sparse_workspace_bytes(c, t.n_heads, t.max_len, sp)) return COVSPEC_WORKSPACE_TOO_SMALL;
   const Attend a = attend_of(c, t, q, k_cache, v_cache, k_scale, v_scale, visible, out, lse_out);
-  Sparse sp;
-  sp.top = p->top; sp.first = p->first; sp.recent = p->recent; sp.given = p->given != 0;
   sp.summary = (const int8_t*)summary; sp.scales = summary_scale; sp.blocks = blocks;
   discard_pending_error();
   return launched("launch_sparse", launch_sparse(c, a, sp, workspace, (hipStream_t)stream));

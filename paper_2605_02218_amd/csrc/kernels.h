@@ -311,7 +311,7 @@ struct Sparse {
 };
 bool summary_fits(const Paged& c);
 hipError_t launch_summary(const Paged& c, const void* kc, const float* ks, int8_t* summary, float* scales, hipStream_t stream);
-size_t sparse_workspace_bytes(const Paged& c, int heads, int max_len, int top, bool given);
+size_t sparse_workspace_bytes(const Paged& c, int heads, int max_len, const Sparse& sp);
 bool sparse_fits(const Paged& c, int heads, int max_len, int top);
 hipError_t launch_sparse(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream);
 

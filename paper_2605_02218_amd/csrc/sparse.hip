@@ -16,16 +16,27 @@ namespace {
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
-// Rows and lengths as covspec_attend takes them.  t uniform in the wave; false: a padding row.
+// Rows and lengths as covspec_attend takes them.  t uniform in the wave; false: a padding row.  Starts and lengths of 64 sequences come at once, so that a row of
+// the first 63 takes one load's time.
 struct Row { int s, row0, n, old; };
 __device__ __forceinline__ bool row_of(const Paged& c, int t, Row& r) {
-  r.s = seq_of_wave<1>(c.start, c.S, t);
-  if (t >= c.T || r.s < 0 || r.s >= c.S) return false;
-  r.s = __builtin_amdgcn_readfirstlane(r.s);
-  r.row0 = min(max(c.start[r.s], 0), c.T);
-  r.n = max(min(c.start[r.s + 1], c.T), r.row0) - r.row0;
-  r.old = (int)max((long)c.length[r.s] - r.n, -(1l << 30));
-  return true;
+  const int lane = threadIdx.x & 63;
+  if (t >= c.T) return false;
+  for (int s0 = c.S > 1024 ? max(seq_of(c.start, c.S, t), 0) & ~63 : 0; s0 < c.S; s0 += 64) {
+    const int start = s0 + lane <= c.S ? c.start[s0 + lane] : 0x7FFFFFFF, len = c.length[min(s0 + lane, c.S - 1)];
+    const int at = __popcll(__ballot(start <= t)) - 1;                  // the last one that begins at or in front of t, if it lies here
+    if (at < 0) return false;
+    const bool last = at == 63;
+    if (last && s0 + 64 <= c.S && c.start[s0 + 64] <= t) continue;
+    r.s = s0 + at;
+    if (r.s >= c.S) return false;
+    r.row0 = min(max(__builtin_amdgcn_readlane(start, at), 0), c.T);
+    const int end = last ? c.start[r.s + 1] : __builtin_amdgcn_readlane(start, at + 1);
+    r.n = max(min(end, c.T), r.row0) - r.row0;
+    r.old = (int)max((long)__builtin_amdgcn_readlane(len, at) - r.n, -(1l << 30));
+    return true;
+  }
+  return false;
 }
 // End of what row i of the chunk sees.
 __device__ __forceinline__ int seen_end(const Paged& c, const Row& r, int i, int max_len, bool tree) {
@@ -42,6 +53,14 @@ template <int DT, int KEPT, int D> struct Piece {
   static constexpr int LANES = D / N <= 4 ? 4 : D / N <= 8 ? 8 : 16;       // of a row; head dimension 96 leaves a quarter without work
 };
 
+// Over the lanes that are `LANES` apart.
+template <int LANES, typename F>
+__device__ __forceinline__ float over_rows(float x, F f) {
+  if constexpr (LANES <= 4) x = f(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x124, 0xf, 0xf, true)));      // row_ror 4
+  if constexpr (LANES <= 8) x = f(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, true)));      // row_ror 8
+  return over_groups<16>(x, f);
+}
+
 // A wave takes a page of a key head, or (WAVES = 4) a workgroup a large one.  BY_ROW: an item is a row, the first of its sequence's on the page does the work;
 // else items are the pages that each sequence's rows touch, one sequence behind the other.
 template <int DT, int KEPT, int D, int WAVES, bool BY_ROW>
@@ -55,24 +74,26 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
   if (item >= items) return;
   const int x = (int)(item / c.H), g = (int)(item % c.H);
   const int shift = c.page_shift, cap = c.max_pages << shift;
-  int s = -1, block = 0;
+  int s = -1, block = 0, len = 0;
   if constexpr (BY_ROW) {
     Row r;
     if (!row_of(c, x, r)) return;
-    const long pos = (long)c.length[r.s] - c.start[r.s + 1] + x;
-    if (pos < 0 || pos >= cap || (x != c.start[r.s] && (pos & ((1 << shift) - 1)) != 0)) return;
+    const long pos = (long)r.old + (x - r.row0);
+    if (pos < 0 || pos >= cap || (x != r.row0 && (pos & ((1 << shift) - 1)) != 0)) return;
     s = r.s;
     block = (int)(pos >> shift);
+    len = r.old + r.n;
   } else {
     int left = x;
     for (int s0 = 0; s0 < c.S && s < 0; s0 += 64) {
-      const int mine = min(s0 + lane, c.S - 1), row0 = min(max(c.start[mine], 0), c.T), n = max(min(c.start[mine + 1], c.T), row0) - row0, len = c.length[mine];
-      const int lo = max(len - n, 0), hi = min(len, cap);
+      const int mine = min(s0 + lane, c.S - 1), row0 = min(max(c.start[mine], 0), c.T), n = max(min(c.start[mine + 1], c.T), row0) - row0, length = c.length[mine];
+      const int lo = max(length - n, 0), hi = min(length, cap);
       const int own = s0 + lane < c.S && n > 0 && lo < hi ? ((hi - 1) >> shift) - (lo >> shift) + 1 : 0, upto = wave_inscan(own);
       const unsigned long long over = __ballot(upto > left);
       if (over) {
         const int at = __ffsll((long long)over) - 1;
         s = s0 + at;
+        len = __builtin_amdgcn_readlane(length, at);
         block = (__builtin_amdgcn_readlane(lo, at) >> shift) + left - __builtin_amdgcn_readlane(upto, at) + __builtin_amdgcn_readlane(own, at);
       }
       left -= __builtin_amdgcn_readlane(upto, 63);
@@ -81,7 +102,7 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
   }
   const int page = c.pages[(long)s * c.max_pages + block];
   if (page < 0 || page >= c.n_pages) return;
-  const int count = min(min(c.length[s], cap) - (block << shift), 1 << shift);          // positions of the page: at least one, if `start` ascends
+  const int count = min(min(len, cap) - (block << shift), 1 << shift);          // positions of the page: at least one, if `start` ascends
   if (count < 1) return;
   const long first = ((long)page * c.H + g) << shift;
   const int piece = lane % LANES, row = lane / LANES;
@@ -128,14 +149,11 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
     }
   }
 #pragma unroll
-  for (int o = LANES; o < 64; o <<= 1)
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      top[e] = fmaxf(top[e], __shfl_xor(top[e], o, 64));
-      low[e] = fminf(low[e], __shfl_xor(low[e], o, 64));
-    }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) size = max(size, (uint32_t)__shfl_xor((int)size, o, 64));
+  for (int e = 0; e < N; ++e) {
+    top[e] = over_rows<LANES>(top[e], [](float x, float y) { return fmaxf(x, y); });
+    low[e] = over_rows<LANES>(low[e], [](float x, float y) { return fminf(x, y); });
+  }
+  size = wave_max(size);
   if constexpr (WAVES > 1) {
     if (row == 0 && piece * N < D) {
 #pragma unroll
@@ -174,10 +192,11 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
 
 // ---- scores
 
-// A score as an integer of the same order; NaN above all others; 0 is left for blocks that are not there.
-__device__ __forceinline__ uint32_t score_key(float f) { return f != f ? 0xFFFFFFFFu : float_order_key(f); }
+// A score as an integer of the same order; NaN above all others; 0 is left for blocks that are not there, the largest for those that are always taken.
+constexpr uint32_t kAlways = 0xFFFFFFFFu;
+__device__ __forceinline__ uint32_t score_key(float f) { return f != f ? kAlways - 1 : float_order_key(f); }
 
-// Largest over runs of GP lanes, GP a power of two up to 16.
+// Largest over runs of gp lanes, a power of two up to 16.
 __device__ __forceinline__ uint32_t run_max(uint32_t v, int gp) {
   if (gp >= 2) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));        // quad_perm 1 0 3 2
   if (gp >= 4) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));        // quad_perm 2 3 0 1
@@ -186,55 +205,33 @@ __device__ __forceinline__ uint32_t run_max(uint32_t v, int gp) {
   return v;
 }
 
-// Blocks are rows of the product, 16 at a time, (token, query head) its columns, 16 NT for a wave: gp columns a token, its heads and then none.
-// A wave takes 64 blocks, all their summaries on their way before the first product.
-constexpr int SCORED = 256;                       // blocks of a workgroup
-template <int DT, int D, int NT>
-__global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, int chunks, int pitch, const int8_t* __restrict__ summary,
-                                                    const float* __restrict__ scales, uint32_t* __restrict__ keys) {
-  constexpr int STEPS = 2 * D / 64;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
-  const int G = a.heads / c.H, tokens = 16 * NT / gp;
-  const long item = blockIdx.x / c.H;
-  const int g = blockIdx.x % c.H, t0 = (int)(item / chunks), chunk = (int)(item % chunks);
-  Row r;
-  if (!row_of(c, t0, r)) return;
-  const int i0 = t0 - r.row0;
-  if (i0 % tokens != 0) return;                   // the first row of `tokens` does the work
-  const int i1 = min(i0 + tokens, r.n);
-  const int nb = blocks_up_to(c, seen_end(c, r, i1 - 1, a.max_len, a.visible != nullptr));
-  const int b0 = chunk * SCORED + wave * 64;
-  if (b0 >= nb) return;
-  const int b = b0 + lane;
-  int id = b < nb ? c.pages[(long)r.s * c.max_pages + b] : -1;
-  const bool there = id >= 0 && id < c.n_pages;
-  id = there ? id : 0;
-  const float scale = scales[(long)id * c.H + g];
-  const unsigned long long exists = __ballot(there);
-  i32x4_t m[4][STEPS];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const long from = ((long)__shfl(id, 16 * j + col, 64) * c.H + g) * 2 * D + 16 * quad;
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k) m[j][k] = *(const i32x4_t*)(summary + from + 64 * k);
-  }
-  // the queries' codes
-  i32x4_t q[NT][STEPS];
-  float qs[NT];
+// Blocks are rows of the product, 16 at a time, (token, query head) its columns; the terms are max(c, 0) largest, then min(c, 0) smallest, 64 a step.  A lane has
+// column lane % 16 of a product and 16 neighbouring terms of each step.
+template <int D> constexpr int kSteps = 2 * D / 64;
+
+template <int D, int NT> struct Codes {
+  i32x4_t q[NT][kSteps<D>];
+  float scale[NT];
   bool real[NT];
+};
+// from(n): the query of the lane's column 16 n + lane % 16, or null
+template <int DT, int D, int NT, typename F>
+__device__ __forceinline__ void query_codes(F from, Codes<D, NT>& r) {
+  constexpr int STEPS = kSteps<D>, OWN = D == 96 ? STEPS : STEPS / 2;  // a lane's terms below and above zero are the same elements but for D = 96
+  const int quad = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int x = 16 * n + col, i = i0 + x / gp, h = x % gp;
-    real[n] = i < i1 && h < G;
-    u32x4_t raw[STEPS][2];
+    const uint16_t* const x = from(n);
+    r.real[n] = x != nullptr;
+    u32x4_t raw[OWN][2];
     uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
+    for (int k = 0; k < OWN; ++k) {
       const int k0 = 64 * k + 16 * quad, d = k0 >= D ? k0 - D : k0;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         raw[k][p] = (u32x4_t){};
-        if (real[n]) raw[k][p] = *(const u32x4_t*)((const uint16_t*)a.q + (long)(r.row0 + i) * a.q_pitch + (long)(g * G + h) * D + d + 8 * p);
+        if (x) raw[k][p] = *(const u32x4_t*)(x + d + 8 * p);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const f32x2_t f = Half<DT>::unpack(raw[k][p][e]);
@@ -245,38 +242,67 @@ __global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, i
     top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
     float inv;
-    const bool finite = code_step<DT_I8>(top, inv, qs[n]);
+    const bool finite = code_step<DT_I8>(top, inv, r.scale[n]);
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-      const bool neg = 64 * k + 16 * quad >= D;
+    for (int k = 0; k < OWN; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const f32x2_t f = Half<DT>::unpack(raw[k][w / 2][2 * (w & 1) + e]);
-          y[2 * e] = neg ? fminf(f[0], 0.f) : fmaxf(f[0], 0.f);
-          y[2 * e + 1] = neg ? fminf(f[1], 0.f) : fmaxf(f[1], 0.f);
+        const f32x2_t f0 = Half<DT>::unpack(raw[k][w / 2][2 * (w & 1)]), f1 = Half<DT>::unpack(raw[k][w / 2][2 * (w & 1) + 1]);
+        const float y[4] = {f0[0], f0[1], f1[0], f1[1]};
+        const uint32_t code = encode_row4<DT_I8>(y, inv, finite), below = (code >> 7 & 0x01010101u) * 0xFFu;      // bytes of codes below zero
+        if constexpr (D == 96) {
+          r.q[n][k][w] = (int)(64 * k + 16 * quad >= D ? code & below : code & ~below);
+        } else {
+          r.q[n][k][w] = (int)(code & ~below);
+          r.q[n][k + OWN][w] = (int)(code & below);
         }
-        q[n][k][w] = (int)encode_row4<DT_I8>(y, inv, finite);
       }
-    }
   }
+}
+
+// 64 blocks of a sequence, block b0 + lane in a lane: on their way, then their scores.
+template <int D> struct Scored {
+  i32x4_t m[4][kSteps<D>];
+  float scale;
+  unsigned long long exists;
+};
+__device__ __forceinline__ int block_id(const Paged& c, int s, int b, int nb) { return b < nb ? c.pages[(long)s * c.max_pages + b] : -1; }
+template <int D>
+__device__ __forceinline__ void load_blocks(const Paged& c, int g, const int8_t* summary, const float* scales, int id, Scored<D>& r) {
+  const int lane = threadIdx.x & 63;
+  const bool there = id >= 0 && id < c.n_pages;
+  id = there ? id : 0;
+  r.exists = __ballot(there);
+  r.scale = scales[(long)id * c.H + g];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const long from = ((long)__shfl(id, 16 * j + (lane & 15), 64) * c.H + g) * 2 * D + 16 * (lane >> 4);
+#pragma unroll
+    for (int k = 0; k < kSteps<D>; ++k) r.m[j][k] = *(const i32x4_t*)(summary + from + 64 * k);
+  }
+}
+// put(n, j, keys): keys of blocks 16 j + 4 (lane / 16) + 0 .. 3 for the token whose first column is 16 n + lane % 16, in those lanes; gp columns a token, `columns` in all
+template <int D, int NT, typename F>
+__device__ __forceinline__ void score_blocks(const Scored<D>& b, const Codes<D, NT>& q, int gp, int columns, F put) {
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     float ksc[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) ksc[e] = __shfl(scale, 16 * j + 4 * quad + e, 64);
+    for (int e = 0; e < 4; ++e) ksc[e] = __shfl(b.scale, 16 * j + 4 * quad + e, 64);
     uint32_t best[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) best[n][e] = 0;
+      if (16 * n >= columns) continue;
       i32x4_t acc = {0, 0, 0, 0};
 #pragma unroll
-      for (int k = 0; k < STEPS; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(m[j][k], q[n][k], acc, 0, 0, 0);
+      for (int k = 0; k < kSteps<D>; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b.m[j][k], q.q[n][k], acc, 0, 0, 0);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool ok = real[n] && (exists >> (16 * j + 4 * quad + e) & 1);
-        best[n][e] = run_max(ok ? score_key(__fmul_rn(__fmul_rn((float)acc[e], ksc[e]), qs[n])) : 0u, min(gp, 16));
+        const bool ok = q.real[n] && (b.exists >> (16 * j + 4 * quad + e) & 1);
+        best[n][e] = run_max(ok ? score_key(__fmul_rn(__fmul_rn((float)acc[e], ksc[e]), q.scale[n])) : 0u, min(gp, 16));
       }
     }
 #pragma unroll
@@ -290,117 +316,226 @@ __global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, i
 #pragma unroll
             for (int e = 0; e < 4; ++e) best[n][e] = max(best[n][e], best[n + o][e]);
       }
-      const int x = 16 * n + col, i = i0 + x / gp;
-      if (x % gp == 0 && i < i1)
-        *(u32x4_t*)(keys + ((long)(r.row0 + i) * c.H + g) * pitch + b0 + 16 * j + 4 * quad) = (u32x4_t){best[n][0], best[n][1], best[n][2], best[n][3]};
+      if ((16 * n + col) % gp == 0) put(n, j, (u32x4_t){best[n][0], best[n][1], best[n][2], best[n][3]});
     }
   }
 }
 
+// Scores of few rows, their blocks spread over the device: a workgroup takes 256 blocks for as many tokens of a sequence as 16 NT columns hold.
+constexpr int SCORED = 256;
+template <int DT, int D, int NT>
+__global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, int chunks, int pitch, const int8_t* __restrict__ summary,
+                                                    const float* __restrict__ scales, uint32_t* __restrict__ keys) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.heads / c.H, tokens = 16 * NT / gp;
+  const long item = blockIdx.x / c.H;
+  const int g = blockIdx.x % c.H, chunk = (int)(item % chunks);
+  // groups of `tokens` rows of a sequence, one sequence behind the other
+  int left = (int)(item / chunks), s = -1, row0 = 0, n = 0, len = 0, i0 = 0;
+  for (int s0 = 0; s0 < c.S && s < 0; s0 += 64) {
+    const int mine = min(s0 + lane, c.S - 1), first = min(max(c.start[mine], 0), c.T), rows = max(min(c.start[mine + 1], c.T), first) - first, length = c.length[mine];
+    const int own = s0 + lane < c.S ? (rows + tokens - 1) / tokens : 0, upto = wave_inscan(own);
+    const unsigned long long over = __ballot(upto > left);
+    if (over) {
+      const int at = __ffsll((long long)over) - 1;
+      s = s0 + at;
+      row0 = __builtin_amdgcn_readlane(first, at);
+      n = __builtin_amdgcn_readlane(rows, at);
+      len = __builtin_amdgcn_readlane(length, at);
+      i0 = (left - __builtin_amdgcn_readlane(upto, at) + __builtin_amdgcn_readlane(own, at)) * tokens;
+    }
+    left -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (s < 0) return;
+  const Row r = {s, row0, n, (int)max((long)len - n, -(1l << 30))};
+  const int i1 = min(i0 + tokens, n), nb = blocks_up_to(c, seen_end(c, r, i1 - 1, a.max_len, a.visible != nullptr)), b0 = chunk * SCORED + wave * 64;
+  if (b0 >= nb) return;
+  Scored<D> b;
+  load_blocks<D>(c, g, summary, scales, block_id(c, s, b0 + lane, nb), b);
+  Codes<D, NT> q;
+  query_codes<DT, D, NT>([&](int y) -> const uint16_t* {
+    const int x = 16 * y + (lane & 15), i = i0 + x / gp, h = x % gp;
+    return i < i1 && h < G ? (const uint16_t*)a.q + (long)(row0 + i) * a.q_pitch + (long)(g * G + h) * D : nullptr;
+  }, q);
+  score_blocks<D, NT>(b, q, gp, (i1 - i0) * gp, [&](int y, int j, u32x4_t key) {
+    const int i = i0 + (16 * y + (lane & 15)) / gp;
+    if (i < i1) *(u32x4_t*)(keys + ((long)(row0 + i) * c.H + g) * pitch + b0 + 16 * j + 4 * (lane >> 4)) = key;
+  });
+}
+
 // ---- the choice
 
-// One workgroup for a row and key head, KPT blocks a thread in registers: the top-th largest key by halving its range, two bits at a time, then the blocks above
-// it and the first ones at it, in order.
-template <int WAVES, int KPT>
-__global__ __launch_bounds__(64 * WAVES) void choose_kernel(Paged c, int max_len, bool tree, int top, int first, int recent, int pitch,
-                                                            const uint32_t* __restrict__ keys, int32_t* __restrict__ blocks) {
-  constexpr int WORDS = WAVES * KPT;
-  __shared__ unsigned long long above[WORDS], equal[WORDS];
-  __shared__ int offset[WORDS], counts[2][3][WAVES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+// The keys of a row's blocks lie in LDS, `count` of them with zeros behind the last up to a multiple of 256; a lane takes four neighbours.  The key that parts those
+// taken from the others is found by counting keys in 1024 equal parts of the range where it must lie, then in the part that holds it, at most four times, twice as
+// a rule; then the blocks above it and the first ones at it, in order.
+constexpr int BINS = 1024, PASSES = 4, GROUPS = 128;       // 256 neighbouring blocks a group
+struct ChoiceLds {
+  int bins[PASSES][BINS];
+  int above[GROUPS], equal[GROUPS];
+  int counts[16][4];
+};
+template <int THREADS>
+__device__ __forceinline__ void clear_bins(ChoiceLds& l) {
+  for (int i = threadIdx.x; i < PASSES * BINS / 4; i += THREADS) ((i32x4_t*)l.bins)[i] = (i32x4_t){0, 0, 0, 0};
+}
+// Blocks taken, ascending, through put(place, block); their number is returned.  All threads.
+template <int THREADS, typename F>
+__device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, ChoiceLds& l, F put) {
+  constexpr int WAVES = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), groups = count >> 8;
+  const u32x4_t* const mine = (const u32x4_t*)keys + lane;             // of group x: mine[64 x]
+  uint32_t lo = kAlways, hi = 0;
+  int always = 0, there = 0;
+  for (int x = wave; x < groups; x += WAVES) {
+    const u32x4_t k = mine[64 * x];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      always += k[e] == kAlways;
+      there += k[e] != 0;
+      if (k[e] != 0 && k[e] != kAlways) { lo = min(lo, k[e]); hi = max(hi, k[e]); }
+    }
+  }
+  always = __builtin_amdgcn_readlane(wave_inscan(always), 63);
+  there = __builtin_amdgcn_readlane(wave_inscan(there), 63);
+  lo = wave_min(lo);
+  hi = wave_max(hi);
+  if (lane == 0) { l.counts[wave][0] = always; l.counts[wave][1] = there; l.counts[wave][2] = (int)lo; l.counts[wave][3] = (int)hi; }
+  __syncthreads();
+  always = there = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const i32x4_t v = *(const i32x4_t*)l.counts[w];
+    always += v[0];
+    there += v[1];
+    lo = min(lo, (uint32_t)v[2]);
+    hi = max(hi, (uint32_t)v[3]);
+  }
+  uint32_t at = 0;                                // all above it are taken, and `more` of those at it
+  int more = 0, need = top - always;
+  if (there - always > need) {
+    at = kAlways - 1;
+    for (int pass = 0; need > 0; ++pass) {
+      const uint32_t width = hi - lo;
+      if (width == 0) { at = lo; more = need; break; }
+      const int shift = max(0, 22 - __builtin_clz(width));             // of 32 - clz bits ten count
+      for (int x = wave; x < groups; x += WAVES) {
+        const u32x4_t k = mine[64 * x];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (k[e] >= lo && k[e] <= hi) atomicAdd(&l.bins[pass][(k[e] - lo) >> shift], 1);
+      }
+      __syncthreads();
+      int own[16], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const i32x4_t v = ((const i32x4_t*)l.bins[pass])[lane * 4 + i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { own[4 * i + e] = v[e]; sum += v[e]; }
+      }
+      const int upto = wave_inscan(sum), over = __builtin_amdgcn_readlane(upto, 63) - upto;      // keys in the parts of later lanes
+      int bin = -1, before = over, here = 0;
+#pragma unroll
+      for (int i = 15; i >= 0; --i)
+        if (bin < 0) {
+          if (before + own[i] >= need) { bin = 16 * lane + i; here = own[i]; }
+          else before += own[i];
+        }
+      const unsigned long long who = __ballot(over < need && bin >= 0);
+      const int from = 63 - __builtin_clzll(who);                      // one lane
+      bin = __builtin_amdgcn_readlane(bin, from);
+      before = __builtin_amdgcn_readlane(before, from);
+      here = __builtin_amdgcn_readlane(here, from);
+      need -= before;
+      lo += (uint32_t)bin << shift;
+      hi = min(hi, lo + ((1u << shift) - 1));
+      if (need == here) { at = lo - 1; break; }
+    }
+  }
+  // in order
+  const bool ties = at != 0 && more > 0;
+  for (int x = wave; x < groups; x += WAVES) {
+    const u32x4_t k = mine[64 * x];
+    int up = 0, eq = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      up += __popcll(__ballot(k[e] > at));
+      eq += __popcll(__ballot(ties && k[e] == at));
+    }
+    if (lane == 0) { l.above[x] = up; l.equal[x] = eq; }
+  }
+  __syncthreads();
+  int up_before = 0, eq_before = 0;               // in front of the 64 groups at hand
+  for (int x0 = 0; x0 < groups; x0 += 64) {
+    const int up = x0 + lane < groups ? l.above[x0 + lane] : 0, eq = x0 + lane < groups ? l.equal[x0 + lane] : 0;
+    const int up_upto = wave_inscan(up), eq_upto = wave_inscan(eq);
+    for (int i = wave; i < 64 && x0 + i < groups; i += WAVES) {
+      const u32x4_t k = mine[64 * (x0 + i)];
+      const int ups = up_before + __builtin_amdgcn_readlane(up_upto - up, i), eqs = eq_before + __builtin_amdgcn_readlane(eq_upto - eq, i);
+      const unsigned long long below = (1ull << lane) - 1;
+      int before_up = ups, before_eq = eqs;       // in front of the lane's four
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        before_up += __popcll(__ballot(k[e] > at) & below);
+        if (ties) before_eq += __popcll(__ballot(k[e] == at) & below);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool is_up = k[e] > at, is_eq = ties && k[e] == at;
+        if (is_up || (is_eq && before_eq < more)) put(before_up + min(before_eq, more), ((x0 + i) * 64 + lane) * 4 + e);
+        before_up += is_up;
+        before_eq += is_eq;
+      }
+    }
+    up_before += __builtin_amdgcn_readlane(up_upto, 63);
+    eq_before += __builtin_amdgcn_readlane(eq_upto, 63);
+  }
+  return up_before + min(eq_before, more);
+}
+
+// Key of block b of nb as the choice takes it.
+__device__ __forceinline__ uint32_t key_of(const Sparse& sp, int nb, int b, uint32_t k) { return b >= nb ? 0u : b < sp.first || b >= nb - sp.recent ? kAlways : k; }
+// A row's scores of an earlier launch into LDS.
+template <int THREADS>
+__device__ __forceinline__ void take_scores(const Sparse& sp, const uint32_t* scored, int nb, int count, uint32_t* keys) {
+  for (int b = 4 * threadIdx.x; b < count; b += 4 * THREADS) {
+    u32x4_t k = {0, 0, 0, 0};
+    if (b < nb) k = *(const u32x4_t*)(scored + b);                     // their pitch is a multiple of 64
+    *(u32x4_t*)(keys + b) = (u32x4_t){key_of(sp, nb, b, k[0]), key_of(sp, nb, b + 1, k[1]), key_of(sp, nb, b + 2, k[2]), key_of(sp, nb, b + 3, k[3])};
+  }
+}
+size_t choice_lds(int blocks) { return sizeof(ChoiceLds) + ((size_t)blocks + 255) / 256 * 256 * sizeof(uint32_t); }
+
+// A workgroup for each row and key head, where there are so many blocks that several workgroups of the attention should not choose among them.
+constexpr int CHOOSERS = 1024;
+__global__ __launch_bounds__(CHOOSERS) void choose_kernel(Paged c, int max_len, bool tree, Sparse sp, int pitch, const uint32_t* __restrict__ keys) {
+  extern __shared__ __align__(1024) char smem[];
   const int t = blockIdx.x / c.H;
   Row r;
   if (!row_of(c, t, r)) return;
-  const int nb = blocks_up_to(c, seen_end(c, r, t - r.row0, max_len, tree));
-  const uint32_t* const mine = keys + (long)blockIdx.x * pitch;
-  int32_t* const out = blocks + (long)blockIdx.x * top;
-  uint32_t key[KPT];
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const int b = i * 64 * WAVES + tid;
-    key[i] = 0;
-    if (b < nb) key[i] = b < first || b >= nb - recent ? 0xFFFFFFFFu : min(mine[b], 0xFFFFFFFEu);
-  }
-  int turn = 0;
-  // how many keys are at least x[0], x[1], x[2]
-  auto count3 = [&](const uint32_t (&x)[3], int (&n)[3]) {
-#pragma unroll
-    for (int w = 0; w < 3; ++w) n[w] = 0;
-#pragma unroll
-    for (int i = 0; i < KPT; ++i)
-#pragma unroll
-      for (int w = 0; w < 3; ++w) n[w] += __popcll(__ballot(key[i] >= x[w]));
-    if constexpr (WAVES > 1) {
-      if (lane < 3) counts[turn][lane][wave] = lane == 0 ? n[0] : lane == 1 ? n[1] : n[2];
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < 3; ++w) {
-        n[w] = 0;
-#pragma unroll
-        for (int k = 0; k < WAVES; ++k) n[w] += counts[turn][w][k];
-      }
-      turn ^= 1;
-    }
-  };
-  uint32_t at = 1;                                // the key of the last one taken
-  int n[3], taken, more;                          // taken: blocks in all; more: of them at `at` itself
-  {
-    const uint32_t x[3] = {1u, 1u, 1u};
-    count3(x, n);
-  }
-  taken = min(n[0], top);
-  if (n[0] > top) {
-    at = 0;
-    for (int shift = 30; shift >= 0; shift -= 2) {
-      const uint32_t x[3] = {at | 1u << shift, at | 2u << shift, at | 3u << shift};
-      count3(x, n);
-      at = n[2] >= top ? x[2] : n[1] >= top ? x[1] : n[0] >= top ? x[0] : at;
-    }
-    const uint32_t x[3] = {at == 0xFFFFFFFFu ? at : at + 1, 0xFFFFFFFFu, 0xFFFFFFFFu};
-    count3(x, n);
-    more = top - (at == 0xFFFFFFFFu ? 0 : n[0]);
-  } else {
-    more = 0;
-    at = 0;
-  }
-  // in order: word i WAVES + wave holds 64 neighbouring blocks
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const unsigned long long up = __ballot(key[i] > at), eq = __ballot(at != 0 && key[i] == at);
-    if (lane == 0) { above[i * WAVES + wave] = up; equal[i * WAVES + wave] = eq; }
-  }
+  const int nb = blocks_up_to(c, seen_end(c, r, t - r.row0, max_len, tree)), count = (nb + 255) & ~255;
+  ChoiceLds& choice = *(ChoiceLds*)smem;
+  uint32_t* const lds_keys = (uint32_t*)(smem + sizeof(ChoiceLds));
+  int32_t* const list = sp.blocks + (long)blockIdx.x * sp.top;
+  clear_bins<CHOOSERS>(choice);
+  take_scores<CHOOSERS>(sp, keys + (long)blockIdx.x * pitch, nb, count, lds_keys);
   __syncthreads();
-  if (wave == 0) {
-    int eq_before = 0, before = 0;
-    for (int w0 = 0; w0 < WORDS; w0 += 64) {
-      const int w = w0 + lane;
-      unsigned long long up = w < WORDS ? above[w] : 0, eq = w < WORDS ? equal[w] : 0;
-      const int eqs = __popcll(eq), eq_upto = wave_inscan(eqs);
-      int room = min(max(more - (eq_before + eq_upto - eqs), 0), eqs);
-      for (int k = eqs; k > room; --k) eq &= ~(1ull << (63 - __builtin_clzll(eq)));
-      up |= eq;
-      const int own = __popcll(up), upto = wave_inscan(own);
-      if (w < WORDS) { above[w] = up; offset[w] = before + upto - own; }
-      eq_before += __builtin_amdgcn_readlane(eq_upto, 63);
-      before += __builtin_amdgcn_readlane(upto, 63);
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const unsigned long long w = above[i * WAVES + wave];
-    if (w >> lane & 1) out[offset[i * WAVES + wave] + __popcll(w & ((1ull << lane) - 1))] = i * 64 * WAVES + tid;
-  }
-  for (int e = taken + tid; e < top; e += 64 * WAVES) out[e] = -1;
+  const int taken = choose<CHOOSERS>(lds_keys, count, sp.top, choice, [&](int at, int b) { list[at] = b; });
+  for (int e = taken + (int)threadIdx.x; e < sp.top; e += CHOOSERS) list[e] = -1;
 }
 
 // ---- attention over the choice
 
 // An item is the query heads of one key head of one row, M of them, over its blocks one behind the other: positions v = 0 .. top page_size - 1 of a list.  They all
-// see the same.  Four waves take every fourth tile of 32; `pieces` workgroups share a long list, sparse_join_kernel adds them up.  Forms of tiles, products and
+// see the same.  The list is the caller's (GIVEN), or chosen first: by scores of an earlier launch (SCORES), or by the workgroup's own (WHOLE), for whom keys and values
+// of the choice and all summaries are read at once.  Four waves take every fourth tile of 32; `pieces` workgroups share a long list, sparse_join_kernel adds them up.  Forms of tiles, products and
 // softmax as in the attention over whole caches (attend.hip); what the row does not see is -infinity among the scores and zeros in V.
 constexpr int KT = 32, KW = 4;
-struct Listed { int top, pieces, span; const int32_t* blocks; };        // span: positions of a piece, a multiple of 128
+enum { GIVEN, SCORES, WHOLE };
+struct Listed {
+  int pieces, span;                    // span: positions of a piece, a multiple of 128
+  int from, pitch;                     // from: GIVEN, SCORES, WHOLE; pitch: of the scores of an item
+  const uint32_t* keys;
+};
 
 template <int DT, int KEPT, int D, int M> struct Sizes {
   typedef Form<DT, KEPT, D> F;
@@ -411,7 +546,7 @@ template <int DT, int KEPT, int D, int M> struct Sizes {
 };
 
 template <int DT, int KEPT, int D, int M>
-__global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Attend a, Listed ls, float* __restrict__ part, f32x2_t* __restrict__ stat) {
+__global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Attend a, Sparse sp, Listed ls, float* __restrict__ part, f32x2_t* __restrict__ stat) {
   typedef Sizes<DT, KEPT, D, M> Z;
   typedef Form<DT, KEPT, D> F;
   constexpr bool CODES = KEPT != DT;
@@ -438,17 +573,63 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   const unsigned long long bits = a.visible ? (unsigned long long)a.visible[t] : 0;
 
   // ---- the piece's blocks
-  const int begin = piece * ls.span, end = min(begin + ls.span, ls.top << shift);
+  const int begin = piece * ls.span, end = min(begin + ls.span, sp.top << shift);
   const int e0 = begin >> shift, entries = ((end - 1) >> shift) - e0 + 1;
+  int32_t* const list = sp.blocks + ((long)t * c.H + g) * sp.top;
   if (tid == 0) list_end = 0;
+  if (ls.from == GIVEN) {
+    for (int e = tid; e < entries; e += 64 * KW) list_block[e] = list[e0 + e];
+  } else {
+    const int nb = blocks_up_to(c, hi), count = (nb + 255) & ~255;
+    uint32_t* const keys = (uint32_t*)(smem + sizeof(ChoiceLds));
+    ChoiceLds& choice = *(ChoiceLds*)smem;
+    clear_bins<256>(choice);
+    if (ls.from == SCORES) {
+      take_scores<256>(sp, ls.keys + ((long)t * c.H + g) * ls.pitch, nb, count, keys);
+    } else {
+      constexpr int NT = M == 16 ? 1 : 4;
+      Scored<D> next;
+      int id = block_id(c, row.s, kw * 64 + lane, nb);
+      if (kw * 64 < nb) load_blocks<D>(c, g, sp.summary, sp.scales, id, next);
+      id = block_id(c, row.s, 256 + kw * 64 + lane, nb);
+      Codes<D, NT> codes;
+      query_codes<DT, D, NT>([&](int y) -> const uint16_t* {
+        const int h = 16 * y + (lane & 15);
+        return h < G ? (const uint16_t*)a.q + t * a.q_pitch + (long)(g * G + h) * D : nullptr;
+      }, codes);
+      for (int b0 = kw * 64; b0 < count; b0 += 256) {
+        const Scored<D> now = next;
+        if (b0 + 256 < nb) load_blocks<D>(c, g, sp.summary, sp.scales, id, next);
+        id = block_id(c, row.s, b0 + 512 + lane, nb);
+        if (b0 < nb) {
+          score_blocks<D, NT>(now, codes, 16 * NT, G, [&](int, int j, u32x4_t key) {
+            const int b = b0 + 16 * j + 4 * (lane >> 4);
+            *(u32x4_t*)(keys + b) = (u32x4_t){key_of(sp, nb, b, key[0]), key_of(sp, nb, b + 1, key[1]), key_of(sp, nb, b + 2, key[2]), key_of(sp, nb, b + 3, key[3])};
+          });
+        } else {
+          keys[b0 + lane] = 0;
+        }
+      }
+    }
+    __syncthreads();
+    const bool writes = piece == 0 && blockIdx.y == 0;
+    const int taken = choose<256>(keys, count, sp.top, choice, [&](int at, int b) {
+      if (at >= e0 && at < e0 + entries) list_block[at - e0] = b;
+      if (writes) list[at] = b;
+    });
+    for (int e = tid; e < sp.top; e += 256)
+      if (e >= taken) {
+        if (e >= e0 && e < e0 + entries) list_block[e - e0] = -1;
+        if (writes) list[e] = -1;
+      }
+  }
   __syncthreads();
   for (int e = tid; e < entries; e += 64 * KW) {
-    const int b = ls.blocks[((long)t * c.H + g) * ls.top + e0 + e];
+    const int b = list_block[e];
     int page = -1;
     if (b >= 0 && b < c.max_pages && ((long)b << shift) < hi) page = c.pages[(long)row.s * c.max_pages + b];
     if (page >= c.n_pages) page = -1;
     list_page[e] = page;
-    list_block[e] = b;
     if (page >= 0) atomicMax(&list_end, e + 1);
   }
   __syncthreads();
@@ -831,49 +1012,57 @@ Pieces pieces_of(const Paged& c, int heads, int top) {
   const int G = heads / c.H, M = G <= 16 ? 16 : 32;
   const long items = (long)c.T * c.H * ((G + M - 1) / M), positions = (long)top << c.page_shift;
   const int slots = c.kept == c.dtype && c.D > 64 ? 256 : 512;        // workgroups at work at once, by their LDS
-  long pieces = 2 * items > slots ? 1 : std::min<long>(slots / items, (positions + 255) / 256);
+  long pieces = 2 * items > slots ? 1 : std::max(1l, std::min<long>(slots / items, positions / 512));
   long span = ((positions + pieces - 1) / pieces + 127) / 128 * 128;
   pieces = (positions + span - 1) / span;
   return Pieces{(int)pieces, (int)span};
 }
 
-size_t key_bytes(const Paged& c, int max_len, bool given) { return given ? 0 : ((size_t)c.T * c.H * key_pitch(c, max_len) * sizeof(uint32_t) + 255) / 256 * 256; }
+int choice_from(const Paged& c, const Sparse& sp);
+size_t key_bytes(const Paged& c, int max_len, const Sparse& sp) {
+  return choice_from(c, sp) == SCORES ? ((size_t)c.T * c.H * key_pitch(c, max_len) * sizeof(uint32_t) + 255) / 256 * 256 : 0;
+}
+
+// Which way the choice goes: by each item's own workgroup where there are enough of them.
+int choice_from(const Paged& c, const Sparse& sp) { return sp.given ? GIVEN : (long)c.T * c.H >= 256 && 2l * c.T <= 3l * c.S ? WHOLE : SCORES; }
 
 template <int DT, int D>
-hipError_t launch_choice(const Paged& c, const Attend& a, const Sparse& sp, uint32_t* keys, hipStream_t stream) {
+hipError_t launch_scores(const Paged& c, const Attend& a, const Sparse& sp, uint32_t* keys, hipStream_t stream) {
   const int nb = blocks_of(c, a.max_len), pitch = key_pitch(c, a.max_len), gp = run_of(a.heads / c.H), chunks = (nb + SCORED - 1) / SCORED;
   const bool one = gp <= 16 && (long)c.T * gp <= 16l * c.S;            // 16 columns hold the rows of a sequence, in the mean
-  const dim3 grid((unsigned)((long)c.T * c.H * chunks));
+  const int tokens = (one ? 16 : 64) / gp;
+  const dim3 grid((unsigned)(std::min<long>(c.T, c.T / tokens + (long)c.S) * c.H * chunks));
   if (one)
     hipLaunchKernelGGL((score_kernel<DT, D, 1>), grid, dim3(256), 0, stream, c, a, gp, chunks, pitch, sp.summary, sp.scales, keys);
   else
     hipLaunchKernelGGL((score_kernel<DT, D, 4>), grid, dim3(256), 0, stream, c, a, gp, chunks, pitch, sp.summary, sp.scales, keys);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const dim3 rows((unsigned)((long)c.T * c.H));
-  const bool tree = a.visible != nullptr;
-  if (nb <= 1024)
-    hipLaunchKernelGGL((choose_kernel<1, 16>), rows, dim3(64), 0, stream, c, a.max_len, tree, sp.top, sp.first, sp.recent, pitch, (const uint32_t*)keys, sp.blocks);
-  else if (nb <= 4096)
-    hipLaunchKernelGGL((choose_kernel<4, 16>), rows, dim3(256), 0, stream, c, a.max_len, tree, sp.top, sp.first, sp.recent, pitch, (const uint32_t*)keys, sp.blocks);
-  else
-    hipLaunchKernelGGL((choose_kernel<16, 32>), rows, dim3(1024), 0, stream, c, a.max_len, tree, sp.top, sp.first, sp.recent, pitch, (const uint32_t*)keys, sp.blocks);
   return hipGetLastError();
 }
+
+PerDeviceInt raised_choose;
 
 template <int DT, int KEPT, int D, int M>
 hipError_t launch_form(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream) {
   const Pieces pc = pieces_of(c, a.heads, sp.top);
-  constexpr size_t lds = Sizes<DT, KEPT, D, M>::LDS;
+  int from = choice_from(c, sp);
+  const int nb = blocks_of(c, a.max_len), pitch = key_pitch(c, a.max_len);
+  const bool apart = from == SCORES && (long)pc.pieces * nb > 8192;
+  const size_t lds = std::max<size_t>(Sizes<DT, KEPT, D, M>::LDS, from == GIVEN || apart ? 0 : choice_lds(nb));
   static PerDeviceInt raised;
   hipError_t e = ensure_dynamic_lds(raised, (const void*)sparse_attend_kernel<DT, KEPT, D, M>, lds);
   if (e != hipSuccess) return e;
-  if (!sp.given && (e = launch_choice<DT, D>(c, a, sp, (uint32_t*)ws, stream)) != hipSuccess) return e;
-  float* part = (float*)((char*)ws + key_bytes(c, a.max_len, sp.given));
+  if (from == SCORES && (e = launch_scores<DT, D>(c, a, sp, (uint32_t*)ws, stream)) != hipSuccess) return e;
+  if (apart) {
+    if ((e = ensure_dynamic_lds(raised_choose, (const void*)choose_kernel, choice_lds(nb))) != hipSuccess) return e;
+    hipLaunchKernelGGL(choose_kernel, dim3((unsigned)((long)c.T * c.H)), dim3(CHOOSERS), choice_lds(nb), stream, c, a.max_len, a.visible != nullptr, sp, pitch, (const uint32_t*)ws);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    from = GIVEN;
+  }
+  float* part = (float*)((char*)ws + key_bytes(c, a.max_len, sp));
   f32x2_t* stat = (f32x2_t*)(part + (size_t)c.T * a.heads * pc.pieces * D);
-  const Listed ls{sp.top, pc.pieces, pc.span, sp.blocks};
+  const Listed ls{pc.pieces, pc.span, from, pitch, (const uint32_t*)ws};
   const int G = a.heads / c.H;
-  hipLaunchKernelGGL((sparse_attend_kernel<DT, KEPT, D, M>), dim3((unsigned)((long)c.T * c.H * pc.pieces), (G + M - 1) / M), dim3(64 * KW), lds, stream, c, a, ls, part, stat);
+  hipLaunchKernelGGL((sparse_attend_kernel<DT, KEPT, D, M>), dim3((unsigned)((long)c.T * c.H * pc.pieces), (G + M - 1) / M), dim3(64 * KW), lds, stream, c, a, sp, ls, part, stat);
   if ((e = hipGetLastError()) != hipSuccess || pc.pieces == 1) return e;
   const long rows = (long)c.T * a.heads;
   hipLaunchKernelGGL((sparse_join_kernel<DT, D>), dim3((unsigned)((rows + JT / 32 - 1) / (JT / 32))), dim3(JT), 0, stream, c, a, pc.pieces, (const float*)part, (const f32x2_t*)stat);
@@ -902,10 +1091,10 @@ hipError_t with_forms(const Paged& c, F f) {
 
 }  // namespace
 
-size_t sparse_workspace_bytes(const Paged& c, int heads, int max_len, int top, bool given) {
-  const Pieces pc = pieces_of(c, heads, top);
+size_t sparse_workspace_bytes(const Paged& c, int heads, int max_len, const Sparse& sp) {
+  const Pieces pc = pieces_of(c, heads, sp.top);
   const size_t parts = pc.pieces == 1 ? 0 : (size_t)c.T * heads * pc.pieces * (c.D + 2) * sizeof(float);
-  return std::max<size_t>(key_bytes(c, max_len, given) + parts, 256);
+  return std::max<size_t>(key_bytes(c, max_len, sp) + parts, 256);
 }
 
 // A launch has fewer than 2^32 threads.
