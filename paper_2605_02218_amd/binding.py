@@ -610,8 +610,23 @@ def stream_step(p: StreamParams, n_keep: int, id_base: int, X_frame, s_fused, st
     return nxt.value, (c if (want_c and n_keep + p.frame_m > p.keep_k) else None)
 
 
+class _Laid:
+    """Parameters that keep their block until a field changes."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_block", None)
+
+    def _kept(self, key, make):
+        block = self.__dict__.get("_block")
+        if block is None or block[0] != key:
+            block = (key, make())
+            self.__dict__["_block"] = block
+        return block[1]
+
+
 @dataclass
-class CacheParams:
+class CacheParams(_Laid):
     n_seq: int
     n_tokens: int
     n_kv_heads: int
@@ -623,8 +638,8 @@ class CacheParams:
     cache_dtype: int = BF16
 
     def c_struct(self, row_pitch: int = 0) -> CovspecCacheParams:
-        return CovspecCacheParams(self.n_seq, self.n_tokens, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, self.max_pages, self.dtype,
-                                  self.cache_dtype, 0, row_pitch)
+        return self._kept(row_pitch, lambda: CovspecCacheParams(self.n_seq, self.n_tokens, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, self.max_pages,
+                                                                self.dtype, self.cache_dtype, 0, row_pitch))
 
 
 _TORCH = {}        # torch types by the library's numbers, and by name; filled with torch's first use here
@@ -634,7 +649,7 @@ def _types():
     if not _TORCH:
         import torch
         _TORCH.update({FP32: torch.float32, BF16: torch.bfloat16, FP16: torch.float16, INT8: torch.int8, E4M3: torch.float8_e4m3fn, "i32": torch.int32,
-                       "i64": torch.int64, "f32": torch.float32})
+                       "i64": torch.int64, "f32": torch.float32, "u8": torch.uint8, "torch": torch})
     return _TORCH
 
 
@@ -654,14 +669,14 @@ def _same_device(*tensors):
 
 def _stream_of(index: int) -> int:
     """Handle of the current stream of a device: without the stream object around it, which takes 3 us to make, where torch offers that."""
-    import torch
+    torch = _types()["torch"]
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _call_on(dev, fn, *args):
     """fn(*args, stream) with `dev` current, on its current stream."""
-    import torch
+    torch = _types()["torch"]
     if torch.cuda.current_device() == dev.index:
         return fn(*args, _stream_of(dev.index))
     with torch.cuda.device(dev):
@@ -827,8 +842,56 @@ def adjust_logits(p: LogitsParams, z, history, history_start, penalties, prompt_
 
 
 # ---------------------------------------------------------------- page tables, rotary positions, attention over selected pages
+# Small calls of these are bound by the host, so what is checked here is checked once for each tensor, and a parameter block is laid out again only after a change.
+def _given(dev, *items):
+    """Pointers of contiguous tensors on `dev`, None for None.  Items: (tensor, name, shape, type)."""
+    out = []
+    for t, name, shape, dtype in items:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not dtype or t.shape != shape:
+            raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+        if t.device != dev or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous tensor on %s" % (name, dev))
+        out.append(t.data_ptr())
+    return out
+
+
+def _given_rows(dev, t, name, n, heads, dim, dtype):
+    """(pointer, pitch) of rows as _rows takes them, on `dev`."""
+    if t.device != dev:
+        raise ValueError("%s must be on %s" % (name, dev))
+    return _rows(t, name, n, heads, dim, dtype)
+
+
+def _device_of(t):
+    if t is None or not t.is_cuda:
+        raise ValueError("tensors must be on a device")
+    return t.device
+
+
+def _launch(dev, name, *args):
+    """The library's entry point `name` with `dev` current, on its current stream."""
+    st = _call_on(dev, getattr(load_library(), name), *args)
+    if st != OK:
+        raise CovspecError(st, name)
+
+
+def _scratch(dev, workspace, size, p, name, *how):
+    """(address, bytes) of the caller's workspace, or of a new one."""
+    if workspace is None:
+        n = size(p, *how)
+        if n == 0:
+            raise CovspecError(INVALID_ARG, name)
+        workspace = _types()["torch"].empty(n + 256, dtype=_types()["u8"], device=dev)
+    elif workspace.device != dev:
+        raise ValueError("the workspace must be on %s" % dev)
+    return _ws_args(workspace)
+
+
 @dataclass
-class PagesParams:
+class PagesParams(_Laid):
     n_seq: int
     n_tokens: int
     page_size: int
@@ -836,7 +899,7 @@ class PagesParams:
     max_pages: int
 
     def c_struct(self) -> CovspecPagesParams:
-        return CovspecPagesParams(self.n_seq, self.n_tokens, self.page_size, self.n_pages, self.max_pages)
+        return self._kept(None, lambda: CovspecPagesParams(self.n_seq, self.n_tokens, self.page_size, self.n_pages, self.max_pages))
 
 
 class PagesStep(NamedTuple):
@@ -861,28 +924,23 @@ def pages_alloc(p: PagesParams, device="cuda"):
             torch.arange(p.n_pages - 1, -1, -1, dtype=i32, device=device), torch.full((1,), p.n_pages, dtype=i32, device=device))
 
 
-def pages_step(p: PagesParams, state, want, rows, workspace=None, want_slots=True) -> PagesStep:
-    """covspec_pages_step on `state` (of pages_alloc), which it changes; slots and positions are None without `want_slots`."""
-    import torch
+def pages_step(p: PagesParams, state, want, rows, workspace=None, want_slots=True, out=None) -> PagesStep:
+    """covspec_pages_step on `state` (of pages_alloc), which it changes; slots and positions are None without `want_slots`.  `out`: a PagesStep to fill again."""
     pages, held, borrowed, free, n_free = state
-    dev = _same_device(want, rows, workspace, *state)
-    i32, S, T = torch.int32, p.n_seq, p.n_tokens
-    args = [_expect(want, "want", (S,), i32), _expect(rows, "rows", (S,), i32), _expect(pages, "pages", (S, p.max_pages), i32), _expect(held, "held", (S,), i32),
-            _expect(borrowed, "borrowed", (S,), i32), _expect(free, "free_pages", (p.n_pages,), i32), _expect(n_free, "n_free", (1,), i32)]
-    if workspace is None:
-        n = pages_workspace_size(p)
-        if n == 0:
-            raise CovspecError(INVALID_ARG, "covspec_pages_workspace_size")
-        workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
-    slots = want_slots and T > 0
-    r = PagesStep(torch.empty(S + 1, dtype=i32, device=dev), torch.empty(S, dtype=i32, device=dev), torch.empty(S, dtype=i32, device=dev),
-                  torch.empty(T, dtype=torch.int64, device=dev) if slots else None, torch.empty(T, dtype=i32, device=dev) if slots else None)
-    wp, wb = _ws_args(workspace)
-    cs = p.c_struct()
-    st = _call_on(dev, load_library().covspec_pages_step, ctypes.byref(cs), *args, *[_ptr(t) for t in r], wp, wb)
-    if st != OK:
-        raise CovspecError(st, "covspec_pages_step")
-    return r
+    dev, types = _device_of(want), _types()
+    i32, S, T = types["i32"], p.n_seq, p.n_tokens
+    wp, wb = _scratch(dev, workspace, pages_workspace_size, p, "covspec_pages_workspace_size")
+    if out is None:
+        empty, i64 = types["torch"].empty, types["i64"]
+        slots = want_slots and T > 0
+        out = PagesStep(empty(S + 1, dtype=i32, device=dev), empty(S, dtype=i32, device=dev), empty(S, dtype=i32, device=dev),
+                        empty(T, dtype=i64, device=dev) if slots else None, empty(T, dtype=i32, device=dev) if slots else None)
+    one, row = (S,), (T,)
+    args = _given(dev, (want, "want", one, i32), (rows, "rows", one, i32), (pages, "pages", (S, p.max_pages), i32), (held, "held", one, i32), (borrowed, "borrowed", one, i32),
+                  (free, "free_pages", (p.n_pages,), i32), (n_free, "n_free", (1,), i32), (out[0], "start", (S + 1,), i32), (out[1], "length", one, i32),
+                  (out[2], "outcome", one, i32), (out[3], "slots", row, types["i64"]), (out[4], "positions", row, i32))
+    _launch(dev, "covspec_pages_step", ctypes.byref(p.c_struct()), *args, wp, wb)
+    return out
 
 
 def rotary_steps(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, original: int = 0, low: float = 0.0, high: float = 0.0,
@@ -899,7 +957,7 @@ def rotary_steps(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_P
 
 
 @dataclass
-class RotaryParams:
+class RotaryParams(_Laid):
     n_seq: int
     n_tokens: int
     n_heads: int
@@ -912,59 +970,63 @@ class RotaryParams:
     magnitude: float = 1.0
 
     def c_struct(self, q_pitch: int = 0, k_pitch: int = 0, q_out_pitch: int = 0, k_out_pitch: int = 0) -> CovspecRotaryParams:
-        return CovspecRotaryParams(self.n_seq, self.n_tokens, self.n_heads, self.n_kv_heads, self.head_dim, self.rotary_dim or self.head_dim, int(self.interleaved),
-                                   self.n_axes, self.dtype, self.magnitude, q_pitch, k_pitch, q_out_pitch, k_out_pitch)
+        return self._kept((q_pitch, k_pitch, q_out_pitch, k_out_pitch), lambda: CovspecRotaryParams(
+            self.n_seq, self.n_tokens, self.n_heads, self.n_kv_heads, self.head_dim, self.rotary_dim or self.head_dim, int(self.interleaved), self.n_axes, self.dtype,
+            self.magnitude, q_pitch, k_pitch, q_out_pitch, k_out_pitch))
 
 
-def _rotary_ptrs(p: RotaryParams, steps, positions, axis, start, length):
+def _rotary_args(dev, p: RotaryParams, steps, positions, axis, start, length):
     types = _types()
-    i32, half = types["i32"], (p.rotary_dim or p.head_dim) // 2
-    return [_expect(steps, "steps", (half,), types["i64"]), _expect(positions, "positions", (p.n_axes, p.n_tokens), i32), _expect(axis, "axis", (half,), i32),
-            _expect(start, "start", (p.n_seq + 1,), i32), _expect(length, "length", (p.n_seq,), i32)]
+    i32, half = types["i32"], ((p.rotary_dim or p.head_dim) // 2,)
+    return _given(dev, (steps, "steps", half, types["i64"]), (positions, "positions", (p.n_axes, p.n_tokens), i32), (axis, "axis", half, i32),
+                  (start, "start", (p.n_seq + 1,), i32), (length, "length", (p.n_seq,), i32))
 
 
 def rotate(p: RotaryParams, q, k, steps, start=None, length=None, positions=None, axis=None, q_out=None, k_out=None):
     """covspec_rotate: (q, k) turned, in q_out and k_out (which may be q and k) or new tensors; q or k may be None.  Padding rows of outputs allocated here
     are unspecified."""
-    import torch
-    dev = _same_device(q, k, steps, start, length, positions, axis, q_out, k_out)
-    dt = _types()[p.dtype]
-    got, pitch = [], {}
+    dev = _device_of(steps)
+    types = _types()
+    dt, T, D = types[p.dtype], p.n_tokens, p.head_dim
+    got = []
     for name, x, out, heads in (("q", q, q_out, p.n_heads), ("k", k, k_out, p.n_kv_heads)):
         if x is None:
             if out is not None:
                 raise ValueError("%s_out without %s" % (name, name))
-            got += [None, None, None]
+            got += [None, 0, None, 0, None]
             continue
-        out = torch.empty(p.n_tokens, heads, p.head_dim, dtype=dt, device=dev) if out is None else out
-        xp, pitch[name + "_pitch"] = _rows(x, name, p.n_tokens, heads, p.head_dim, dt)
-        op, pitch[name + "_out_pitch"] = _rows(out, name + "_out", p.n_tokens, heads, p.head_dim, dt)
-        got += [xp, op, out]
-    cs = p.c_struct(**pitch)
-    st = _call_on(dev, load_library().covspec_rotate, ctypes.byref(cs), got[0], got[3], *_rotary_ptrs(p, steps, positions, axis, start, length), got[1], got[4])
-    if st != OK:
-        raise CovspecError(st, "covspec_rotate")
-    return got[2], got[5]
+        out = types["torch"].empty((T, heads, D), dtype=dt, device=dev) if out is None else out
+        got += [*_given_rows(dev, x, name, T, heads, D, dt), *_given_rows(dev, out, name + "_out", T, heads, D, dt), out]
+    qp, q_pitch, qo, q_out_pitch, q_out, kp, k_pitch, ko, k_out_pitch, k_out = got
+    args = _rotary_args(dev, p, steps, positions, axis, start, length)
+    _launch(dev, "covspec_rotate", ctypes.byref(p.c_struct(q_pitch, k_pitch, q_out_pitch, k_out_pitch)), qp, kp, *args, qo, ko)
+    return q_out, k_out
+
+
+def _cache_args(dev, p: CacheParams, start, length, pages, cache):
+    types = _types()
+    k, v, ks, vs = cache
+    shape, i32, dt, f32 = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim), types["i32"], types[p.cache_dtype], types["f32"]
+    got = _given(dev, (start, "start", (p.n_seq + 1,), i32), (length, "length", (p.n_seq,), i32), (pages, "pages", (p.n_seq, p.max_pages), i32),
+                 (k, "k_cache", shape, dt), (v, "v_cache", shape, dt), (ks, "k_scale", shape[:3], f32), (vs, "v_scale", shape[:3], f32))
+    return got[:3], got[3:]
 
 
 def rotate_write(p: RotaryParams, c: CacheParams, q, k, v, steps, start, length, pages, cache, positions=None, axis=None, q_out=None):
     """covspec_rotate_write: q turned, in q_out (which may be q) or a new tensor; k, turned, and v into `cache` (of cache_alloc)."""
-    import torch
-    dev = _same_device(q, k, v, steps, start, length, pages, positions, axis, q_out, *cache)
-    dt = _types()[p.dtype]
-    qp, q_pitch = _rows(q, "q", p.n_tokens, p.n_heads, p.head_dim, dt)
-    q_out = torch.empty(p.n_tokens, p.n_heads, p.head_dim, dtype=dt, device=dev) if q_out is None else q_out
-    op, q_out_pitch = _rows(q_out, "q_out", p.n_tokens, p.n_heads, p.head_dim, dt)
-    kp, pitch = _rows(k, "k", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
-    vp, pitch_v = _rows(v, "v", p.n_tokens, p.n_kv_heads, p.head_dim, dt)
+    dev = _device_of(steps)
+    types = _types()
+    dt, T, H, D = types[p.dtype], p.n_tokens, p.n_kv_heads, p.head_dim
+    qp, q_pitch = _given_rows(dev, q, "q", T, p.n_heads, D, dt)
+    q_out = types["torch"].empty((T, p.n_heads, D), dtype=dt, device=dev) if q_out is None else q_out
+    op, q_out_pitch = _given_rows(dev, q_out, "q_out", T, p.n_heads, D, dt)
+    kp, pitch = _given_rows(dev, k, "k", T, H, D, dt)
+    vp, pitch_v = _given_rows(dev, v, "v", T, H, D, dt)
     if pitch != pitch_v:
         raise ValueError("k and v must have the same distance between rows")
-    batch, pool = _cache_ptrs(c, start, length, pages, cache)
-    cs, cc = p.c_struct(q_pitch, pitch, q_out_pitch), c.c_struct()
-    st = _call_on(dev, load_library().covspec_rotate_write, ctypes.byref(cs), ctypes.byref(cc), qp, kp, vp, *_rotary_ptrs(p, steps, positions, axis, start, length),
-                  batch[2], op, *pool)
-    if st != OK:
-        raise CovspecError(st, "covspec_rotate_write")
+    batch, pool = _cache_args(dev, c, start, length, pages, cache)
+    args = _rotary_args(dev, p, steps, positions, axis, None, None)
+    _launch(dev, "covspec_rotate_write", ctypes.byref(p.c_struct(q_pitch, pitch, q_out_pitch)), ctypes.byref(c.c_struct()), qp, kp, vp, *args[:3], *batch, op, *pool)
     return q_out
 
 
@@ -975,31 +1037,33 @@ def block_alloc(p: CacheParams, device="cuda"):
             torch.zeros(p.n_pages, p.n_kv_heads, dtype=torch.float32, device=device))
 
 
-def _summary_ptrs(p: CacheParams, summary):
+def _summary_args(dev, p: CacheParams, summary):
     types = _types()
-    return [_expect(summary[0], "summary", (p.n_pages, p.n_kv_heads, 2, p.head_dim), types[INT8]), _expect(summary[1], "summary scales", (p.n_pages, p.n_kv_heads), types["f32"])]
+    return _given(dev, (summary[0], "summary", (p.n_pages, p.n_kv_heads, 2, p.head_dim), types[INT8]), (summary[1], "summary scales", (p.n_pages, p.n_kv_heads), types["f32"]))
 
 
 def block_summary(p: CacheParams, start, length, pages, cache, summary):
     """covspec_block_summary: the pages that hold rows of the batch, summarised in `summary` (of block_alloc)."""
-    dev = _same_device(start, length, pages, *cache, *summary)
-    batch, pool = _cache_ptrs(p, start, length, pages, cache)
-    cs = p.c_struct()
-    st = _call_on(dev, load_library().covspec_block_summary, ctypes.byref(cs), *batch, pool[0], pool[2], *_summary_ptrs(p, summary))
-    if st != OK:
-        raise CovspecError(st, "covspec_block_summary")
+    dev = _device_of(start)
+    batch, pool = _cache_args(dev, p, start, length, pages, cache)
+    _launch(dev, "covspec_block_summary", ctypes.byref(p.c_struct()), *batch, pool[0], pool[2], *_summary_args(dev, p, summary))
     return summary
 
 
 @dataclass
-class SparseParams:
+class SparseParams(_Laid):
     attend: AttendParams
     top: int
     first: int = 1
     recent: int = 1
 
     def c_struct(self, q_pitch: int = 0, out_pitch: int = 0, given: bool = False) -> CovspecSparseParams:
-        return CovspecSparseParams(self.attend.c_struct(q_pitch, out_pitch), self.top, self.first, self.recent, int(given))
+        # the blocks inside may have changed on their own
+        a = self.attend
+        c = a.cache
+        key = (q_pitch, out_pitch, given, a.n_heads, a.max_len, a.window, a.scale, c.n_seq, c.n_tokens, c.n_kv_heads, c.head_dim, c.page_size, c.n_pages, c.max_pages,
+               c.dtype, c.cache_dtype)
+        return self._kept(key, lambda: CovspecSparseParams(a.c_struct(q_pitch, out_pitch), self.top, self.first, self.recent, int(given)))
 
 
 def sparse_workspace_size(p: SparseParams, given: bool = False) -> int:
@@ -1010,33 +1074,23 @@ def sparse_workspace_size(p: SparseParams, given: bool = False) -> int:
 def sparse_attend(p: SparseParams, q, start, length, pages, cache, summary, visible=None, blocks=None, workspace=None, out=None, want_lse=False, blocks_out=None):
     """covspec_sparse_attend: (out [T, heads, D], lse [T, heads] fp32 or None, blocks [T, Hkv, top] int32).  With `blocks` these are attended to and
     `summary` may be None; else the choice goes to blocks_out or a new tensor.  Padding rows of outputs allocated here are unspecified."""
-    import torch
     c, a = p.attend.cache, p.attend
     given = blocks is not None
     if given and blocks_out is not None:
         raise ValueError("blocks are either given or chosen")
     if not given and summary is None:
         raise ValueError("blocks are chosen by their summaries")
-    dev = _same_device(q, start, length, pages, visible, workspace, out, blocks, blocks_out, *cache, *(summary or ()))
-    dt = _types()[c.dtype]
-    qp, q_pitch = _rows(q, "q", c.n_tokens, a.n_heads, c.head_dim, dt)
-    out = torch.empty(c.n_tokens, a.n_heads, c.head_dim, dtype=dt, device=dev) if out is None else out
-    op, out_pitch = _rows(out, "out", c.n_tokens, a.n_heads, c.head_dim, dt)
-    batch, pool = _cache_ptrs(c, start, length, pages, cache)
-    bits = _expect(visible, "visible", (c.n_tokens,), _types()["i64"])
+    dev, types = _device_of(q), _types()
+    dt, empty, T, H = types[c.dtype], types["torch"].empty, c.n_tokens, c.n_kv_heads
+    qp, q_pitch = _given_rows(dev, q, "q", T, a.n_heads, c.head_dim, dt)
+    out = empty((T, a.n_heads, c.head_dim), dtype=dt, device=dev) if out is None else out
+    op, out_pitch = _given_rows(dev, out, "out", T, a.n_heads, c.head_dim, dt)
+    batch, pool = _cache_args(dev, c, start, length, pages, cache)
     if not given:
-        blocks = torch.empty(c.n_tokens, c.n_kv_heads, p.top, dtype=torch.int32, device=dev) if blocks_out is None else blocks_out
-    bp = _expect(blocks, "blocks", (c.n_tokens, c.n_kv_heads, p.top), _types()["i32"])
-    sp = [None, None] if summary is None else _summary_ptrs(c, summary)
-    if workspace is None:
-        n = sparse_workspace_size(p, given)
-        if n == 0:
-            raise CovspecError(INVALID_ARG, "covspec_sparse_workspace_size")
-        workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
-    lse = torch.empty(c.n_tokens, a.n_heads, dtype=torch.float32, device=dev) if want_lse else None
-    wp, wb = _ws_args(workspace)
-    cs = p.c_struct(q_pitch, out_pitch, given)
-    st = _call_on(dev, load_library().covspec_sparse_attend, ctypes.byref(cs), qp, *batch, *pool, *sp, bits, bp, op, _ptr(lse), wp, wb)
-    if st != OK:
-        raise CovspecError(st, "covspec_sparse_attend")
+        blocks = empty((T, H, p.top), dtype=types["i32"], device=dev) if blocks_out is None else blocks_out
+    more = _given(dev, (visible, "visible", (T,), types["i64"]), (blocks, "blocks", (T, H, p.top), types["i32"]))
+    made = (None, None) if summary is None else _summary_args(dev, c, summary)
+    wp, wb = _scratch(dev, workspace, sparse_workspace_size, p, "covspec_sparse_workspace_size", given)
+    lse = empty((T, a.n_heads), dtype=types["f32"], device=dev) if want_lse else None
+    _launch(dev, "covspec_sparse_attend", ctypes.byref(p.c_struct(q_pitch, out_pitch, given)), qp, *batch, *pool, *made, *more, op, None if lse is None else lse.data_ptr(), wp, wb)
     return out, lse, blocks

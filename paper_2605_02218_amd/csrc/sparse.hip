@@ -192,69 +192,106 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
 
 // ---- scores
 
-// A score as an integer of the same order; NaN above all others; 0 is left for blocks that are not there, the largest for those that are always taken.
-constexpr uint32_t kAlways = 0xFFFFFFFFu;
-__device__ __forceinline__ uint32_t score_key(float f) { return f != f ? kAlways - 1 : float_order_key(f); }
-
-// Largest over runs of gp lanes, a power of two up to 16.
-__device__ __forceinline__ uint32_t run_max(uint32_t v, int gp) {
-  if (gp >= 2) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));        // quad_perm 1 0 3 2
-  if (gp >= 4) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));        // quad_perm 2 3 0 1
-  if (gp >= 8) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));       // row_half_mirror
-  if (gp >= 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));      // row_mirror
-  return v;
+// A score as an integer of the same order.  A NaN comes above all others if it is positive, as the canonical one; kAbsent, a NaN of all ones, becomes 0, for a block
+// that is not there: as a block's scale it goes through its products (a NaN among the factors comes out as it is, before one in the summand).  The largest key is
+// left for blocks that are taken whatever their score.
+constexpr uint32_t kAbsent = 0xFFFFFFFFu, kNone = 0u, kAlways = 0xFFFFFFFFu;
+__device__ __forceinline__ uint32_t score_key(float f) {
+  const uint32_t u = __float_as_uint(f);
+  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 
 // Blocks are rows of the product, 16 at a time, (token, query head) its columns; the terms are max(c, 0) largest, then min(c, 0) smallest, 64 a step.  A lane has
 // column lane % 16 of a product and 16 neighbouring terms of each step.
+// The largest over runs of gp neighbouring lanes, a power of two, up to 16.
+template <int N>
+__device__ __forceinline__ void over_run(uint32_t (&v)[N], int gp) {
+  auto over = [&](auto step) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = max(v[i], (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v[i], step.value, 0xf, 0xf, true));
+  };
+  if (gp >= 2) over(std::integral_constant<int, 0xB1>{});              // quad_perm 1 0 3 2
+  if (gp >= 4) over(std::integral_constant<int, 0x4E>{});              // quad_perm 2 3 0 1
+  if (gp >= 8) over(std::integral_constant<int, 0x141>{});             // row_half_mirror
+  if (gp >= 16) over(std::integral_constant<int, 0x140>{});            // row_mirror
+}
+
 template <int D> constexpr int kSteps = 2 * D / 64;
 
-template <int D, int NT> struct Codes {
-  i32x4_t q[NT][kSteps<D>];
-  float scale[NT];
+template <int D> constexpr int kOwn = D == 96 ? kSteps<D> : kSteps<D> / 2;          // a lane's terms below and above zero are the same elements but for D = 96
+template <int D, int NT> struct Queries {
+  u32x4_t raw[NT][kOwn<D>][2];
   bool real[NT];
 };
+template <int D, int NT> struct Codes {
+  i32x4_t q[NT][kSteps<D>];
+  float scale[NT], bias[NT];                      // bias: 0; -infinity for a column of no query; NaN for a query that is none of numbers, whose scale is then 0
+};
 // from(n): the query of the lane's column 16 n + lane % 16, or null
-template <int DT, int D, int NT, typename F>
-__device__ __forceinline__ void query_codes(F from, Codes<D, NT>& r) {
-  constexpr int STEPS = kSteps<D>, OWN = D == 96 ? STEPS : STEPS / 2;  // a lane's terms below and above zero are the same elements but for D = 96
+template <int D, int NT, typename F>
+__device__ __forceinline__ void load_queries(F from, Queries<D, NT>& r) {
   const int quad = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const uint16_t* const x = from(n);
     r.real[n] = x != nullptr;
-    u32x4_t raw[OWN][2];
-    uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < OWN; ++k) {
+    for (int k = 0; k < kOwn<D>; ++k) {
       const int k0 = 64 * k + 16 * quad, d = k0 >= D ? k0 - D : k0;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        raw[k][p] = (u32x4_t){};
-        if (x) raw[k][p] = *(const u32x4_t*)(x + d + 8 * p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x2_t f = Half<DT>::unpack(raw[k][p][e]);
-          top = max(top, max(__float_as_uint(f[0]) & 0x7FFFFFFFu, __float_as_uint(f[1]) & 0x7FFFFFFFu));
-        }
+        r.raw[n][k][p] = (u32x4_t){};
+        if (x) r.raw[n][k][p] = *(const u32x4_t*)(x + d + 8 * p);
       }
     }
+  }
+}
+// Four int8 codes: beside 1.5 2^23 the nearest whole number, ties to even, is the low byte; at most 127 (1 + 3 2^-24) before, so 127 behind.
+__device__ __forceinline__ uint32_t int_codes(const float (&y)[4], float inv) {
+#pragma clang fp contract(off)
+  uint32_t b[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = y[e] * inv;                                        // rounded on its own
+    b[e] = __float_as_uint(x + 12582912.f);
+  }
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+}
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+template <int DT, int D, int NT>
+__device__ __forceinline__ void query_codes(const Queries<D, NT>& r, int columns, Codes<D, NT>& c) {
+  constexpr int OWN = kOwn<D>;
+  const int quad = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    if (16 * n >= columns) break;
+    u16x2_t most = {0, 0};                        // magnitudes of both types are in the order of their bits
+#pragma unroll
+    for (int k = 0; k < OWN; ++k)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, r.raw[n][k][p][e] & 0x7FFF7FFFu));
+    uint32_t top = max(most[0], most[1]);
     top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
     float inv;
-    const bool finite = code_step<DT_I8>(top, inv, r.scale[n]);
+    const bool finite = code_step<DT_I8>(__float_as_uint(Half<DT>::unpack(top)[0]), inv, c.scale[n]);
+    const uint32_t keep = finite ? ~0u : 0u;
+    if (!finite) c.scale[n] = 0.f;
+    c.bias[n] = !r.real[n] ? -INFINITY : finite ? 0.f : __uint_as_float(0x7FC00000u);
 #pragma unroll
     for (int k = 0; k < OWN; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const f32x2_t f0 = Half<DT>::unpack(raw[k][w / 2][2 * (w & 1)]), f1 = Half<DT>::unpack(raw[k][w / 2][2 * (w & 1) + 1]);
+        const f32x2_t f0 = Half<DT>::unpack(r.raw[n][k][w / 2][2 * (w & 1)]), f1 = Half<DT>::unpack(r.raw[n][k][w / 2][2 * (w & 1) + 1]);
         const float y[4] = {f0[0], f0[1], f1[0], f1[1]};
-        const uint32_t code = encode_row4<DT_I8>(y, inv, finite), below = (code >> 7 & 0x01010101u) * 0xFFu;      // bytes of codes below zero
+        const uint32_t code = int_codes(y, inv) & keep, sign = code >> 7 & 0x01010101u, below = (sign << 8) - sign;       // bytes of codes below zero
         if constexpr (D == 96) {
-          r.q[n][k][w] = (int)(64 * k + 16 * quad >= D ? code & below : code & ~below);
+          c.q[n][k][w] = (int)(64 * k + 16 * quad >= D ? code & below : code & ~below);
         } else {
-          r.q[n][k][w] = (int)(code & ~below);
-          r.q[n][k + OWN][w] = (int)(code & below);
+          c.q[n][k][w] = (int)(code & ~below);
+          c.q[n][k + OWN][w] = (int)(code & below);
         }
       }
   }
@@ -264,7 +301,6 @@ __device__ __forceinline__ void query_codes(F from, Codes<D, NT>& r) {
 template <int D> struct Scored {
   i32x4_t m[4][kSteps<D>];
   float scale;
-  unsigned long long exists;
 };
 __device__ __forceinline__ int block_id(const Paged& c, int s, int b, int nb) { return b < nb ? c.pages[(long)s * c.max_pages + b] : -1; }
 template <int D>
@@ -272,8 +308,8 @@ __device__ __forceinline__ void load_blocks(const Paged& c, int g, const int8_t*
   const int lane = threadIdx.x & 63;
   const bool there = id >= 0 && id < c.n_pages;
   id = there ? id : 0;
-  r.exists = __ballot(there);
   r.scale = scales[(long)id * c.H + g];
+  if (!there) r.scale = __uint_as_float(kAbsent);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const long from = ((long)__shfl(id, 16 * j + (lane & 15), 64) * c.H + g) * 2 * D + 16 * (lane >> 4);
@@ -281,42 +317,36 @@ __device__ __forceinline__ void load_blocks(const Paged& c, int g, const int8_t*
     for (int k = 0; k < kSteps<D>; ++k) r.m[j][k] = *(const i32x4_t*)(summary + from + 64 * k);
   }
 }
-// put(n, j, keys): keys of blocks 16 j + 4 (lane / 16) + 0 .. 3 for the token whose first column is 16 n + lane % 16, in those lanes; gp columns a token, `columns` in all
+// put(n, j, keys): those of blocks 16 j + 4 (lane / 16) + 0 .. 3 for the token whose first column is 16 n + lane % 16, in those lanes; gp columns a token, a power of two
+// up to 16 NT, `columns` in all
 template <int D, int NT, typename F>
 __device__ __forceinline__ void score_blocks(const Scored<D>& b, const Codes<D, NT>& q, int gp, int columns, F put) {
-  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int lane = threadIdx.x & 63, quad = lane >> 4, parts = gp <= 16 ? 1 : gp >> 4;
+  const bool first = (lane & 15 & (gp - 1)) == 0;
+  float ksc[16];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    float ksc[4];
+  for (int i = 0; i < 16; ++i) ksc[i] = __shfl(b.scale, 16 * (i / 4) + 4 * quad + i % 4, 64);
+  uint32_t best[16];                              // blocks 16 (i / 4) + 4 quad + i % 4
 #pragma unroll
-    for (int e = 0; e < 4; ++e) ksc[e] = __shfl(b.scale, 16 * j + 4 * quad + e, 64);
-    uint32_t best[NT][4];
+  for (int n = 0; n < NT; ++n) {
+    if (16 * n >= columns) break;
+    const bool more = (n & (parts - 1)) != 0;     // heads of the same token
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) best[n][e] = 0;
-      if (16 * n >= columns) continue;
+    for (int j = 0; j < 4; ++j) {
       i32x4_t acc = {0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < kSteps<D>; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b.m[j][k], q.q[n][k], acc, 0, 0, 0);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool ok = q.real[n] && (b.exists >> (16 * j + 4 * quad + e) & 1);
-        best[n][e] = run_max(ok ? score_key(__fmul_rn(__fmul_rn((float)acc[e], ksc[e]), q.scale[n])) : 0u, min(gp, 16));
+        const uint32_t key = score_key(__builtin_fmaf((float)acc[e] * ksc[4 * j + e], q.scale[n], q.bias[n]));       // a product's rounding: what is added is 0
+        best[4 * j + e] = more ? max(best[4 * j + e], key) : key;
       }
     }
+    if ((n & (parts - 1)) != parts - 1 && 16 * (n + 1) < columns) continue;
+    over_run(best, gp);
+    if (first) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if (gp > 16) {                              // a token's heads are in several products; its first one collects them
-        const int parts = gp / 16;
-        if (n % parts != 0) continue;
-#pragma unroll
-        for (int o = 1; o < NT; ++o)
-          if (o < parts && n + o < NT)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) best[n][e] = max(best[n][e], best[n + o][e]);
-      }
-      if ((16 * n + col) % gp == 0) put(n, j, (u32x4_t){best[n][0], best[n][1], best[n][2], best[n][3]});
+      for (int j = 0; j < 4; ++j) put(n & ~(parts - 1), j, (u32x4_t){best[4 * j], best[4 * j + 1], best[4 * j + 2], best[4 * j + 3]});
     }
   }
 }
@@ -350,15 +380,19 @@ __global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, i
   const Row r = {s, row0, n, (int)max((long)len - n, -(1l << 30))};
   const int i1 = min(i0 + tokens, n), nb = blocks_up_to(c, seen_end(c, r, i1 - 1, a.max_len, a.visible != nullptr)), b0 = chunk * SCORED + wave * 64;
   if (b0 >= nb) return;
-  Scored<D> b;
-  load_blocks<D>(c, g, summary, scales, block_id(c, s, b0 + lane, nb), b);
-  Codes<D, NT> q;
-  query_codes<DT, D, NT>([&](int y) -> const uint16_t* {
-    const int x = 16 * y + (lane & 15), i = i0 + x / gp, h = x % gp;
+  const int id = block_id(c, s, b0 + lane, nb);
+  const int shift = __builtin_ctz(gp);
+  Queries<D, NT> raw;
+  load_queries<D, NT>([&](int y) -> const uint16_t* {
+    const int x = 16 * y + (lane & 15), i = i0 + (x >> shift), h = x & (gp - 1);
     return i < i1 && h < G ? (const uint16_t*)a.q + (long)(row0 + i) * a.q_pitch + (long)(g * G + h) * D : nullptr;
-  }, q);
+  }, raw);
+  Scored<D> b;
+  load_blocks<D>(c, g, summary, scales, id, b);
+  Codes<D, NT> q;
+  query_codes<DT, D, NT>(raw, (i1 - i0) * gp, q);
   score_blocks<D, NT>(b, q, gp, (i1 - i0) * gp, [&](int y, int j, u32x4_t key) {
-    const int i = i0 + (16 * y + (lane & 15)) / gp;
+    const int i = i0 + ((16 * y + (lane & 15)) >> shift);
     if (i < i1) *(u32x4_t*)(keys + ((long)(row0 + i) * c.H + g) * pitch + b0 + 16 * j + 4 * (lane >> 4)) = key;
   });
 }
@@ -372,11 +406,39 @@ constexpr int BINS = 1024, PASSES = 4, GROUPS = 128;       // 256 neighbouring b
 struct ChoiceLds {
   int bins[PASSES][BINS];
   int above[GROUPS], equal[GROUPS];
-  int counts[16][4];
+  int counts[16][4], found[PASSES][4];
 };
 template <int THREADS>
 __device__ __forceinline__ void clear_bins(ChoiceLds& l) {
   for (int i = threadIdx.x; i < PASSES * BINS / 4; i += THREADS) ((i32x4_t*)l.bins)[i] = (i32x4_t){0, 0, 0, 0};
+}
+__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));      // row_shr 1, 2, 4, 8
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, true));      // row_bcast 15, 31
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, true));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+// Where the `need`-th largest of counted keys lies: the part, how many are beyond it, how many in it.  N parts for each lane, `own`, in the order of the lanes.
+struct Part { int bin, before, here; };
+template <int N>
+__device__ __forceinline__ Part part_of(const int (&own)[N], int need) {
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum += own[i];
+  const int upto = wave_inscan(sum), over = __builtin_amdgcn_readlane(upto, 63) - upto;    // keys in the parts of later lanes
+  const int from = 63 - __builtin_clzll(__ballot(over < need && over + sum >= need));      // one lane
+  int bin = 0, before = over, here = 0;
+#pragma unroll
+  for (int i = N - 1; i >= 0; --i) {
+    const bool past = before + here >= need;      // found in a part above
+    before += past ? 0 : here;
+    here = past ? here : own[i];
+    bin = past ? bin : i;
+  }
+  return Part{from * N + __builtin_amdgcn_readlane(bin, from), __builtin_amdgcn_readlane(before, from), __builtin_amdgcn_readlane(here, from)};
 }
 // Blocks taken, ascending, through put(place, block); their number is returned.  All threads.
 template <int THREADS, typename F>
@@ -397,9 +459,9 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, 
   }
   always = __builtin_amdgcn_readlane(wave_inscan(always), 63);
   there = __builtin_amdgcn_readlane(wave_inscan(there), 63);
-  lo = wave_min(lo);
-  hi = wave_max(hi);
-  if (lane == 0) { l.counts[wave][0] = always; l.counts[wave][1] = there; l.counts[wave][2] = (int)lo; l.counts[wave][3] = (int)hi; }
+  lo = ~wave_top(~lo);
+  hi = wave_top(hi);
+  if (lane == 0) *(i32x4_t*)l.counts[wave] = (i32x4_t){always, there, (int)lo, (int)hi};
   __syncthreads();
   always = there = 0;
 #pragma unroll
@@ -425,30 +487,27 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, 
           if (k[e] >= lo && k[e] <= hi) atomicAdd(&l.bins[pass][(k[e] - lo) >> shift], 1);
       }
       __syncthreads();
-      int own[16], sum = 0;
+      Part p = {};
+      if (WAVES <= 4 || wave == 0) {              // four waves do it each for itself, more would be in one another's way
+        int own[BINS / 64];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const i32x4_t v = ((const i32x4_t*)l.bins[pass])[lane * 4 + i];
+        for (int i = 0; i < BINS / 256; ++i) {
+          const i32x4_t v = ((const i32x4_t*)l.bins[pass])[lane * (BINS / 256) + i];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { own[4 * i + e] = v[e]; sum += v[e]; }
-      }
-      const int upto = wave_inscan(sum), over = __builtin_amdgcn_readlane(upto, 63) - upto;      // keys in the parts of later lanes
-      int bin = -1, before = over, here = 0;
-#pragma unroll
-      for (int i = 15; i >= 0; --i)
-        if (bin < 0) {
-          if (before + own[i] >= need) { bin = 16 * lane + i; here = own[i]; }
-          else before += own[i];
+          for (int e = 0; e < 4; ++e) own[4 * i + e] = v[e];
         }
-      const unsigned long long who = __ballot(over < need && bin >= 0);
-      const int from = 63 - __builtin_clzll(who);                      // one lane
-      bin = __builtin_amdgcn_readlane(bin, from);
-      before = __builtin_amdgcn_readlane(before, from);
-      here = __builtin_amdgcn_readlane(here, from);
-      need -= before;
-      lo += (uint32_t)bin << shift;
+        p = part_of(own, need);
+      }
+      if (WAVES > 4) {
+        if (threadIdx.x == 0) *(i32x4_t*)l.found[pass] = (i32x4_t){p.bin, p.before, p.here, 0};
+        __syncthreads();
+        const i32x4_t v = *(const i32x4_t*)l.found[pass];
+        p = Part{v[0], v[1], v[2]};
+      }
+      need -= p.before;
+      lo += (uint32_t)p.bin << shift;
       hi = min(hi, lo + ((1u << shift) - 1));
-      if (need == here) { at = lo - 1; break; }
+      if (need == p.here) { at = lo - 1; break; }
     }
   }
   // in order
@@ -492,35 +551,141 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, 
   return up_before + min(eq_before, more);
 }
 
-// Key of block b of nb as the choice takes it.
-__device__ __forceinline__ uint32_t key_of(const Sparse& sp, int nb, int b, uint32_t k) { return b >= nb ? 0u : b < sp.first || b >= nb - sp.recent ? kAlways : k; }
-// A row's scores of an earlier launch into LDS.
+// Keys of a lane's four blocks b .. b + 3 of nb as the choice takes them.
+__device__ __forceinline__ u32x4_t keys_of(const Sparse& sp, int nb, int b, u32x4_t scored) {
+  u32x4_t k;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) k[e] = b + e >= nb ? kNone : b + e < sp.first || b + e >= nb - sp.recent ? kAlways : scored[e];
+  return k;
+}
+// A row's scores of an earlier launch into LDS, four loads on their way at a time.
 template <int THREADS>
 __device__ __forceinline__ void take_scores(const Sparse& sp, const uint32_t* scored, int nb, int count, uint32_t* keys) {
-  for (int b = 4 * threadIdx.x; b < count; b += 4 * THREADS) {
-    u32x4_t k = {0, 0, 0, 0};
-    if (b < nb) k = *(const u32x4_t*)(scored + b);                     // their pitch is a multiple of 64
-    *(u32x4_t*)(keys + b) = (u32x4_t){key_of(sp, nb, b, k[0]), key_of(sp, nb, b + 1, k[1]), key_of(sp, nb, b + 2, k[2]), key_of(sp, nb, b + 3, k[3])};
+  for (int b0 = 4 * threadIdx.x; b0 < count; b0 += 16 * THREADS) {
+    u32x4_t k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = b0 + 4 * THREADS * i;
+      k[i] = (u32x4_t){0, 0, 0, 0};
+      if (b < nb) k[i] = *(const u32x4_t*)(scored + b);                // their pitch is a multiple of 64
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = b0 + 4 * THREADS * i;
+      if (b < count) *(u32x4_t*)(keys + b) = keys_of(sp, nb, b, k[i]);
+    }
   }
 }
 size_t choice_lds(int blocks) { return sizeof(ChoiceLds) + ((size_t)blocks + 255) / 256 * 256 * sizeof(uint32_t); }
 
-// A workgroup for each row and key head, where there are so many blocks that several workgroups of the attention should not choose among them.
+// A workgroup for each row and key head: for few rows of many blocks.
 constexpr int CHOOSERS = 1024;
-__global__ __launch_bounds__(CHOOSERS) void choose_kernel(Paged c, int max_len, bool tree, Sparse sp, int pitch, const uint32_t* __restrict__ keys) {
+__global__ __launch_bounds__(CHOOSERS) void choose_kernel(Paged c, int max_len, bool tree, Sparse sp, int pitch, const uint32_t* __restrict__ scores) {
   extern __shared__ __align__(1024) char smem[];
   const int t = blockIdx.x / c.H;
   Row r;
   if (!row_of(c, t, r)) return;
   const int nb = blocks_up_to(c, seen_end(c, r, t - r.row0, max_len, tree)), count = (nb + 255) & ~255;
   ChoiceLds& choice = *(ChoiceLds*)smem;
-  uint32_t* const lds_keys = (uint32_t*)(smem + sizeof(ChoiceLds));
+  uint32_t* const keys = (uint32_t*)(smem + sizeof(ChoiceLds));
   int32_t* const list = sp.blocks + (long)blockIdx.x * sp.top;
   clear_bins<CHOOSERS>(choice);
-  take_scores<CHOOSERS>(sp, keys + (long)blockIdx.x * pitch, nb, count, lds_keys);
+  take_scores<CHOOSERS>(sp, scores + (long)blockIdx.x * pitch, nb, count, keys);
   __syncthreads();
-  const int taken = choose<CHOOSERS>(lds_keys, count, sp.top, choice, [&](int at, int b) { list[at] = b; });
+  const int taken = choose<CHOOSERS>(keys, count, sp.top, choice, [&](int at, int b) { list[at] = b; });
   for (int e = taken + (int)threadIdx.x; e < sp.top; e += CHOOSERS) list[e] = -1;
+}
+
+// A wave for each row and key head: for many rows of up to 2048 blocks, 32 keys in a lane.  The same steps with 256 parts.
+constexpr int ROW_BLOCKS = 2048;
+__global__ __launch_bounds__(256) void choose_rows_kernel(Paged c, int max_len, bool tree, Sparse sp, int pitch, const uint32_t* __restrict__ scores) {
+  constexpr int TRIPS = ROW_BLOCKS / 256;
+  __shared__ __align__(16) int bins[4][256];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long item = (long)blockIdx.x * 4 + wave;
+  const int t = (int)(item / c.H);
+  Row r;
+  if (!row_of(c, t, r)) return;
+  const int nb = blocks_up_to(c, seen_end(c, r, t - r.row0, max_len, tree));
+  const uint32_t* const scored = scores + item * pitch;
+  u32x4_t k[TRIPS];
+#pragma unroll
+  for (int i = 0; i < TRIPS; ++i) {
+    const int b = 256 * i + 4 * lane;
+    k[i] = (u32x4_t){0, 0, 0, 0};
+    if (b < nb) k[i] = *(const u32x4_t*)(scored + b);
+  }
+  uint32_t lo = kAlways, hi = 0;
+  int always = 0, there = 0;
+#pragma unroll
+  for (int i = 0; i < TRIPS; ++i) {
+    k[i] = keys_of(sp, nb, 256 * i + 4 * lane, k[i]);
+    if (256 * i < nb) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = k[i][e];
+        always += x == kAlways;
+        there += x != kNone;
+        lo = min(lo, x - 1 < kAlways - 1 ? x : kAlways);
+        hi = max(hi, x == kAlways ? 0u : x);
+      }
+    }
+  }
+  always = __builtin_amdgcn_readlane(wave_inscan(always), 63);
+  there = __builtin_amdgcn_readlane(wave_inscan(there), 63);
+  lo = ~wave_top(~lo);
+  hi = wave_top(hi);
+  uint32_t at = 0;
+  int more = 0, need = sp.top - always;
+  int* const mine = bins[wave];
+  if (there - always > need) {
+    at = kAlways - 1;
+    while (need > 0) {
+      const uint32_t width = hi - lo;
+      if (width == 0) { at = lo; more = need; break; }
+      const int shift = max(0, 24 - __builtin_clz(width));             // of 32 - clz bits eight count
+      ((i32x4_t*)mine)[lane] = (i32x4_t){0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < TRIPS; ++i)
+        if (256 * i < nb) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (k[i][e] - lo <= width) atomicAdd(&mine[(k[i][e] - lo) >> shift], 1);
+        }
+      const i32x4_t v = ((const i32x4_t*)mine)[lane];                  // a wave's accesses to LDS keep their order
+      const int own[4] = {v[0], v[1], v[2], v[3]};
+      const Part p = part_of(own, need);
+      need -= p.before;
+      lo += (uint32_t)p.bin << shift;
+      hi = min(hi, lo + ((1u << shift) - 1));
+      if (need == p.here) { at = lo - 1; break; }
+    }
+  }
+  const bool ties = at != 0 && more > 0;
+  int32_t* const list = sp.blocks + item * sp.top;
+  int up_before = 0, eq_before = 0;
+  const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < TRIPS; ++i)
+    if (256 * i < nb) {
+      int ups = up_before, eqs = eq_before;       // in front of the lane's four
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const unsigned long long up = __ballot(k[i][e] > at), eq = __ballot(ties && k[i][e] == at);
+        ups += __popcll(up & below);
+        eqs += __popcll(eq & below);
+        up_before += __popcll(up);
+        eq_before += __popcll(eq);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool is_up = k[i][e] > at, is_eq = ties && k[i][e] == at;
+        if (is_up || (is_eq && eqs < more)) list[ups + min(eqs, more)] = 256 * i + 4 * lane + e;
+        ups += is_up;
+        eqs += is_eq;
+      }
+    }
+  for (int e = up_before + min(eq_before, more) + lane; e < sp.top; e += 64) list[e] = -1;
 }
 
 // ---- attention over the choice
@@ -534,8 +699,10 @@ enum { GIVEN, SCORES, WHOLE };
 struct Listed {
   int pieces, span;                    // span: positions of a piece, a multiple of 128
   int from, pitch;                     // from: GIVEN, SCORES, WHOLE; pitch: of the scores of an item
-  const uint32_t* keys;
+  const uint32_t* scores;
 };
+constexpr int OWN_BLOCKS = 4096;       // of a choice by a workgroup of the attention
+
 
 template <int DT, int KEPT, int D, int M> struct Sizes {
   typedef Form<DT, KEPT, D> F;
@@ -581,33 +748,35 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
     for (int e = tid; e < entries; e += 64 * KW) list_block[e] = list[e0 + e];
   } else {
     const int nb = blocks_up_to(c, hi), count = (nb + 255) & ~255;
-    uint32_t* const keys = (uint32_t*)(smem + sizeof(ChoiceLds));
     ChoiceLds& choice = *(ChoiceLds*)smem;
+    uint32_t* const keys = (uint32_t*)(smem + sizeof(ChoiceLds));
     clear_bins<256>(choice);
     if (ls.from == SCORES) {
-      take_scores<256>(sp, ls.keys + ((long)t * c.H + g) * ls.pitch, nb, count, keys);
+      take_scores<256>(sp, ls.scores + ((long)t * c.H + g) * ls.pitch, nb, count, keys);
     } else {
       constexpr int NT = M == 16 ? 1 : 4;
       Scored<D> next;
       int id = block_id(c, row.s, kw * 64 + lane, nb);
+      Queries<D, NT> raw;
+      load_queries<D, NT>([&](int y) -> const uint16_t* {
+        const int h = 16 * y + (lane & 15);
+        return h < G ? (const uint16_t*)a.q + t * a.q_pitch + (long)(g * G + h) * D : nullptr;
+      }, raw);
       if (kw * 64 < nb) load_blocks<D>(c, g, sp.summary, sp.scales, id, next);
       id = block_id(c, row.s, 256 + kw * 64 + lane, nb);
       Codes<D, NT> codes;
-      query_codes<DT, D, NT>([&](int y) -> const uint16_t* {
-        const int h = 16 * y + (lane & 15);
-        return h < G ? (const uint16_t*)a.q + t * a.q_pitch + (long)(g * G + h) * D : nullptr;
-      }, codes);
+      query_codes<DT, D, NT>(raw, G, codes);
       for (int b0 = kw * 64; b0 < count; b0 += 256) {
         const Scored<D> now = next;
         if (b0 + 256 < nb) load_blocks<D>(c, g, sp.summary, sp.scales, id, next);
         id = block_id(c, row.s, b0 + 512 + lane, nb);
         if (b0 < nb) {
-          score_blocks<D, NT>(now, codes, 16 * NT, G, [&](int, int j, u32x4_t key) {
+          score_blocks<D, NT>(now, codes, 16 * NT, G, [&](int, int j, u32x4_t scored) {
             const int b = b0 + 16 * j + 4 * (lane >> 4);
-            *(u32x4_t*)(keys + b) = (u32x4_t){key_of(sp, nb, b, key[0]), key_of(sp, nb, b + 1, key[1]), key_of(sp, nb, b + 2, key[2]), key_of(sp, nb, b + 3, key[3])};
+            *(u32x4_t*)(keys + b) = keys_of(sp, nb, b, scored);
           });
         } else {
-          keys[b0 + lane] = 0;
+          keys[b0 + lane] = kNone;
         }
       }
     }
@@ -1007,24 +1176,30 @@ int run_of(int G) {
   return gp;
 }
 
+// Workgroups of the attention at work at once, by their LDS: 128 KB of tiles, or half of it.
+int slots_of(const Paged& c) { return c.kept == c.dtype && c.D > 64 ? 256 : 512; }
+
+#ifndef PIECE
+#define PIECE 512
+#endif
 struct Pieces { int pieces, span; };
 Pieces pieces_of(const Paged& c, int heads, int top) {
   const int G = heads / c.H, M = G <= 16 ? 16 : 32;
   const long items = (long)c.T * c.H * ((G + M - 1) / M), positions = (long)top << c.page_shift;
-  const int slots = c.kept == c.dtype && c.D > 64 ? 256 : 512;        // workgroups at work at once, by their LDS
-  long pieces = 2 * items > slots ? 1 : std::max(1l, std::min<long>(slots / items, positions / 512));
+  const int slots = slots_of(c);
+  long pieces = 2 * items > slots ? 1 : std::max(1l, std::min<long>(slots / items, positions / PIECE));
   long span = ((positions + pieces - 1) / pieces + 127) / 128 * 128;
   pieces = (positions + span - 1) / span;
   return Pieces{(int)pieces, (int)span};
 }
 
-int choice_from(const Paged& c, const Sparse& sp);
+int choice_from(const Paged& c, int max_len, const Sparse& sp);
 size_t key_bytes(const Paged& c, int max_len, const Sparse& sp) {
-  return choice_from(c, sp) == SCORES ? ((size_t)c.T * c.H * key_pitch(c, max_len) * sizeof(uint32_t) + 255) / 256 * 256 : 0;
+  return choice_from(c, max_len, sp) == SCORES ? ((size_t)c.T * c.H * key_pitch(c, max_len) * sizeof(uint32_t) + 255) / 256 * 256 : 0;
 }
 
 // Which way the choice goes: by each item's own workgroup where there are enough of them.
-int choice_from(const Paged& c, const Sparse& sp) { return sp.given ? GIVEN : (long)c.T * c.H >= 256 && 2l * c.T <= 3l * c.S ? WHOLE : SCORES; }
+int choice_from(const Paged& c, int max_len, const Sparse& sp) { return sp.given ? GIVEN : (long)c.T * c.H >= 256 && 2l * c.T <= 3l * c.S && blocks_of(c, max_len) <= OWN_BLOCKS ? WHOLE : SCORES; }
 
 template <int DT, int D>
 hipError_t launch_scores(const Paged& c, const Attend& a, const Sparse& sp, uint32_t* keys, hipStream_t stream) {
@@ -1040,22 +1215,33 @@ hipError_t launch_scores(const Paged& c, const Attend& a, const Sparse& sp, uint
 }
 
 PerDeviceInt raised_choose;
+hipError_t launch_choice(const Paged& c, const Attend& a, const Sparse& sp, int pitch, const uint32_t* scores, hipStream_t stream) {
+  const int nb = blocks_of(c, a.max_len);
+  const long rows = (long)c.T * c.H;
+  if (nb <= ROW_BLOCKS && rows >= 128) {
+    hipLaunchKernelGGL(choose_rows_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, c, a.max_len, a.visible != nullptr, sp, pitch, scores);
+    return hipGetLastError();
+  }
+  hipError_t e = ensure_dynamic_lds(raised_choose, (const void*)choose_kernel, choice_lds(nb));
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(choose_kernel, dim3((unsigned)rows), dim3(CHOOSERS), choice_lds(nb), stream, c, a.max_len, a.visible != nullptr, sp, pitch, scores);
+  return hipGetLastError();
+}
 
 template <int DT, int KEPT, int D, int M>
 hipError_t launch_form(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream) {
   const Pieces pc = pieces_of(c, a.heads, sp.top);
-  int from = choice_from(c, sp);
+  int from = choice_from(c, a.max_len, sp);
   const int nb = blocks_of(c, a.max_len), pitch = key_pitch(c, a.max_len);
-  const bool apart = from == SCORES && (long)pc.pieces * nb > 8192;
+    const bool apart = from == SCORES && (nb > OWN_BLOCKS || (long)pc.pieces * nb > 8192 || (slots_of(c) == 256 && (long)c.T * c.H * pc.pieces > 256));
   const size_t lds = std::max<size_t>(Sizes<DT, KEPT, D, M>::LDS, from == GIVEN || apart ? 0 : choice_lds(nb));
   static PerDeviceInt raised;
   hipError_t e = ensure_dynamic_lds(raised, (const void*)sparse_attend_kernel<DT, KEPT, D, M>, lds);
   if (e != hipSuccess) return e;
   if (from == SCORES && (e = launch_scores<DT, D>(c, a, sp, (uint32_t*)ws, stream)) != hipSuccess) return e;
   if (apart) {
-    if ((e = ensure_dynamic_lds(raised_choose, (const void*)choose_kernel, choice_lds(nb))) != hipSuccess) return e;
-    hipLaunchKernelGGL(choose_kernel, dim3((unsigned)((long)c.T * c.H)), dim3(CHOOSERS), choice_lds(nb), stream, c, a.max_len, a.visible != nullptr, sp, pitch, (const uint32_t*)ws);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = launch_choice(c, a, sp, pitch, (const uint32_t*)ws, stream);
+    if (e != hipSuccess) return e;
     from = GIVEN;
   }
   float* part = (float*)((char*)ws + key_bytes(c, a.max_len, sp));
