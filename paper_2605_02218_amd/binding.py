@@ -931,10 +931,11 @@ def pages_step(p: PagesParams, state, want, rows, workspace=None, want_slots=Tru
     i32, S, T = types["i32"], p.n_seq, p.n_tokens
     wp, wb = _scratch(dev, workspace, pages_workspace_size, p, "covspec_pages_workspace_size")
     if out is None:
-        empty, i64 = types["torch"].empty, types["i64"]
+        # one allocation for what is int32: an allocation takes longer than its part of the split
         slots = want_slots and T > 0
-        out = PagesStep(empty(S + 1, dtype=i32, device=dev), empty(S, dtype=i32, device=dev), empty(S, dtype=i32, device=dev),
-                        empty(T, dtype=i64, device=dev) if slots else None, empty(T, dtype=i32, device=dev) if slots else None)
+        empty = types["torch"].empty
+        parts = empty(3 * S + 1 + (T if slots else 0), dtype=i32, device=dev).split((S + 1, S, S, T) if slots else (S + 1, S, S))
+        out = PagesStep(*parts[:3], empty(T, dtype=types["i64"], device=dev) if slots else None, parts[3] if slots else None)
     one, row = (S,), (T,)
     args = _given(dev, (want, "want", one, i32), (rows, "rows", one, i32), (pages, "pages", (S, p.max_pages), i32), (held, "held", one, i32), (borrowed, "borrowed", one, i32),
                   (free, "free_pages", (p.n_pages,), i32), (n_free, "n_free", (1,), i32), (out[0], "start", (S + 1,), i32), (out[1], "length", one, i32),

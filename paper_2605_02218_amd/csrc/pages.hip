@@ -4,8 +4,8 @@
 // and every row is then found on its own: the j-th page given out comes from place there - 1 - j of the stack, where it was before, or, above that,
 // is the r-th one given back, looked up in the table that it leaves.  Nothing is read that the same step writes.
 //
-// One workgroup takes the sums, and, where rows and sequences are few, the pages and rows too (one launch: latency is all that counts there); else a
-// second launch moves them with as many threads as there are rows or sequences.
+// Where rows and sequences are few one workgroup does everything, a sequence a thread, with all sums in LDS: latency is all that counts there.  Else one workgroup
+// takes the sums, and a second launch moves pages and places rows with as many threads as there are.
 #include "common.h"
 #include "kernels.h"
 
@@ -14,7 +14,7 @@ namespace covspec {
 namespace {
 
 constexpr int PT = 1024;
-constexpr int kFew = 4096;                       // rows and sequences for which one workgroup does everything
+constexpr int kFewSeq = 1024, kFewRows = 4096;   // one workgroup does everything
 
 // Exclusive prefix sums of two numbers a thread over a workgroup, and their totals.
 struct Two { long a, b; };
@@ -82,12 +82,12 @@ __device__ __forceinline__ void move_pages(const Pages& p, const Plan& pl, const
     for (int i = thread; i < keep - held; i += threads) row[held + i] = page_given(p, pl, u, asked + i);      // keep: what it will hold
 }
 
-__device__ __forceinline__ void place_row(const Pages& p, const Plan& pl, const Sums& u, const int* start, int total, int t) {
+__device__ __forceinline__ void place_row(const Pages& p, const Plan& pl, const Sums& u, const int* start, const int* length, int total, int t) {
   long slot = -1;
   int pos = -1;
   if (t < total) {
     const int s = last_not_beyond(start, p.S, t);
-    pos = p.length[s] - start[s + 1] + t;
+    pos = length[s] - start[s + 1] + t;
     const int at = pos >> p.page_shift, held = pl.held[s];
     int page = -1;
     if (at >= held) {
@@ -101,7 +101,6 @@ __device__ __forceinline__ void place_row(const Pages& p, const Plan& pl, const 
   if (p.positions) p.positions[t] = pos;
 }
 
-template <bool ALL>
 __global__ __launch_bounds__(PT) void pages_plan_kernel(Pages p, int* __restrict__ ws) {
   __shared__ Two waves[PT / 64];
   __shared__ int most;                           // rows that have room: those up to the first sequence whose rows do not fit
@@ -181,11 +180,75 @@ __global__ __launch_bounds__(PT) void pages_plan_kernel(Pages p, int* __restrict
     pl.scalars[2] = u.there;
     pl.scalars[3] = u.after;
   }
-  if constexpr (ALL) {
-    __syncthreads();
-    for (int s = tid >> 4; s < p.S; s += PT / 16) move_pages(p, pl, u, s, tid & 15, 16);
-    for (int t = tid; t < p.T; t += PT) place_row(p, pl, u, p.start, filled, t);
+}
+
+// Exclusive sums of two numbers a thread, and their totals; fewer than 2^31 in all.  `sums` is used by no other call.
+struct Two32 { int a, b; };
+__device__ __forceinline__ Two32 exscan2_32(Two32 v, Two32* sums, Two32* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int a = wave_inscan(v.a), b = wave_inscan(v.b);
+  if (lane == 63) sums[w] = Two32{a, b};
+  __syncthreads();
+  const Two32 mine = lane < PT / 64 ? sums[lane] : Two32{0, 0};
+  const int ups_a = wave_inscan(mine.a), ups_b = wave_inscan(mine.b);
+  *total = Two32{__builtin_amdgcn_readlane(ups_a, PT / 64 - 1), __builtin_amdgcn_readlane(ups_b, PT / 64 - 1)};
+  const int at = __builtin_amdgcn_readfirstlane(w);
+  return Two32{__builtin_amdgcn_readlane(ups_a - mine.a, at) + a - v.a, __builtin_amdgcn_readlane(ups_b - mine.b, at) + b - v.b};
+}
+
+__global__ __launch_bounds__(PT) void pages_few_kernel(Pages p) {
+  __shared__ Two32 sums[2][PT / 64];
+  __shared__ int keep_of[kFewSeq], held_of[kFewSeq], given_of[kFewSeq + 1], asked_of[kFewSeq], length_of[kFewSeq], start_of[kFewSeq + 1], filled;
+  const int s = threadIdx.x;
+  const bool real = s < p.S;
+  int want = 0, rows = 0, held = 0, borrowed = 0;
+  if (real) {
+    want = max(p.want[s], 0);
+    rows = between(p.rows[s], 0, want);
+    held = between(p.held[s], 0, p.max_pages);
+    borrowed = between(p.borrowed[s], 0, held);
   }
+  Sums u;
+  u.before = between(p.n_free[0], 0, p.n_pages);
+  const int need = (int)(((long)want + (1 << p.page_shift) - 1) >> p.page_shift);
+  const bool fits = need <= p.max_pages;
+  const int goal = fits ? need : held, keep = max(goal, borrowed), back = max(held - keep, 0), asks = max(goal - held, 0);
+  Two32 total;
+  const Two32 front = exscan2_32(Two32{back, asks}, sums[0], &total);
+  u.given = total.a;
+  u.there = min(u.before + u.given, p.n_pages);
+  const bool served = asks == 0 || front.b + asks <= u.there, ok = fits && served;
+  const int now = ok ? need : held, n = ok ? min(rows, p.T + 1) : 0;                   // 1024 (4096 + 1) rows at most
+  const Two32 ahead = exscan2_32(Two32{n, served ? asks : 0}, sums[1], &total);
+  u.after = u.there - total.b;
+  const int upto = ahead.a + n;
+  const bool room = n == 0 || upto <= p.T;
+  if (s == 0) { filled = 0; start_of[0] = 0; given_of[p.S] = u.given; }
+  __syncthreads();
+  if (real && upto <= p.T) atomicMax(&filled, upto);
+  __syncthreads();
+  if (real) {
+    const int start = min(upto, filled), length = ok && room ? want : (int)min((long)want - rows, (long)now << p.page_shift);
+    keep_of[s] = keep;
+    held_of[s] = held;
+    given_of[s] = front.a;
+    asked_of[s] = asks > 0 && served ? front.b : -1;
+    length_of[s] = length;
+    start_of[s + 1] = start;
+    p.outcome[s] = ok ? room ? 0 : 2 : 1;
+    p.length[s] = length;
+    p.start[s + 1] = start;
+    p.held[s] = now;
+    p.borrowed[s] = min(borrowed, now);
+  }
+  if (s == 0) {
+    p.start[0] = 0;
+    p.n_free[0] = u.after;
+  }
+  __syncthreads();
+  const Plan pl = {keep_of, held_of, given_of, asked_of, nullptr};
+  for (int t = threadIdx.x; t < p.T; t += PT) place_row(p, pl, u, start_of, length_of, filled, t);
+  for (int i = threadIdx.x >> 4; i < p.S; i += PT / 16) move_pages(p, pl, u, i, threadIdx.x & 15, 16);
 }
 
 constexpr int MT = 256;
@@ -194,7 +257,7 @@ __global__ __launch_bounds__(MT) void pages_move_kernel(Pages p, int* __restrict
   const Sums u = {pl.scalars[0], pl.scalars[1], pl.scalars[2], pl.scalars[3]};
   if ((int)blockIdx.x < row_groups) {
     const int t = blockIdx.x * MT + threadIdx.x;
-    if (t < p.T) place_row(p, pl, u, p.start, p.start[p.S], t);
+    if (t < p.T) place_row(p, pl, u, p.start, p.length, p.start[p.S], t);
   } else {
     const int s = (blockIdx.x - row_groups) * (MT / 64) + threadIdx.x / 64;
     if (s < p.S) move_pages(p, pl, u, s, threadIdx.x & 63, 64);
@@ -206,11 +269,11 @@ __global__ __launch_bounds__(MT) void pages_move_kernel(Pages p, int* __restrict
 size_t pages_workspace_bytes(int S) { return ((size_t)4 * S + 1 + 4) * sizeof(int); }
 
 hipError_t launch_pages(const Pages& p, void* ws, hipStream_t stream) {
-  if (p.S <= kFew && p.T <= kFew) {
-    hipLaunchKernelGGL((pages_plan_kernel<true>), dim3(1), dim3(PT), 0, stream, p, (int*)ws);
+  if (p.S <= kFewSeq && p.T <= kFewRows) {
+    hipLaunchKernelGGL(pages_few_kernel, dim3(1), dim3(PT), 0, stream, p);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((pages_plan_kernel<false>), dim3(1), dim3(PT), 0, stream, p, (int*)ws);
+  hipLaunchKernelGGL(pages_plan_kernel, dim3(1), dim3(PT), 0, stream, p, (int*)ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int row_groups = p.slots || p.positions ? (p.T + MT - 1) / MT : 0;

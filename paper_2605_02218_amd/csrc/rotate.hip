@@ -15,6 +15,9 @@ namespace covspec {
 namespace {
 
 constexpr int RT = 256;
+// Groups of lanes that share a token's heads, at most, where there are rows enough to fill the device.  us with 4, 8 and 16: 8 x 3008 tokens of 40 + 8 heads of 128 into a
+// 16-bit cache 129, 120, 114 (5.2 TB/s); 20480 tokens of 32 heads with three axes 75, 70.5, 72.5: fewer rows a lane even out better, more share its angles.
+constexpr int STEP = 16;
 
 struct Turn { float c, s; };
 // Cosine and sine of a 64-bit fraction of a turn: series around the nearest quarter, |x| <= pi / 4, errors below 2^-28 of 1; the conversion to a
@@ -77,21 +80,31 @@ __global__ __launch_bounds__(RT) void rotate_kernel(Paged c, Rotate r) {
       if constexpr (CACHE) place = place_of(c, s, at, 0);
     }
   }
-  // which elements: eight pairs, or 16 neighbouring ones that are not turned
+  // which elements: eight at a and eight at b, neighbouring lanes' next to each other; eight pairs, across the two (FAR) or four in each, or 16 that are not turned
   const bool turns = lane * 16 < r.R;
-  const int a = FAR && turns ? 8 * lane : 16 * lane, b = FAR && turns ? r.R / 2 + 8 * lane : 16 * lane + 8;
+  const int at = turns ? lane : lane - r.R / 16, a = (turns ? 0 : r.R) + 8 * at, b = a + (turns ? r.R : D - r.R) / 2;
   Turn w[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) w[e] = Turn{1.f, 0.f};
   if (turns && mine) {
+    int p[4] = {pos, pos, pos, pos};
+    if (r.positions) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      int p = pos;
-      if (r.positions) {
-        const int axis = r.axis ? min(max(r.axis[8 * lane + e], 0), r.n_axes - 1) : 0;
-        p = r.positions[(long)axis * c.T + t];
+      for (int x = 0; x < 4; ++x) p[x] = r.positions[(long)min(x, r.n_axes - 1) * c.T + t];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int pair = FAR ? 8 * lane + 4 * h : 4 * lane + h * (r.R / 4);       // and three behind it
+      int axis[4] = {0, 0, 0, 0};
+      if (r.axis) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) axis[e] = r.axis[pair + e];
       }
-      w[e] = turn_of((uint64_t)(int64_t)p * r.steps[8 * lane + e], r.magnitude);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = axis[e] <= 0 ? p[0] : axis[e] == 1 ? p[1] : axis[e] == 2 ? p[2] : p[3];      // beyond the last axis p repeats it
+        w[4 * h + e] = turn_of((uint64_t)(int64_t)at * r.steps[pair + e], r.magnitude);
+      }
     }
   }
   auto turned = [&](float (&y)[16]) {
@@ -125,44 +138,49 @@ __global__ __launch_bounds__(RT) void rotate_kernel(Paged c, Rotate r) {
     }
   };
   const int rows_q = r.q ? r.heads : 0, rows = rows_q + (r.k ? c.H : 0);
-  // all lanes of a wave stay to the end of the loop where rows exchange their maxima
+  const bool goes = CACHE ? mine && place >= 0 : mine;                 // rows of k and v
+  // row h of q, or, behind those, of k, and of v for a cache
+  struct Raw { u32x4_t x[2], v[2]; };
+  auto request = [&](int h, Raw& f) {
+    f.x[0] = f.x[1] = f.v[0] = f.v[1] = (u32x4_t){};
+    const bool far = h >= rows_q;
+    const long row = far ? t * r.k_pitch + (long)(h - rows_q) * D : t * r.q_pitch + (long)h * D;
+    if (h < rows && (far ? goes : mine)) {
+      load16((far ? r.k : r.q) + row, a, b, f.x);
+      if constexpr (CACHE)
+        if (far) load16(r.v + row, a, b, f.v);
+    }
+  };
+  Raw now;
+  request(first, now);
+  // all lanes of a wave stay to the end of the loop, where rows exchange their maxima; a row is on its way while the one before is turned
   for (int h0 = 0; h0 < rows; h0 += r.step) {
     const int h = h0 + first;
-    const bool has = mine && h < rows;
+    Raw next;
+    request(h + r.step, next);
+    float y[16];
+    unpack16<DT>(now.x, y);
+    turned(y);
     if (h < rows_q) {
-      if (has) {
-        u32x4_t raw[2];
-        float y[16];
-        load16(r.q + t * r.q_pitch + (long)h * D, a, b, raw);
-        unpack16<DT>(raw, y);
-        turned(y);
-        store16<DT>(r.q_out + t * r.q_out_pitch + (long)h * D, a, b, y);
-      }
+      if (mine) store16<DT>(r.q_out + t * r.q_out_pitch + (long)h * D, a, b, y);
     } else {
+      const bool has = goes && h < rows;
       const int g = h - rows_q;
-      u32x4_t raw[2] = {}, raw_v[2] = {};
-      float y[16];
-      const bool goes = CACHE ? has && place >= 0 : has;
-      if (goes) {
-        load16(r.k + t * r.k_pitch + (long)g * D, a, b, raw);
-        if constexpr (CACHE) load16(r.v + t * r.k_pitch + (long)g * D, a, b, raw_v);
-      }
-      unpack16<DT>(raw, y);
-      turned(y);
       if constexpr (CACHE) {
         const long to = place + ((long)g << c.page_shift);
-        keep(y, goes, to, r.kc, r.ks);
+        keep(y, has, to, r.kc, r.ks);
         if constexpr (CODES) {
-          unpack16<DT>(raw_v, y);
-          keep(y, goes, to, r.vc, r.vs);
-        } else if (goes) {
-          *(u32x4_t*)((uint16_t*)r.vc + to * D + a) = raw_v[0];
-          *(u32x4_t*)((uint16_t*)r.vc + to * D + b) = raw_v[1];
+          unpack16<DT>(now.v, y);
+          keep(y, has, to, r.vc, r.vs);
+        } else if (has) {
+          *(u32x4_t*)((uint16_t*)r.vc + to * D + a) = now.v[0];
+          *(u32x4_t*)((uint16_t*)r.vc + to * D + b) = now.v[1];
         }
-      } else if (goes) {
+      } else if (has) {
         store16<DT>(r.k_out + t * r.k_out_pitch + (long)g * D, a, b, y);
       }
     }
+    now = next;
   }
 }
 
@@ -171,7 +189,7 @@ hipError_t launch_dim(const Paged& c, Rotate r, hipStream_t stream) {
   constexpr int LANES = D == 64 ? 4 : 8;
   const int rows = (r.q ? r.heads : 0) + (r.k ? c.H : 0);
   r.step = rows;
-  while (r.step > 4 && (long)c.T * r.step * LANES > 256l * 2048) r.step = (r.step + 1) / 2;
+  while (r.step > STEP && (long)c.T * r.step * LANES > 256l * 2048) r.step = (r.step + 1) / 2;
   const unsigned grid = (unsigned)(((long)c.T * r.step * LANES + RT - 1) / RT);
   if (r.interleaved)
     hipLaunchKernelGGL((rotate_kernel<DT, KEPT, D, false>), dim3(grid), dim3(RT), 0, stream, c, r);

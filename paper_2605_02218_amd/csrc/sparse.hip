@@ -405,7 +405,7 @@ __global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, i
 constexpr int BINS = 1024, PASSES = 4, GROUPS = 128;       // 256 neighbouring blocks a group
 struct ChoiceLds {
   int bins[PASSES][BINS];
-  int above[GROUPS], equal[GROUPS];
+  int above[GROUPS];
   int counts[16][4], found[PASSES][4];
 };
 template <int THREADS>
@@ -440,41 +440,65 @@ __device__ __forceinline__ Part part_of(const int (&own)[N], int need) {
   }
   return Part{from * N + __builtin_amdgcn_readlane(bin, from), __builtin_amdgcn_readlane(before, from), __builtin_amdgcn_readlane(here, from)};
 }
-// Blocks taken, ascending, through put(place, block); their number is returned.  All threads.
+// What a thread has seen of the keys.
+struct Seen { uint32_t lo = kAlways, hi = 0; int always = 0, there = 0; };
+__device__ __forceinline__ void see(Seen& s, const u32x4_t& k) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t x = k[e];
+    s.always += x == kAlways;
+    s.there += x != kNone;
+    s.lo = min(s.lo, x - 1 < kAlways - 1 ? x : kAlways);
+    s.hi = max(s.hi, x == kAlways ? 0u : x);
+  }
+}
+__device__ __forceinline__ Seen over_wave(const Seen& s) {
+  Seen r;
+  r.lo = ~wave_top(~s.lo);
+  r.hi = wave_top(s.hi);
+  r.always = __builtin_amdgcn_readlane(wave_inscan(s.always), 63);
+  r.there = __builtin_amdgcn_readlane(wave_inscan(s.there), 63);
+  return r;
+}
+// Of a lane's four keys those above `at` and, 16 bits further up, those at it.
+__device__ __forceinline__ int above_and_at(const u32x4_t& k, uint32_t at, bool ties) {
+  int n = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) n += k[e] > at ? 1 : ties && k[e] == at ? 1 << 16 : 0;
+  return n;
+}
+// The lane's taken ones of blocks b .. b + 3, with `ups` above `at` and `eqs` at it in front of them.
+template <typename F>
+__device__ __forceinline__ void put_taken(const u32x4_t& k, int b, uint32_t at, bool ties, int more, int ups, int eqs, F put) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool is_up = k[e] > at, is_eq = ties && k[e] == at;
+    if (is_up || (is_eq && eqs < more)) put(ups + min(eqs, more), b + e);
+    ups += is_up;
+    eqs += is_eq;
+  }
+}
+// Blocks taken, ascending, through put(place, block); their number is returned.  All threads, with what they have seen of all keys between them.
 template <int THREADS, typename F>
-__device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, ChoiceLds& l, F put) {
+__device__ __forceinline__ int choose(const uint32_t* keys, int count, const Seen& seen, int top, ChoiceLds& l, F put) {
   constexpr int WAVES = THREADS / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), groups = count >> 8;
   const u32x4_t* const mine = (const u32x4_t*)keys + lane;             // of group x: mine[64 x]
-  uint32_t lo = kAlways, hi = 0;
-  int always = 0, there = 0;
-  for (int x = wave; x < groups; x += WAVES) {
-    const u32x4_t k = mine[64 * x];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      always += k[e] == kAlways;
-      there += k[e] != 0;
-      if (k[e] != 0 && k[e] != kAlways) { lo = min(lo, k[e]); hi = max(hi, k[e]); }
-    }
+  Seen all = over_wave(seen);
+  if (lane == 0) *(i32x4_t*)l.counts[wave] = (i32x4_t){all.always, all.there, (int)all.lo, (int)all.hi};
+  __syncthreads();                                                     // the keys are there as well
+  all = Seen();
+  if (lane < WAVES) {
+    const i32x4_t v = *(const i32x4_t*)l.counts[lane];
+    all.always = v[0];
+    all.there = v[1];
+    all.lo = (uint32_t)v[2];
+    all.hi = (uint32_t)v[3];
   }
-  always = __builtin_amdgcn_readlane(wave_inscan(always), 63);
-  there = __builtin_amdgcn_readlane(wave_inscan(there), 63);
-  lo = ~wave_top(~lo);
-  hi = wave_top(hi);
-  if (lane == 0) *(i32x4_t*)l.counts[wave] = (i32x4_t){always, there, (int)lo, (int)hi};
-  __syncthreads();
-  always = there = 0;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const i32x4_t v = *(const i32x4_t*)l.counts[w];
-    always += v[0];
-    there += v[1];
-    lo = min(lo, (uint32_t)v[2]);
-    hi = max(hi, (uint32_t)v[3]);
-  }
-  uint32_t at = 0;                                // all above it are taken, and `more` of those at it
-  int more = 0, need = top - always;
-  if (there - always > need) {
+  all = over_wave(all);
+  uint32_t lo = all.lo, hi = all.hi, at = 0;      // all above `at` are taken, and `more` of those at it
+  int more = 0, need = top - all.always;
+  if (all.there - all.always > need) {
     at = kAlways - 1;
     for (int pass = 0; need > 0; ++pass) {
       const uint32_t width = hi - lo;
@@ -484,7 +508,7 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, 
         const u32x4_t k = mine[64 * x];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (k[e] >= lo && k[e] <= hi) atomicAdd(&l.bins[pass][(k[e] - lo) >> shift], 1);
+          if (k[e] - lo <= width) atomicAdd(&l.bins[pass][(k[e] - lo) >> shift], 1);
       }
       __syncthreads();
       Part p = {};
@@ -502,7 +526,7 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, 
         if (threadIdx.x == 0) *(i32x4_t*)l.found[pass] = (i32x4_t){p.bin, p.before, p.here, 0};
         __syncthreads();
         const i32x4_t v = *(const i32x4_t*)l.found[pass];
-        p = Part{v[0], v[1], v[2]};
+        p = Part{__builtin_amdgcn_readfirstlane(v[0]), __builtin_amdgcn_readfirstlane(v[1]), __builtin_amdgcn_readfirstlane(v[2])};
       }
       need -= p.before;
       lo += (uint32_t)p.bin << shift;
@@ -513,42 +537,23 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, int top, 
   // in order
   const bool ties = at != 0 && more > 0;
   for (int x = wave; x < groups; x += WAVES) {
-    const u32x4_t k = mine[64 * x];
-    int up = 0, eq = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      up += __popcll(__ballot(k[e] > at));
-      eq += __popcll(__ballot(ties && k[e] == at));
-    }
-    if (lane == 0) { l.above[x] = up; l.equal[x] = eq; }
+    const int n = wave_inscan(above_and_at(mine[64 * x], at, ties));
+    if (lane == 63) l.above[x] = n;
   }
   __syncthreads();
-  int up_before = 0, eq_before = 0;               // in front of the 64 groups at hand
+  int ups = 0, eqs = 0;                           // in front of the 64 groups at hand
   for (int x0 = 0; x0 < groups; x0 += 64) {
-    const int up = x0 + lane < groups ? l.above[x0 + lane] : 0, eq = x0 + lane < groups ? l.equal[x0 + lane] : 0;
-    const int up_upto = wave_inscan(up), eq_upto = wave_inscan(eq);
+    const int n = x0 + lane < groups ? l.above[x0 + lane] : 0, up = n & 0xFFFF, eq = n >> 16, up_upto = wave_inscan(up), eq_upto = wave_inscan(eq);
     for (int i = wave; i < 64 && x0 + i < groups; i += WAVES) {
       const u32x4_t k = mine[64 * (x0 + i)];
-      const int ups = up_before + __builtin_amdgcn_readlane(up_upto - up, i), eqs = eq_before + __builtin_amdgcn_readlane(eq_upto - eq, i);
-      const unsigned long long below = (1ull << lane) - 1;
-      int before_up = ups, before_eq = eqs;       // in front of the lane's four
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        before_up += __popcll(__ballot(k[e] > at) & below);
-        if (ties) before_eq += __popcll(__ballot(k[e] == at) & below);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool is_up = k[e] > at, is_eq = ties && k[e] == at;
-        if (is_up || (is_eq && before_eq < more)) put(before_up + min(before_eq, more), ((x0 + i) * 64 + lane) * 4 + e);
-        before_up += is_up;
-        before_eq += is_eq;
-      }
+      const int own = above_and_at(k, at, ties), front = wave_inscan(own) - own;
+      put_taken(k, ((x0 + i) * 64 + lane) * 4, at, ties, more, ups + __builtin_amdgcn_readlane(up_upto - up, i) + (front & 0xFFFF),
+                eqs + __builtin_amdgcn_readlane(eq_upto - eq, i) + (front >> 16), put);
     }
-    up_before += __builtin_amdgcn_readlane(up_upto, 63);
-    eq_before += __builtin_amdgcn_readlane(eq_upto, 63);
+    ups += __builtin_amdgcn_readlane(up_upto, 63);
+    eqs += __builtin_amdgcn_readlane(eq_upto, 63);
   }
-  return up_before + min(eq_before, more);
+  return ups + min(eqs, more);
 }
 
 // Keys of a lane's four blocks b .. b + 3 of nb as the choice takes them.
@@ -560,7 +565,8 @@ __device__ __forceinline__ u32x4_t keys_of(const Sparse& sp, int nb, int b, u32x
 }
 // A row's scores of an earlier launch into LDS, four loads on their way at a time.
 template <int THREADS>
-__device__ __forceinline__ void take_scores(const Sparse& sp, const uint32_t* scored, int nb, int count, uint32_t* keys) {
+__device__ __forceinline__ Seen take_scores(const Sparse& sp, const uint32_t* scored, int nb, int count, uint32_t* keys) {
+  Seen seen;
   for (int b0 = 4 * threadIdx.x; b0 < count; b0 += 16 * THREADS) {
     u32x4_t k[4];
 #pragma unroll
@@ -572,9 +578,14 @@ __device__ __forceinline__ void take_scores(const Sparse& sp, const uint32_t* sc
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int b = b0 + 4 * THREADS * i;
-      if (b < count) *(u32x4_t*)(keys + b) = keys_of(sp, nb, b, k[i]);
+      if (b < count) {
+        k[i] = keys_of(sp, nb, b, k[i]);
+        see(seen, k[i]);
+        *(u32x4_t*)(keys + b) = k[i];
+      }
     }
   }
+  return seen;
 }
 size_t choice_lds(int blocks) { return sizeof(ChoiceLds) + ((size_t)blocks + 255) / 256 * 256 * sizeof(uint32_t); }
 
@@ -590,9 +601,8 @@ __global__ __launch_bounds__(CHOOSERS) void choose_kernel(Paged c, int max_len, 
   uint32_t* const keys = (uint32_t*)(smem + sizeof(ChoiceLds));
   int32_t* const list = sp.blocks + (long)blockIdx.x * sp.top;
   clear_bins<CHOOSERS>(choice);
-  take_scores<CHOOSERS>(sp, scores + (long)blockIdx.x * pitch, nb, count, keys);
-  __syncthreads();
-  const int taken = choose<CHOOSERS>(keys, count, sp.top, choice, [&](int at, int b) { list[at] = b; });
+  const Seen seen = take_scores<CHOOSERS>(sp, scores + (long)blockIdx.x * pitch, nb, count, keys);
+  const int taken = choose<CHOOSERS>(keys, count, seen, sp.top, choice, [&](int at, int b) { list[at] = b; });
   for (int e = taken + (int)threadIdx.x; e < sp.top; e += CHOOSERS) list[e] = -1;
 }
 
@@ -615,30 +625,17 @@ __global__ __launch_bounds__(256) void choose_rows_kernel(Paged c, int max_len, 
     k[i] = (u32x4_t){0, 0, 0, 0};
     if (b < nb) k[i] = *(const u32x4_t*)(scored + b);
   }
-  uint32_t lo = kAlways, hi = 0;
-  int always = 0, there = 0;
+  Seen all;
 #pragma unroll
   for (int i = 0; i < TRIPS; ++i) {
     k[i] = keys_of(sp, nb, 256 * i + 4 * lane, k[i]);
-    if (256 * i < nb) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t x = k[i][e];
-        always += x == kAlways;
-        there += x != kNone;
-        lo = min(lo, x - 1 < kAlways - 1 ? x : kAlways);
-        hi = max(hi, x == kAlways ? 0u : x);
-      }
-    }
+    if (256 * i < nb) see(all, k[i]);
   }
-  always = __builtin_amdgcn_readlane(wave_inscan(always), 63);
-  there = __builtin_amdgcn_readlane(wave_inscan(there), 63);
-  lo = ~wave_top(~lo);
-  hi = wave_top(hi);
-  uint32_t at = 0;
-  int more = 0, need = sp.top - always;
+  all = over_wave(all);
+  uint32_t lo = all.lo, hi = all.hi, at = 0;
+  int more = 0, need = sp.top - all.always;
   int* const mine = bins[wave];
-  if (there - always > need) {
+  if (all.there - all.always > need) {
     at = kAlways - 1;
     while (need > 0) {
       const uint32_t width = hi - lo;
@@ -663,29 +660,16 @@ __global__ __launch_bounds__(256) void choose_rows_kernel(Paged c, int max_len, 
   }
   const bool ties = at != 0 && more > 0;
   int32_t* const list = sp.blocks + item * sp.top;
-  int up_before = 0, eq_before = 0;
-  const unsigned long long below = (1ull << lane) - 1;
+  int ups = 0, eqs = 0;
 #pragma unroll
   for (int i = 0; i < TRIPS; ++i)
     if (256 * i < nb) {
-      int ups = up_before, eqs = eq_before;       // in front of the lane's four
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned long long up = __ballot(k[i][e] > at), eq = __ballot(ties && k[i][e] == at);
-        ups += __popcll(up & below);
-        eqs += __popcll(eq & below);
-        up_before += __popcll(up);
-        eq_before += __popcll(eq);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool is_up = k[i][e] > at, is_eq = ties && k[i][e] == at;
-        if (is_up || (is_eq && eqs < more)) list[ups + min(eqs, more)] = 256 * i + 4 * lane + e;
-        ups += is_up;
-        eqs += is_eq;
-      }
+      const int own = above_and_at(k[i], at, ties), upto = wave_inscan(own), front = upto - own, sum = __builtin_amdgcn_readlane(upto, 63);
+      put_taken(k[i], 256 * i + 4 * lane, at, ties, more, ups + (front & 0xFFFF), eqs + (front >> 16), [&](int place, int b) { list[place] = b; });
+      ups += sum & 0xFFFF;
+      eqs += sum >> 16;
     }
-  for (int e = up_before + min(eq_before, more) + lane; e < sp.top; e += 64) list[e] = -1;
+  for (int e = ups + min(eqs, more) + lane; e < sp.top; e += 64) list[e] = -1;
 }
 
 // ---- attention over the choice
@@ -733,6 +717,23 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   const int tid = threadIdx.x, lane = tid & 63, kw = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane / M;
   const int G = a.heads / c.H, shift = c.page_shift, page_mask = (1 << shift) - 1;
   const int g = blockIdx.x % c.H, x = blockIdx.x / c.H, t = x % c.T, piece = x / c.T, h0 = blockIdx.y * M;
+  // what goes by the row's number alone is on its way first: a given list, the queries
+  const int begin = piece * ls.span, end = min(begin + ls.span, sp.top << shift);
+  const int e0 = begin >> shift, entries = ((end - 1) >> shift) - e0 + 1;
+  int32_t* const list = sp.blocks + ((long)t * c.H + g) * sp.top;
+  int listed = -1;
+  if (ls.from == GIVEN && tid < entries) listed = list[e0 + tid];
+  const int in_tile = lane % M, rg = h0 + in_tile, head = g * G + rg;
+  const bool has = rg < G;
+  const float unit = fmaxf(fabsf(a.scale), 1.2e-38f), c2 = unit * kLog2E;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;             // a negative scale negates the query
+  u32x4_t raw_q[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    raw_q[k] = (u32x4_t){};
+    if (has) raw_q[k] = *(const u32x4_t*)((const uint16_t*)a.q + t * a.q_pitch + (long)head * D + KM * k + 8 * grp);
+  }
+
   Row row;
   if (!row_of(c, t, row)) return;
   const int hi = seen_end(c, row, t - row.row0, a.max_len, a.visible != nullptr);
@@ -740,19 +741,17 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   const unsigned long long bits = a.visible ? (unsigned long long)a.visible[t] : 0;
 
   // ---- the piece's blocks
-  const int begin = piece * ls.span, end = min(begin + ls.span, sp.top << shift);
-  const int e0 = begin >> shift, entries = ((end - 1) >> shift) - e0 + 1;
-  int32_t* const list = sp.blocks + ((long)t * c.H + g) * sp.top;
   if (tid == 0) list_end = 0;
   if (ls.from == GIVEN) {
-    for (int e = tid; e < entries; e += 64 * KW) list_block[e] = list[e0 + e];
+    for (int e = tid; e < entries; e += 64 * KW) list_block[e] = e == tid ? listed : list[e0 + e];
   } else {
     const int nb = blocks_up_to(c, hi), count = (nb + 255) & ~255;
     ChoiceLds& choice = *(ChoiceLds*)smem;
     uint32_t* const keys = (uint32_t*)(smem + sizeof(ChoiceLds));
+    Seen seen;
     clear_bins<256>(choice);
     if (ls.from == SCORES) {
-      take_scores<256>(sp, ls.scores + ((long)t * c.H + g) * ls.pitch, nb, count, keys);
+      seen = take_scores<256>(sp, ls.scores + ((long)t * c.H + g) * ls.pitch, nb, count, keys);
     } else {
       constexpr int NT = M == 16 ? 1 : 4;
       Scored<D> next;
@@ -773,16 +772,17 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
         if (b0 < nb) {
           score_blocks<D, NT>(now, codes, 16 * NT, G, [&](int, int j, u32x4_t scored) {
             const int b = b0 + 16 * j + 4 * (lane >> 4);
-            *(u32x4_t*)(keys + b) = keys_of(sp, nb, b, scored);
+            scored = keys_of(sp, nb, b, scored);
+            see(seen, scored);
+            *(u32x4_t*)(keys + b) = scored;
           });
         } else {
           keys[b0 + lane] = kNone;
         }
       }
     }
-    __syncthreads();
     const bool writes = piece == 0 && blockIdx.y == 0;
-    const int taken = choose<256>(keys, count, sp.top, choice, [&](int at, int b) {
+    const int taken = choose<256>(keys, count, seen, sp.top, choice, [&](int at, int b) {
       if (at >= e0 && at < e0 + entries) list_block[at - e0] = b;
       if (writes) list[at] = b;
     });
@@ -805,17 +805,9 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   const int stop = min(end, (e0 + __builtin_amdgcn_readfirstlane(list_end)) << shift);
   const int count = max(stop - begin + KT - 1, 0) / KT, mine = kw < count ? (count - kw + KW - 1) / KW : 0;
 
-  const int in_tile = lane % M, rg = h0 + in_tile, head = g * G + rg;
-  const bool has = rg < G;
-  const float unit = fmaxf(fabsf(a.scale), 1.2e-38f), c2 = unit * kLog2E;
-  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;             // a negative scale negates the query
   vec q[KS];
 #pragma unroll
-  for (int k = 0; k < KS; ++k) {
-    u32x4_t w = {};
-    if (has) w = *(const u32x4_t*)((const uint16_t*)a.q + t * a.q_pitch + (long)head * D + KM * k + 8 * grp) ^ flip;
-    q[k] = __builtin_bit_cast(vec, w);
-  }
+  for (int k = 0; k < KS; ++k) q[k] = __builtin_bit_cast(vec, raw_q[k] ^ flip);
 
   // ---- tiles into LDS
   const unsigned base = (unsigned)(uintptr_t)(lds_char*)smem + kw * 2 * STAGE;

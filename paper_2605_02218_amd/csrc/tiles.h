@@ -91,17 +91,6 @@ __device__ __forceinline__ float over_groups(float x, F f) {
 template <int M> __device__ __forceinline__ float row_max(float x) { return over_groups<M>(x, [](float a, float b) { return fmaxf(a, b); }); }
 template <int M> __device__ __forceinline__ float row_sum(float x) { return over_groups<M>(x, [](float a, float b) { return a + b; }); }
 
-// Sums of the lanes up to each, in six steps.
-__device__ __forceinline__ int wave_inscan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-  return v;
-}
-
 // Pool to LDS, 16 or 4 bytes a lane: to `lds` + lane * 16 (4).  Written out because the compiler, where it knows of such a load, waits for all
 // of them in front of the first transposing read; here the waits are the kernel's own (wait_loads).  No register is loaded.  s_nop: five cycles
 // between a vector instruction that wrote the address' scalar registers and this, one behind m0, which nothing else here uses.
