@@ -677,7 +677,9 @@ def _stream_of(index: int) -> int:
 def _call_on(dev, fn, *args):
     """fn(*args, stream) with `dev` current, on its current stream."""
     torch = _types()["torch"]
-    if torch.cuda.current_device() == dev.index:
+    # the device of a tensor's runtime is initialised: asked without the check for that, which takes longer than the question
+    now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    if now() == dev.index:
         return fn(*args, _stream_of(dev.index))
     with torch.cuda.device(dev):
         return fn(*args, _stream_of(dev.index))

@@ -196,7 +196,9 @@ __device__ __forceinline__ Two32 exscan2_32(Two32 v, Two32* sums, Two32* total) 
   return Two32{__builtin_amdgcn_readlane(ups_a - mine.a, at) + a - v.a, __builtin_amdgcn_readlane(ups_b - mine.b, at) + b - v.b};
 }
 
-__global__ __launch_bounds__(PT) void pages_few_kernel(Pages p) {
+// ALL: pages and rows as well; else the sums go to the workspace, as those of pages_plan_kernel.
+template <bool ALL>
+__global__ __launch_bounds__(PT) void pages_few_kernel(Pages p, int* __restrict__ ws) {
   __shared__ Two32 sums[2][PT / 64];
   __shared__ int keep_of[kFewSeq], held_of[kFewSeq], given_of[kFewSeq + 1], asked_of[kFewSeq], length_of[kFewSeq], start_of[kFewSeq + 1], filled;
   const int s = threadIdx.x;
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(PT) void pages_few_kernel(Pages p) {
   u.given = total.a;
   u.there = min(u.before + u.given, p.n_pages);
   const bool served = asks == 0 || front.b + asks <= u.there, ok = fits && served;
-  const int now = ok ? need : held, n = ok ? min(rows, p.T + 1) : 0;                   // 1024 (4096 + 1) rows at most
+  const int now = ok ? need : held, n = ok ? min(rows, p.T + 1) : 0;                   // 2^10 (2^20 + 1) rows at most
   const Two32 ahead = exscan2_32(Two32{n, served ? asks : 0}, sums[1], &total);
   u.after = u.there - total.b;
   const int upto = ahead.a + n;
@@ -227,14 +229,22 @@ __global__ __launch_bounds__(PT) void pages_few_kernel(Pages p) {
   __syncthreads();
   if (real && upto <= p.T) atomicMax(&filled, upto);
   __syncthreads();
+  const Plan to = plan_at(ws, p.S);
   if (real) {
-    const int start = min(upto, filled), length = ok && room ? want : (int)min((long)want - rows, (long)now << p.page_shift);
-    keep_of[s] = keep;
-    held_of[s] = held;
-    given_of[s] = front.a;
-    asked_of[s] = asks > 0 && served ? front.b : -1;
-    length_of[s] = length;
-    start_of[s + 1] = start;
+    const int start = min(upto, filled), length = ok && room ? want : (int)min((long)want - rows, (long)now << p.page_shift), asked = asks > 0 && served ? front.b : -1;
+    if constexpr (ALL) {
+      keep_of[s] = keep;
+      held_of[s] = held;
+      given_of[s] = front.a;
+      asked_of[s] = asked;
+      length_of[s] = length;
+      start_of[s + 1] = start;
+    } else {
+      to.keep[s] = keep;
+      to.held[s] = held;
+      to.given[s] = front.a;
+      to.asked[s] = asked;
+    }
     p.outcome[s] = ok ? room ? 0 : 2 : 1;
     p.length[s] = length;
     p.start[s + 1] = start;
@@ -244,11 +254,20 @@ __global__ __launch_bounds__(PT) void pages_few_kernel(Pages p) {
   if (s == 0) {
     p.start[0] = 0;
     p.n_free[0] = u.after;
+    if constexpr (!ALL) {
+      to.given[p.S] = u.given;
+      to.scalars[0] = u.before;
+      to.scalars[1] = u.given;
+      to.scalars[2] = u.there;
+      to.scalars[3] = u.after;
+    }
   }
-  __syncthreads();
-  const Plan pl = {keep_of, held_of, given_of, asked_of, nullptr};
-  for (int t = threadIdx.x; t < p.T; t += PT) place_row(p, pl, u, start_of, length_of, filled, t);
-  for (int i = threadIdx.x >> 4; i < p.S; i += PT / 16) move_pages(p, pl, u, i, threadIdx.x & 15, 16);
+  if constexpr (ALL) {
+    __syncthreads();
+    const Plan pl = {keep_of, held_of, given_of, asked_of, nullptr};
+    for (int t = threadIdx.x; t < p.T; t += PT) place_row(p, pl, u, start_of, length_of, filled, t);
+    for (int i = threadIdx.x >> 4; i < p.S; i += PT / 16) move_pages(p, pl, u, i, threadIdx.x & 15, 16);
+  }
 }
 
 constexpr int MT = 256;
@@ -256,8 +275,17 @@ __global__ __launch_bounds__(MT) void pages_move_kernel(Pages p, int* __restrict
   const Plan pl = plan_at(ws, p.S);
   const Sums u = {pl.scalars[0], pl.scalars[1], pl.scalars[2], pl.scalars[3]};
   if ((int)blockIdx.x < row_groups) {
+    // where the sequences begin is looked up in LDS, where a step of the search takes a fifth of the time
+    __shared__ int starts[kFewSeq + 1];
+    const int total = p.start[p.S];
+    const bool near = p.S <= kFewSeq && (int)(blockIdx.x * MT) < total;
+    if (near) {
+      for (int s = threadIdx.x; s <= p.S; s += MT) starts[s] = p.start[s];
+      __syncthreads();
+    }
+    const int* const start = near ? starts : p.start;
     const int t = blockIdx.x * MT + threadIdx.x;
-    if (t < p.T) place_row(p, pl, u, p.start, p.length, p.start[p.S], t);
+    if (t < p.T) place_row(p, pl, u, start, p.length, total, t);
   } else {
     const int s = (blockIdx.x - row_groups) * (MT / 64) + threadIdx.x / 64;
     if (s < p.S) move_pages(p, pl, u, s, threadIdx.x & 63, 64);
@@ -270,10 +298,13 @@ size_t pages_workspace_bytes(int S) { return ((size_t)4 * S + 1 + 4) * sizeof(in
 
 hipError_t launch_pages(const Pages& p, void* ws, hipStream_t stream) {
   if (p.S <= kFewSeq && p.T <= kFewRows) {
-    hipLaunchKernelGGL(pages_few_kernel, dim3(1), dim3(PT), 0, stream, p);
+    hipLaunchKernelGGL(pages_few_kernel<true>, dim3(1), dim3(PT), 0, stream, p, (int*)ws);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(pages_plan_kernel, dim3(1), dim3(PT), 0, stream, p, (int*)ws);
+  if (p.S <= kFewSeq && p.T <= 1 << 20)          // sums of 2^10 of these stay below 2^31
+    hipLaunchKernelGGL(pages_few_kernel<false>, dim3(1), dim3(PT), 0, stream, p, (int*)ws);
+  else
+    hipLaunchKernelGGL(pages_plan_kernel, dim3(1), dim3(PT), 0, stream, p, (int*)ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int row_groups = p.slots || p.positions ? (p.T + MT - 1) / MT : 0;

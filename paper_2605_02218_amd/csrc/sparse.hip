@@ -47,6 +47,16 @@ __device__ __forceinline__ int blocks_up_to(const Paged& c, int end) { return (i
 
 // ---- summaries
 
+__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));      // row_shr 1, 2, 4, 8
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, true));      // row_bcast 15, 31
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, true));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 template <int DT, int KEPT, int D> struct Piece {
   static constexpr bool CODES = KEPT != DT;
   static constexpr int N = CODES ? 16 : 8;             // channels of a lane: 16 bytes
@@ -107,7 +117,7 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
   const long first = ((long)page * c.H + g) << shift;
   const int piece = lane % LANES, row = lane / LANES;
   float top[N], low[N];
-  uint32_t size = 0;                              // largest magnitude, as bits
+  float bad = 0.f;                                // NaN once a number is not finite
 #pragma unroll
   for (int e = 0; e < N; ++e) { top[e] = -INFINITY; low[e] = INFINITY; }
   if (piece * N < D) {
@@ -143,7 +153,7 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
         for (int e = 0; e < N; ++e) {
           top[e] = fmaxf(top[e], v[e]);
           low[e] = fminf(low[e], v[e]);
-          size = max(size, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+          bad = __builtin_fmaf(v[e], 0.f, bad);
         }
       }
     }
@@ -153,7 +163,11 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
     top[e] = over_rows<LANES>(top[e], [](float x, float y) { return fmaxf(x, y); });
     low[e] = over_rows<LANES>(low[e], [](float x, float y) { return fminf(x, y); });
   }
-  size = wave_max(size);
+  float most = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (piece * N < D) most = fmaxf(most, fmaxf(top[e], -low[e]));
+  uint32_t size = wave_top(__any(bad != 0.f || bad != bad) ? 0x7FC00000u : __float_as_uint(most));     // largest magnitude, as bits
   if constexpr (WAVES > 1) {
     if (row == 0 && piece * N < D) {
 #pragma unroll
@@ -411,15 +425,6 @@ struct ChoiceLds {
 template <int THREADS>
 __device__ __forceinline__ void clear_bins(ChoiceLds& l) {
   for (int i = threadIdx.x; i < PASSES * BINS / 4; i += THREADS) ((i32x4_t*)l.bins)[i] = (i32x4_t){0, 0, 0, 0};
-}
-__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));      // row_shr 1, 2, 4, 8
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, true));      // row_bcast 15, 31
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, true));
-  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 // Where the `need`-th largest of counted keys lies: the part, how many are beyond it, how many in it.  N parts for each lane, `own`, in the order of the lanes.
 struct Part { int bin, before, here; };
@@ -1171,15 +1176,12 @@ int run_of(int G) {
 // Workgroups of the attention at work at once, by their LDS: 128 KB of tiles, or half of it.
 int slots_of(const Paged& c) { return c.kept == c.dtype && c.D > 64 ? 256 : 512; }
 
-#ifndef PIECE
-#define PIECE 512
-#endif
 struct Pieces { int pieces, span; };
 Pieces pieces_of(const Paged& c, int heads, int top) {
   const int G = heads / c.H, M = G <= 16 ? 16 : 32;
   const long items = (long)c.T * c.H * ((G + M - 1) / M), positions = (long)top << c.page_shift;
   const int slots = slots_of(c);
-  long pieces = 2 * items > slots ? 1 : std::max(1l, std::min<long>(slots / items, positions / PIECE));
+  long pieces = 2 * items > slots || positions < 2048 ? 1 : std::min<long>(slots / items, positions / 512);
   long span = ((positions + pieces - 1) / pieces + 127) / 128 * 128;
   pieces = (positions + span - 1) / span;
   return Pieces{(int)pieces, (int)span};
@@ -1191,7 +1193,12 @@ size_t key_bytes(const Paged& c, int max_len, const Sparse& sp) {
 }
 
 // Which way the choice goes: by each item's own workgroup where there are enough of them.
-int choice_from(const Paged& c, int max_len, const Sparse& sp) { return sp.given ? GIVEN : (long)c.T * c.H >= 256 && 2l * c.T <= 3l * c.S && blocks_of(c, max_len) <= OWN_BLOCKS ? WHOLE : SCORES; }
+int choice_from(const Paged& c, int max_len, const Sparse& sp) {
+  if (sp.given) return GIVEN;
+  const long nb = blocks_of(c, max_len), row = (long)c.D * (c.kept == c.dtype ? 2 : 1);
+  const bool alone = 2l * c.T <= 3l * c.S, cheap = (long)c.T * c.H <= slots_of(c) && nb * (2 * c.D + 4) * 4 <= ((long)sp.top << c.page_shift) * 2 * row;
+  return (long)c.T * c.H >= 256 && nb <= OWN_BLOCKS && (alone || cheap) ? WHOLE : SCORES;
+}
 
 template <int DT, int D>
 hipError_t launch_scores(const Paged& c, const Attend& a, const Sparse& sp, uint32_t* keys, hipStream_t stream) {
@@ -1293,7 +1300,7 @@ static long touched_pages(const Paged& c, bool* by_row) {
 
 bool summary_fits(const Paged& c) {
   bool by_row;
-  return (double)touched_pages(c, &by_row) * c.H * (c.page_shift >= 8 ? 256 : 64) < 4e9;
+  return (double)touched_pages(c, &by_row) * c.H * 256 < 4e9;
 }
 
 hipError_t launch_summary(const Paged& c, const void* kc, const float* ks, int8_t* summary, float* scales, hipStream_t stream) {
