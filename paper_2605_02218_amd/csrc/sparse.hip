@@ -16,27 +16,28 @@ namespace {
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
-// Rows and lengths as covspec_attend takes them.  t uniform in the wave; false: a padding row.  Starts and lengths of 64 sequences come at once, so that a row of
-// the first 63 takes one load's time.
+// Rows and lengths as covspec_attend takes them.  t uniform in the wave; false: a padding row.  The sequence is the last one that begins at or in front of t: of 64
+// starts at a time, every 64th part's first while there are more, then all of them with their lengths, so that up to 63 sequences take one load's time.
 struct Row { int s, row0, n, old; };
 __device__ __forceinline__ bool row_of(const Paged& c, int t, Row& r) {
   const int lane = threadIdx.x & 63;
-  if (t >= c.T) return false;
-  for (int s0 = c.S > 1024 ? max(seq_of(c.start, c.S, t), 0) & ~63 : 0; s0 < c.S; s0 += 64) {
-    const int start = s0 + lane <= c.S ? c.start[s0 + lane] : 0x7FFFFFFF, len = c.length[min(s0 + lane, c.S - 1)];
-    const int at = __popcll(__ballot(start <= t)) - 1;                  // the last one that begins at or in front of t, if it lies here
+  int first = 0, n = c.S + 1;                     // it is one of these
+  while (n > 64) {
+    const int step = (n + 63) / 64, i = lane * step;
+    const int at = __popcll(__ballot(i < n && c.start[first + min(i, n - 1)] <= t)) - 1;
     if (at < 0) return false;
-    const bool last = at == 63;
-    if (last && s0 + 64 <= c.S && c.start[s0 + 64] <= t) continue;
-    r.s = s0 + at;
-    if (r.s >= c.S) return false;
-    r.row0 = min(max(__builtin_amdgcn_readlane(start, at), 0), c.T);
-    const int end = last ? c.start[r.s + 1] : __builtin_amdgcn_readlane(start, at + 1);
-    r.n = max(min(end, c.T), r.row0) - r.row0;
-    r.old = (int)max((long)__builtin_amdgcn_readlane(len, at) - r.n, -(1l << 30));
-    return true;
+    first += at * step;
+    n = min(step, n - at * step);
   }
-  return false;
+  const int s = min(first + lane, c.S), start = c.start[s], len = c.length[min(s, c.S - 1)];
+  const int at = __popcll(__ballot(lane < n && start <= t)) - 1;
+  r.s = first + at;
+  if (at < 0 || r.s >= c.S || t >= c.T) return false;
+  r.row0 = min(max(__builtin_amdgcn_readlane(start, at), 0), c.T);
+  const int end = at == 63 ? c.start[r.s + 1] : __builtin_amdgcn_readlane(start, at + 1);
+  r.n = max(min(end, c.T), r.row0) - r.row0;
+  r.old = (int)max((long)__builtin_amdgcn_readlane(len, at) - r.n, -(1l << 30));
+  return true;
 }
 // End of what row i of the chunk sees.
 __device__ __forceinline__ int seen_end(const Paged& c, const Row& r, int i, int max_len, bool tree) {
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const
     int left = x;
     for (int s0 = 0; s0 < c.S && s < 0; s0 += 64) {
       const int mine = min(s0 + lane, c.S - 1), row0 = min(max(c.start[mine], 0), c.T), n = max(min(c.start[mine + 1], c.T), row0) - row0, length = c.length[mine];
-      const int lo = max(length - n, 0), hi = min(length, cap);
+      const int lo = (int)max((long)length - n, 0l), hi = min(length, cap);
       const int own = s0 + lane < c.S && n > 0 && lo < hi ? ((hi - 1) >> shift) - (lo >> shift) + 1 : 0, upto = wave_inscan(own);
       const unsigned long long over = __ballot(upto > left);
       if (over) {

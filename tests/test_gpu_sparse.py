@@ -384,3 +384,72 @@ def test_pools_beyond_four_gigabytes():
     out, _, blocks = C.sparse_attend(C.SparseParams(C.AttendParams(p, 1, 4 * page, 1.0), 2, 1, 1), q, start, length, pages, pool, summary)
     want = (33999.0 * page + 33990.0) / (page + 1)
     assert blocks[0, 0].tolist() == [0, 2] and abs(float(out[0, 0, 0]) - want) <= want * 2.0 ** -8
+
+
+@pytest.mark.parametrize("S", [63, 64, 65, 130, 1100])
+def test_many_sequences(S):
+    """A token or none of each of many sequences; padding in front of none, behind all."""
+    rng = np.random.default_rng(S)
+    new = [int(n) for n in rng.integers(0, 3, S)]
+    new[-1] = 1
+    run(Batch(rng, new, [n + int(rng.integers(0, 130)) for n in new], 16, pad=3), 2, 1, 64, "bf16", "bf16", 4, 1, 1)
+
+
+def test_queries_of_nan_choose_no_page_that_does_not_exist():
+    rng = np.random.default_rng(15)
+    b = Batch(rng, [2, 1], [300, 300], 16)
+    b.pages[0, [2, 5]], b.pages[1, [1, 7]] = -1, b.n_pages
+    import torch
+    import paper_2605_02218_amd as C
+    k, v, q, _ = make(rng, b, 4, 1, 64, "bf16", "bf16")
+    q[0], q[2, 1, 3] = float("nan"), float("inf")
+    codes, scale = summaries(b, k32_of(k), 1, 64)
+    p = C.SparseParams(C.AttendParams(b.params(1, 64, "bf16", "bf16"), 4, 300, 0.1), 9, 1, 1)
+    _, _, got = C.sparse_attend(p, q.cuda(), *b.device(), upload(k, v), (torch.from_numpy(codes).cuda(), torch.from_numpy(scale).cuda()))
+    want = wanted_blocks(b, codes, scale, q.float().numpy(), 4, 1, 9, 1, 1, False, 300)
+    np.testing.assert_array_equal(got.cpu().numpy(), want)
+    assert list(want[0, 0]) == [0, 1, 3, 4, 6, 7, 8, 9, 18] and list(want[2, 0]) == [0, 2, 3, 4, 5, 6, 8, 9, 18]
+
+
+@pytest.mark.parametrize("chosen", [True, False])
+@pytest.mark.parametrize("T,S", [(9, 4), (300, 200)])
+def test_arrays_without_sense_stay_inside_their_memory(chosen, T, S):
+    """Starts that do not ascend, lengths, pages and blocks that are anything: marked memory around everything that is written."""
+    import ctypes
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(T)
+    H, heads, D, page, n_pages, width, top = 2, 4, 64, 16, 30, 6, 5
+    p = C.SparseParams(C.AttendParams(C.CacheParams(S, T, H, D, page, n_pages, width, C.BF16, C.E4M3), heads, page * width, 0.1), top, 1, 1)
+    wild = lambda *n: torch.from_numpy(rng.choice([-2 ** 31, -1, 0, 1, 3, 5, 29, 30, 50, 95, 2 ** 31 - 1], n).astype(np.int32)).cuda()        # noqa: E731
+    for _ in range(4):
+        rooms = []
+
+        def guard(shape, dtype):
+            n = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+            room = torch.full((n + 1024,), 0x5A, dtype=torch.uint8, device="cuda")
+            rooms.append((room, n))
+            return room[512:512 + n].view(dtype).view(shape)
+
+        cache = tuple(guard((n_pages, H, page, D), torch.float8_e4m3fn) for _ in range(2)) + tuple(guard((n_pages, H, page), torch.float32) for _ in range(2))
+        summary = guard((n_pages, H, 2, D), torch.int8), guard((n_pages, H), torch.float32)
+        q, out, lse = guard((T, heads, D), torch.bfloat16), guard((T, heads, D), torch.bfloat16), guard((T, heads), torch.float32)
+        blocks = guard((T, H, top), torch.int32)
+        blocks.copy_(wild(T, H, top))
+        q.copy_(torch.randn(T, heads, D))
+        start, length, pages = wild(S + 1), wild(S), wild(S, width)
+        steps, c = C.rotary_steps(D), p.attend.cache
+        C.rotate_write(C.RotaryParams(S, T, heads, H, D), c, q, q[:, :H], q[:, H:], steps, start, length, pages, cache, q_out=out)
+        C.block_summary(c, start, length, pages, cache, summary)
+        need = C.sparse_workspace_size(p, given=not chosen)
+        ws = torch.full((need + 1024,), 0x5A, dtype=torch.uint8, device="cuda")
+        at = (ws.data_ptr() + 255) // 256 * 256
+        cs = p.c_struct(given=not chosen)
+        st = C.load_library().covspec_sparse_attend(ctypes.byref(cs), q.data_ptr(), start.data_ptr(), length.data_ptr(), pages.data_ptr(), *[t.data_ptr() for t in cache],
+                                                    *[t.data_ptr() for t in summary], None, blocks.data_ptr(), out.data_ptr(), lse.data_ptr(), at, need,
+                                                    torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert st == 0
+        for room, n in rooms:
+            assert bool((room[:512] == 0x5A).all()) and bool((room[512 + n:] == 0x5A).all())
+        assert bool((ws[at - ws.data_ptr() + need:] == 0x5A).all())
