@@ -72,7 +72,8 @@ __device__ __forceinline__ float over_rows(float x, F f) {
   return over_groups<16>(x, f);
 }
 
-// A wave takes a page of a key head, or (WAVES = 4) a workgroup a large one.  BY_ROW: an item is a row, the first of its sequence's on the page does the work;
+// Bound by memory for prompts (8 x 3008 tokens of 8 heads of 128 in 16 bits 11.4 us, 4.3 TB/s), by latency for single tokens (64: 8 us, three loads one behind the other).
+// A wave takes a page of a key head, or (WAVES = 4) a workgroup a large one: four waves on a page of 64 took 20 us instead of 11 for 256 single tokens.  BY_ROW: an item is a row, the first of its sequence's on the page does the work;
 // else items are the pages that each sequence's rows touch, one sequence behind the other.
 template <int DT, int KEPT, int D, int WAVES, bool BY_ROW>
 __global__ __launch_bounds__(256) void summary_kernel(Paged c, long items, const void* __restrict__ kc, const float* __restrict__ ks, int8_t* __restrict__ summary,
@@ -366,7 +367,9 @@ __device__ __forceinline__ void score_blocks(const Scored<D>& b, const Codes<D, 
   }
 }
 
-// Scores of few rows, their blocks spread over the device: a workgroup takes 256 blocks for as many tokens of a sequence as 16 NT columns hold.
+// Scores in a launch of their own, the blocks spread over the device: a workgroup takes 256 blocks for as many tokens of a sequence as 16 NT columns hold, whose codes each
+// wave makes for itself.  Bound by vector instructions, 14 for a score, where the columns are full (8 tokens of 8 heads for each key head, 16 sequences of 375 to 1500 blocks:
+// 23 us, 31 MB of summaries), else by latency: 5 us for a token's 2001 blocks, 8 for four tokens' 15626.
 constexpr int SCORED = 256;
 template <int DT, int D, int NT>
 __global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, int chunks, int pitch, const int8_t* __restrict__ summary,
@@ -612,7 +615,8 @@ __global__ __launch_bounds__(CHOOSERS) void choose_kernel(Paged c, int max_len, 
   for (int e = taken + (int)threadIdx.x; e < sp.top; e += CHOOSERS) list[e] = -1;
 }
 
-// A wave for each row and key head: for many rows of up to 2048 blocks, 32 keys in a lane.  The same steps with 256 parts.
+// A wave for each row and key head: for many rows of up to 2048 blocks, 32 keys in a lane.  The same steps with 256 parts; nobody waits for others (1024 rows of up to
+// 1500 blocks 8.3 us, by workgroups of four waves 9.7).
 constexpr int ROW_BLOCKS = 2048;
 __global__ __launch_bounds__(256) void choose_rows_kernel(Paged c, int max_len, bool tree, Sparse sp, int pitch, const uint32_t* __restrict__ scores) {
   constexpr int TRIPS = ROW_BLOCKS / 256;
@@ -680,11 +684,12 @@ __global__ __launch_bounds__(256) void choose_rows_kernel(Paged c, int max_len, 
 
 // ---- attention over the choice
 
-// An item is the query heads of one key head of one row, M of them, over its blocks one behind the other: positions v = 0 .. top page_size - 1 of a list.  They all
+// Bound by memory: 64 single tokens of 2048 positions each over e4m3, scores and choice included, 75 us, 350 MB, 4.7 TB/s; trees of eight tokens, 1536 positions each over bf16,
+// 113 us, 7.1 TB/s with what rows of a sequence have in common.  An item is the query heads of one key head of one row, M of them, over its blocks one behind the other: positions v = 0 .. top page_size - 1 of a list.  They all
 // see the same.  The list is the caller's (GIVEN), or chosen first: by scores of an earlier launch (SCORES), or by the workgroup's own (WHOLE), for whom keys and values
 // of the choice and all summaries are read at once.  Four waves take every fourth tile of 32; `pieces` workgroups share a long list, sparse_join_kernel adds them up.  Forms of tiles, products and
 // softmax as in the attention over whole caches (attend.hip); what the row does not see is -infinity among the scores and zeros in V.
-constexpr int KT = 32, KW = 4;
+constexpr int KT = 32;
 enum { GIVEN, SCORES, WHOLE };
 struct Listed {
   int pieces, span;                    // span: positions of a piece, a multiple of 128
@@ -694,7 +699,7 @@ struct Listed {
 constexpr int OWN_BLOCKS = 4096;       // of a choice by a workgroup of the attention
 
 
-template <int DT, int KEPT, int D, int M> struct Sizes {
+template <int DT, int KEPT, int D, int M, int KW> struct Sizes {
   typedef Form<DT, KEPT, D> F;
   static constexpr bool CODES = KEPT != DT;
   static constexpr int TILE = KT * F::ROWB, STAGE = 2 * TILE + (CODES ? 8 * KT : 0), SLOT = D * M * 4 + 512;
@@ -702,9 +707,10 @@ template <int DT, int KEPT, int D, int M> struct Sizes {
   static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
 };
 
-template <int DT, int KEPT, int D, int M>
+template <int DT, int KEPT, int D, int M, int KW>
 __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Attend a, Sparse sp, Listed ls, float* __restrict__ part, f32x2_t* __restrict__ stat) {
-  typedef Sizes<DT, KEPT, D, M> Z;
+  typedef Sizes<DT, KEPT, D, M, KW> Z;
+  constexpr int THREADS = 64 * KW;
   typedef Form<DT, KEPT, D> F;
   constexpr bool CODES = KEPT != DT;
   constexpr int VDT = CODES ? DT_BF16 : DT;
@@ -749,15 +755,15 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   // ---- the piece's blocks
   if (tid == 0) list_end = 0;
   if (ls.from == GIVEN) {
-    for (int e = tid; e < entries; e += 64 * KW) list_block[e] = e == tid ? listed : list[e0 + e];
+    for (int e = tid; e < entries; e += THREADS) list_block[e] = e == tid ? listed : list[e0 + e];
   } else {
     const int nb = blocks_up_to(c, hi), count = (nb + 255) & ~255;
     ChoiceLds& choice = *(ChoiceLds*)smem;
     uint32_t* const keys = (uint32_t*)(smem + sizeof(ChoiceLds));
     Seen seen;
-    clear_bins<256>(choice);
+    clear_bins<THREADS>(choice);
     if (ls.from == SCORES) {
-      seen = take_scores<256>(sp, ls.scores + ((long)t * c.H + g) * ls.pitch, nb, count, keys);
+      seen = take_scores<THREADS>(sp, ls.scores + ((long)t * c.H + g) * ls.pitch, nb, count, keys);
     } else {
       constexpr int NT = M == 16 ? 1 : 4;
       Scored<D> next;
@@ -768,13 +774,13 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
         return h < G ? (const uint16_t*)a.q + t * a.q_pitch + (long)(g * G + h) * D : nullptr;
       }, raw);
       if (kw * 64 < nb) load_blocks<D>(c, g, sp.summary, sp.scales, id, next);
-      id = block_id(c, row.s, 256 + kw * 64 + lane, nb);
+      id = block_id(c, row.s, THREADS + kw * 64 + lane, nb);
       Codes<D, NT> codes;
       query_codes<DT, D, NT>(raw, G, codes);
-      for (int b0 = kw * 64; b0 < count; b0 += 256) {
+      for (int b0 = kw * 64; b0 < count; b0 += THREADS) {
         const Scored<D> now = next;
-        if (b0 + 256 < nb) load_blocks<D>(c, g, sp.summary, sp.scales, id, next);
-        id = block_id(c, row.s, b0 + 512 + lane, nb);
+        if (b0 + THREADS < nb) load_blocks<D>(c, g, sp.summary, sp.scales, id, next);
+        id = block_id(c, row.s, b0 + 2 * THREADS + lane, nb);
         if (b0 < nb) {
           score_blocks<D, NT>(now, codes, 16 * NT, G, [&](int, int j, u32x4_t scored) {
             const int b = b0 + 16 * j + 4 * (lane >> 4);
@@ -788,18 +794,18 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
       }
     }
     const bool writes = piece == 0 && blockIdx.y == 0;
-    const int taken = choose<256>(keys, count, seen, sp.top, choice, [&](int at, int b) {
+    const int taken = choose<THREADS>(keys, count, seen, sp.top, choice, [&](int at, int b) {
       if (at >= e0 && at < e0 + entries) list_block[at - e0] = b;
       if (writes) list[at] = b;
     });
-    for (int e = tid; e < sp.top; e += 256)
+    for (int e = tid; e < sp.top; e += THREADS)
       if (e >= taken) {
         if (e >= e0 && e < e0 + entries) list_block[e - e0] = -1;
         if (writes) list[e] = -1;
       }
   }
   __syncthreads();
-  for (int e = tid; e < entries; e += 64 * KW) {
+  for (int e = tid; e < entries; e += THREADS) {
     const int b = list_block[e];
     int page = -1;
     if (b >= 0 && b < c.max_pages && ((long)b << shift) < hi) page = c.pages[(long)row.s * c.max_pages + b];
@@ -1177,6 +1183,9 @@ int run_of(int G) {
 // Workgroups of the attention at work at once, by their LDS: 128 KB of tiles, or half of it.
 int slots_of(const Paged& c) { return c.kept == c.dtype && c.D > 64 ? 256 : 512; }
 
+// Where the items would not fill half of the device their lists are cut, into pieces of 512 positions or more.  us of the attention and of joining, for 16 items of 8192
+// positions (4 rows behind a million, int8): pieces of 256 positions 13.1 and 5.8, of 512 12.2 and 4.2, of 1024 17.7 and 3.9; for 2 items of 1024 positions two pieces 13.5 and
+// 3.9, one piece 17.6 and a launch less.
 struct Pieces { int pieces, span; };
 Pieces pieces_of(const Paged& c, int heads, int top) {
   const int G = heads / c.H, M = G <= 16 ? 16 : 32;
@@ -1193,7 +1202,10 @@ size_t key_bytes(const Paged& c, int max_len, const Sparse& sp) {
   return choice_from(c, max_len, sp) == SCORES ? ((size_t)c.T * c.H * key_pitch(c, max_len) * sizeof(uint32_t) + 255) / 256 * 256 : 0;
 }
 
-// Which way the choice goes: by each item's own workgroup where there are enough of them.
+// Which way the choice goes.  An item's own workgroup scores, chooses and attends (WHOLE) where there is a workgroup for each compute unit and rows do not share their
+// sequence's summaries, or these are little beside the keys and values and all items are at work at once.  us in one launch and in two or three: 64 single tokens behind 9000 to
+// 61000 positions over bf16 120 and 28 + 7 + 97, of head dimension 64 64 and 19 + 54, 256 behind 2000 to 20000 over e4m3 232 and 42 + 205; 12 rows of 32 heads of
+// their own 24.7 and 5 + 21; but 4 tokens each of 64 sequences (2048 items) 107 and 6.6 + 95.
 int choice_from(const Paged& c, int max_len, const Sparse& sp) {
   if (sp.given) return GIVEN;
   const long nb = blocks_of(c, max_len), row = (long)c.D * (c.kept == c.dtype ? 2 : 1);
@@ -1228,15 +1240,17 @@ hipError_t launch_choice(const Paged& c, const Attend& a, const Sparse& sp, int 
   return hipGetLastError();
 }
 
-template <int DT, int KEPT, int D, int M>
+template <int DT, int KEPT, int D, int M, int KW>
 hipError_t launch_form(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream) {
   const Pieces pc = pieces_of(c, a.heads, sp.top);
   int from = choice_from(c, a.max_len, sp);
   const int nb = blocks_of(c, a.max_len), pitch = key_pitch(c, a.max_len);
-    const bool apart = from == SCORES && (nb > OWN_BLOCKS || (long)pc.pieces * nb > 8192 || (slots_of(c) == 256 && (long)c.T * c.H * pc.pieces > 256));
-  const size_t lds = std::max<size_t>(Sizes<DT, KEPT, D, M>::LDS, from == GIVEN || apart ? 0 : choice_lds(nb));
+  // A launch of its own chooses where many pieces, or some thousand workgroups at a compute unit each or two, would do it beside their loads.  us inside and apart:
+  // 2048 items over e4m3 99.5 and 5.3 + 87, 1024 over bf16 125 and 8.6 + 114.5, 768 over e4m3 73.8 and 6 + 67.8; 16 items in 16 pieces of 15626 blocks 104 and 13 + 12.
+  const bool apart = from == SCORES && (nb > OWN_BLOCKS || (long)pc.pieces * nb > 8192 || (long)c.T * c.H * pc.pieces >= 1024);
+  const size_t lds = std::max<size_t>(Sizes<DT, KEPT, D, M, KW>::LDS, from == GIVEN || apart ? 0 : choice_lds(nb));
   static PerDeviceInt raised;
-  hipError_t e = ensure_dynamic_lds(raised, (const void*)sparse_attend_kernel<DT, KEPT, D, M>, lds);
+  hipError_t e = ensure_dynamic_lds(raised, (const void*)sparse_attend_kernel<DT, KEPT, D, M, KW>, lds);
   if (e != hipSuccess) return e;
   if (from == SCORES && (e = launch_scores<DT, D>(c, a, sp, (uint32_t*)ws, stream)) != hipSuccess) return e;
   if (apart) {
@@ -1248,7 +1262,7 @@ hipError_t launch_form(const Paged& c, const Attend& a, const Sparse& sp, void* 
   f32x2_t* stat = (f32x2_t*)(part + (size_t)c.T * a.heads * pc.pieces * D);
   const Listed ls{pc.pieces, pc.span, from, pitch, (const uint32_t*)ws};
   const int G = a.heads / c.H;
-  hipLaunchKernelGGL((sparse_attend_kernel<DT, KEPT, D, M>), dim3((unsigned)((long)c.T * c.H * pc.pieces), (G + M - 1) / M), dim3(64 * KW), lds, stream, c, a, sp, ls, part, stat);
+  hipLaunchKernelGGL((sparse_attend_kernel<DT, KEPT, D, M, KW>), dim3((unsigned)((long)c.T * c.H * pc.pieces), (G + M - 1) / M), dim3(64 * KW), lds, stream, c, a, sp, ls, part, stat);
   if ((e = hipGetLastError()) != hipSuccess || pc.pieces == 1) return e;
   const long rows = (long)c.T * a.heads;
   hipLaunchKernelGGL((sparse_join_kernel<DT, D>), dim3((unsigned)((rows + JT / 32 - 1) / (JT / 32))), dim3(JT), 0, stream, c, a, pc.pieces, (const float*)part, (const f32x2_t*)stat);
@@ -1322,8 +1336,17 @@ hipError_t launch_summary(const Paged& c, const void* kc, const float* ks, int8_
 
 hipError_t launch_sparse(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream) {
   return with_forms(c, [&](auto dt, auto kept, auto dim) {
-    if (a.heads / c.H <= 16) return launch_form<dt.value, kept.value, dim.value, 16>(c, a, sp, ws, stream);
-    return launch_form<dt.value, kept.value, dim.value, 32>(c, a, sp, ws, stream);
+    const int G = a.heads / c.H;
+    if constexpr (kept.value == dt.value && dim.value > 64) {
+      // Two waves where the workgroups are more than the compute units: two of them on each, so that one's beginning is hidden by the other's tiles.  us with four
+      // and with two: 1024 items of 1536 positions 121 and 114, 2048 of 2048 402 and 385, of 1024 154 and 135; but 64 workgroups 12 and 14.
+      if ((long)c.T * c.H * ((G + 31) / 32) * pieces_of(c, a.heads, sp.top).pieces > 256) {
+        if (G <= 16) return launch_form<dt.value, kept.value, dim.value, 16, 2>(c, a, sp, ws, stream);
+        return launch_form<dt.value, kept.value, dim.value, 32, 2>(c, a, sp, ws, stream);
+      }
+    }
+    if (G <= 16) return launch_form<dt.value, kept.value, dim.value, 16, 4>(c, a, sp, ws, stream);
+    return launch_form<dt.value, kept.value, dim.value, 32, 4>(c, a, sp, ws, stream);
   });
 }
 
