@@ -620,8 +620,7 @@ class _Laid:
     def _kept(self, key, make):
         block = self.__dict__.get("_block")
         if block is None or block[0] != key:
-            block = (key, make())
-            self.__dict__["_block"] = block
+            block = self.__dict__["_block"] = (key, make())
         return block[1]
 
 
@@ -649,7 +648,10 @@ def _types():
     if not _TORCH:
         import torch
         _TORCH.update({FP32: torch.float32, BF16: torch.bfloat16, FP16: torch.float16, INT8: torch.int8, E4M3: torch.float8_e4m3fn, "i32": torch.int32,
-                       "i64": torch.int64, "f32": torch.float32, "u8": torch.uint8, "torch": torch})
+                       "i64": torch.int64, "f32": torch.float32, "u8": torch.uint8, "torch": torch,
+                       # the current device and a device's current stream, without the checks and objects that cost more than the answers
+                       "runtime": (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                                   getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream))})
     return _TORCH
 
 
@@ -669,17 +671,13 @@ def _same_device(*tensors):
 
 def _stream_of(index: int) -> int:
     """Handle of the current stream of a device: without the stream object around it, which takes 3 us to make, where torch offers that."""
-    torch = _types()["torch"]
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+    return _types()["runtime"][1](index)
 
 
 def _call_on(dev, fn, *args):
     """fn(*args, stream) with `dev` current, on its current stream."""
     torch = _types()["torch"]
-    # the device of a tensor's runtime is initialised: asked without the check for that, which takes longer than the question
-    now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-    if now() == dev.index:
+    if _types()["runtime"][0]() == dev.index:
         return fn(*args, _stream_of(dev.index))
     with torch.cuda.device(dev):
         return fn(*args, _stream_of(dev.index))
@@ -847,24 +845,32 @@ def adjust_logits(p: LogitsParams, z, history, history_start, penalties, prompt_
 # Small calls of these are bound by the host, so what is checked here is checked once for each tensor, and a parameter block is laid out again only after a change.
 def _given(dev, *items):
     """Pointers of contiguous tensors on `dev`, None for None.  Items: (tensor, name, shape, type)."""
-    out = []
+    out, index = [], dev.index
     for t, name, shape, dtype in items:
         if t is None:
             out.append(None)
-            continue
-        if t.dtype is not dtype or t.shape != shape:
+        elif t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+            out.append(t.data_ptr())
+        elif t.dtype is not dtype or t.shape != shape:
             raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
-        if t.device != dev or not t.is_contiguous():
+        else:
             raise ValueError("%s must be a contiguous tensor on %s" % (name, dev))
-        out.append(t.data_ptr())
     return out
 
 
 def _given_rows(dev, t, name, n, heads, dim, dtype):
     """(pointer, pitch) of rows as _rows takes them, on `dev`."""
-    if t.device != dev:
+    if t.get_device() != dev.index:
         raise ValueError("%s must be on %s" % (name, dev))
     return _rows(t, name, n, heads, dim, dtype)
+
+
+def _rows_out(dev, t, name, n, heads, dim, dtype):
+    """(tensor, pointer, pitch) of output rows: the caller's, or new dense ones, of which there is nothing to check."""
+    if t is not None:
+        return (t, *_given_rows(dev, t, name, n, heads, dim, dtype))
+    t = _types()["torch"].empty((n, heads, dim), dtype=dtype, device=dev)
+    return t, t.data_ptr(), heads * dim
 
 
 def _device_of(t):
@@ -875,7 +881,8 @@ def _device_of(t):
 
 def _launch(dev, name, *args):
     """The library's entry point `name` with `dev` current, on its current stream."""
-    st = _call_on(dev, getattr(load_library(), name), *args)
+    fn, index, now, stream = getattr(_lib or load_library(), name), dev.index, *_types()["runtime"]
+    st = fn(*args, stream(index)) if now() == index else _call_on(dev, fn, *args)
     if st != OK:
         raise CovspecError(st, name)
 
@@ -932,16 +939,19 @@ def pages_step(p: PagesParams, state, want, rows, workspace=None, want_slots=Tru
     dev, types = _device_of(want), _types()
     i32, S, T = types["i32"], p.n_seq, p.n_tokens
     wp, wb = _scratch(dev, workspace, pages_workspace_size, p, "covspec_pages_workspace_size")
-    if out is None:
-        # one allocation for what is int32: an allocation takes longer than its part of the split
-        slots = want_slots and T > 0
-        empty = types["torch"].empty
-        parts = empty(3 * S + 1 + (T if slots else 0), dtype=i32, device=dev).split((S + 1, S, S, T) if slots else (S + 1, S, S))
-        out = PagesStep(*parts[:3], empty(T, dtype=types["i64"], device=dev) if slots else None, parts[3] if slots else None)
     one, row = (S,), (T,)
     args = _given(dev, (want, "want", one, i32), (rows, "rows", one, i32), (pages, "pages", (S, p.max_pages), i32), (held, "held", one, i32), (borrowed, "borrowed", one, i32),
-                  (free, "free_pages", (p.n_pages,), i32), (n_free, "n_free", (1,), i32), (out[0], "start", (S + 1,), i32), (out[1], "length", one, i32),
-                  (out[2], "outcome", one, i32), (out[3], "slots", row, types["i64"]), (out[4], "positions", row, i32))
+                  (free, "free_pages", (p.n_pages,), i32), (n_free, "n_free", (1,), i32))
+    if out is None:
+        # one allocation for what is int32: an allocation takes longer than its part of the split
+        slots, empty = want_slots and T > 0, types["torch"].empty
+        whole = empty(3 * S + 1 + (T if slots else 0), dtype=i32, device=dev)
+        parts, at = whole.split((S + 1, S, S, T) if slots else (S + 1, S, S)), whole.data_ptr()
+        out = PagesStep(*parts[:3], empty(T, dtype=types["i64"], device=dev) if slots else None, parts[3] if slots else None)
+        args += [at, at + 4 * (S + 1), at + 4 * (2 * S + 1), out[3].data_ptr() if slots else None, at + 4 * (3 * S + 1) if slots else None]
+    else:
+        args += _given(dev, (out[0], "start", (S + 1,), i32), (out[1], "length", one, i32), (out[2], "outcome", one, i32), (out[3], "slots", row, types["i64"]),
+                       (out[4], "positions", row, i32))
     _launch(dev, "covspec_pages_step", ctypes.byref(p.c_struct()), *args, wp, wb)
     return out
 
@@ -996,11 +1006,10 @@ def rotate(p: RotaryParams, q, k, steps, start=None, length=None, positions=None
         if x is None:
             if out is not None:
                 raise ValueError("%s_out without %s" % (name, name))
-            got += [None, 0, None, 0, None]
+            got += [None, 0, None, None, 0]
             continue
-        out = types["torch"].empty((T, heads, D), dtype=dt, device=dev) if out is None else out
-        got += [*_given_rows(dev, x, name, T, heads, D, dt), *_given_rows(dev, out, name + "_out", T, heads, D, dt), out]
-    qp, q_pitch, qo, q_out_pitch, q_out, kp, k_pitch, ko, k_out_pitch, k_out = got
+        got += [*_given_rows(dev, x, name, T, heads, D, dt), *_rows_out(dev, out, name + "_out", T, heads, D, dt)]
+    qp, q_pitch, q_out, qo, q_out_pitch, kp, k_pitch, k_out, ko, k_out_pitch = got
     args = _rotary_args(dev, p, steps, positions, axis, start, length)
     _launch(dev, "covspec_rotate", ctypes.byref(p.c_struct(q_pitch, k_pitch, q_out_pitch, k_out_pitch)), qp, kp, *args, qo, ko)
     return q_out, k_out
@@ -1021,8 +1030,7 @@ def rotate_write(p: RotaryParams, c: CacheParams, q, k, v, steps, start, length,
     types = _types()
     dt, T, H, D = types[p.dtype], p.n_tokens, p.n_kv_heads, p.head_dim
     qp, q_pitch = _given_rows(dev, q, "q", T, p.n_heads, D, dt)
-    q_out = types["torch"].empty((T, p.n_heads, D), dtype=dt, device=dev) if q_out is None else q_out
-    op, q_out_pitch = _given_rows(dev, q_out, "q_out", T, p.n_heads, D, dt)
+    q_out, op, q_out_pitch = _rows_out(dev, q_out, "q_out", T, p.n_heads, D, dt)
     kp, pitch = _given_rows(dev, k, "k", T, H, D, dt)
     vp, pitch_v = _given_rows(dev, v, "v", T, H, D, dt)
     if pitch != pitch_v:
@@ -1086,14 +1094,17 @@ def sparse_attend(p: SparseParams, q, start, length, pages, cache, summary, visi
     dev, types = _device_of(q), _types()
     dt, empty, T, H = types[c.dtype], types["torch"].empty, c.n_tokens, c.n_kv_heads
     qp, q_pitch = _given_rows(dev, q, "q", T, a.n_heads, c.head_dim, dt)
-    out = empty((T, a.n_heads, c.head_dim), dtype=dt, device=dev) if out is None else out
-    op, out_pitch = _given_rows(dev, out, "out", T, a.n_heads, c.head_dim, dt)
+    out, op, out_pitch = _rows_out(dev, out, "out", T, a.n_heads, c.head_dim, dt)
     batch, pool = _cache_args(dev, c, start, length, pages, cache)
-    if not given:
-        blocks = empty((T, H, p.top), dtype=types["i32"], device=dev) if blocks_out is None else blocks_out
-    more = _given(dev, (visible, "visible", (T,), types["i64"]), (blocks, "blocks", (T, H, p.top), types["i32"]))
+    if given or blocks_out is not None:
+        blocks = blocks if given else blocks_out
+        bp = _given(dev, (blocks, "blocks", (T, H, p.top), types["i32"]))[0]
+    else:
+        blocks = empty((T, H, p.top), dtype=types["i32"], device=dev)
+        bp = blocks.data_ptr()
+    bits = _given(dev, (visible, "visible", (T,), types["i64"]))[0] if visible is not None else None
     made = (None, None) if summary is None else _summary_args(dev, c, summary)
     wp, wb = _scratch(dev, workspace, sparse_workspace_size, p, "covspec_sparse_workspace_size", given)
     lse = empty((T, a.n_heads), dtype=types["f32"], device=dev) if want_lse else None
-    _launch(dev, "covspec_sparse_attend", ctypes.byref(p.c_struct(q_pitch, out_pitch, given)), qp, *batch, *pool, *made, *more, op, None if lse is None else lse.data_ptr(), wp, wb)
+    _launch(dev, "covspec_sparse_attend", ctypes.byref(p.c_struct(q_pitch, out_pitch, given)), qp, *batch, *pool, *made, bits, bp, op, None if lse is None else lse.data_ptr(), wp, wb)
     return out, lse, blocks
