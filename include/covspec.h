@@ -578,8 +578,8 @@ int covspec_adjust_logits(const covspec_logits_params* p, const void* z, const i
  *      page * page_size + position % page_size, and positions [n_tokens]: -1 for padding rows, the slot also where the page is none of the pool's.
  *      slots and positions may be NULL.
  * held, borrowed and n_free outside their ranges count as the nearest value inside; nothing outside the arrays is touched whatever they hold.
- * Limits: n_seq <= 65536, n_seq * max_pages and n_tokens below 2^30, page_size as above: else COVSPEC_UNSUPPORTED.  n_tokens may be 0 (then
- * without slots and positions).  Workspace: covspec_pages_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on
+ * Limits: n_seq <= 65536; n_seq * max_pages, max_pages * page_size, n_pages and n_tokens below 2^30; page_size as above: else COVSPEC_UNSUPPORTED.
+ * n_tokens may be 0 (then nothing is written to slots and positions).  Workspace: covspec_pages_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on
  * `stream`, does not synchronise, allocates nothing; the launches depend on the parameters alone.
  */
 typedef struct covspec_pages_params {
@@ -666,8 +666,9 @@ int covspec_rotate_write(const covspec_rotary_params* p, const covspec_cache_par
  *   summary [n_pages, n_kv_heads, 2, head_dim] int8, summary_scale [n_pages, n_kv_heads] fp32 (DEVICE, the caller's, beside the pool)
  *   channel by channel the largest, then the smallest key of the page (8-bit caches: code * scale in fp32), as codes: with amax = the largest magnitude
  *   of all of them, scale = amax / 127, code = x * ((1 / amax) * 127) to the nearest, ties to even, each operation rounded to fp32 on its own.
- *   amax < 2^-100: codes and scale zero; a key that is not finite: codes zero, scale NaN.  16-byte aligned; 2^40 bytes at most.  Two sequences of a
- *   call that share a page of which they see different positions leave one's summary or the other's, so share whole pages.
+ *   amax < 2^-100: codes and scale zero; a key that is not finite: codes zero, scale NaN.  16-byte aligned.  Limits: those of covspec_cache_write, and
+ *   n_kv_heads times the pages that rows can touch, min(n_tokens, n_tokens / page_size + 2 n_seq), below 15.6 million: else COVSPEC_UNSUPPORTED.  Two
+ *   sequences of a call that share a page of which they see different positions leave one's summary or the other's, so share whole pages.
  *
  * covspec_sparse_attend: for row t and key head g, q_h the group's queries, quantised each like a row of an INT8 cache (codes c_h, scale s_h):
  *   score of block b = max over h of (sum_d max(c_hd largest_d, c_hd smallest_d)) * summary_scale * s_h, the sum of integers exact, then two fp32
@@ -675,13 +676,14 @@ int covspec_rotate_write(const covspec_rotary_params* p, const covspec_cache_par
  *   Of the blocks 0 .. nb - 1 that begin below the end of what the row sees (position + 1; with `visible` that of its chunk's first 64 rows) it takes the
  *   first `first`, the last `recent`, and of the others those with the largest scores, `top` in all: a NaN counts as the largest, ties go to the
  *   lower block, one on a page that does not exist is not taken.
- *   blocks [n_tokens, n_kv_heads, top] int32 the blocks taken, ascending, then -1; with given != 0 they are the caller's instead (those of another
+ *   blocks [n_tokens, n_kv_heads, top] int32 the blocks taken, ascending, then -1; with given == 1 they are the caller's instead (those of another
  *   layer, say) and summary, summary_scale are not read: any order, entries that are no block of the sequence take no part, a block that is
  *   listed twice counts twice.  Written for the rows of the batch; padding rows stay as they were.
  *   out, lse_out: covspec_attend over the positions of these blocks that the row sees (visible, padding, rows that see nothing, positions that do not exist
  *   as there); probabilities keep 16 bits of significand in their product with v in every form but fp16 over an fp16 cache, 11 there.
- * Limits: those of covspec_attend, with window == 0; top from 1 to 1024, first, recent >= 0, first + recent <= top; at most 32768 blocks, as
- * ceil(max_len / page_size) counts them; n_tokens * n_kv_heads * 32768 below 2^40: else COVSPEC_INVALID_ARG (top, first, recent, window) or COVSPEC_UNSUPPORTED.  Workspace:
+ * Limits: those of covspec_attend, with window == 0; top from 1 to 1024, first, recent >= 0, first + recent <= top: else COVSPEC_INVALID_ARG
+ * (COVSPEC_UNSUPPORTED for top > 1024); at most 32768 blocks, as nb = ceil(max_len / page_size) counts them; n_tokens * n_kv_heads below 3.9 million,
+ * and times ceil(nb / 256) below 15.6 million; n_tokens * n_heads below 125 million: else COVSPEC_UNSUPPORTED.  Workspace:
  * covspec_sparse_workspace_size bytes, 256-byte aligned, contents undefined between calls.  Enqueues on `stream`, does not synchronise, allocates
  * nothing; the launches depend on the parameters alone.  The same call gives the same bits.
  */
@@ -693,7 +695,7 @@ typedef struct covspec_sparse_params {
   int32_t top;          /* blocks of a row and key head                          */
   int32_t first;        /* of them the first ones of the sequence                */
   int32_t recent;       /* and the last ones that the row sees                   */
-  int32_t given;        /* != 0: `blocks` is read                                */
+  int32_t given;        /* 1: `blocks` is read; 0: written                        */
 } covspec_sparse_params;
 
 size_t covspec_sparse_workspace_size(const covspec_sparse_params* p);

@@ -325,7 +325,7 @@ __device__ __forceinline__ void load_blocks(const Paged& c, int g, const int8_t*
   const bool there = id >= 0 && id < c.n_pages;
   id = there ? id : 0;
   r.scale = scales[(long)id * c.H + g];
-  if (!there) r.scale = __uint_as_float(kAbsent);
+  r.scale = __uint_as_float(!there ? kAbsent : r.scale != r.scale ? 0x7FC00000u : __float_as_uint(r.scale));       // a NaN of any sign and payload as the canonical one
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const long from = ((long)__shfl(id, 16 * j + (lane & 15), 64) * c.H + g) * 2 * D + 16 * (lane >> 4);
@@ -565,11 +565,11 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, const See
   return ups + min(eqs, more);
 }
 
-// Keys of a lane's four blocks b .. b + 3 of nb as the choice takes them.
+// Keys of a lane's four blocks b .. b + 3 of nb as the choice takes them.  kAlways is left to the first and recent ones, so that no more than `top` are taken whatever lies there.
 __device__ __forceinline__ u32x4_t keys_of(const Sparse& sp, int nb, int b, u32x4_t scored) {
   u32x4_t k;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) k[e] = b + e >= nb ? kNone : b + e < sp.first || b + e >= nb - sp.recent ? kAlways : scored[e];
+  for (int e = 0; e < 4; ++e) k[e] = b + e >= nb ? kNone : b + e < sp.first || b + e >= nb - sp.recent ? kAlways : min(scored[e], kAlways - 1);
   return k;
 }
 // A row's scores of an earlier launch into LDS, four loads on their way at a time.
@@ -1205,12 +1205,14 @@ size_t key_bytes(const Paged& c, int max_len, const Sparse& sp) {
 // Which way the choice goes.  An item's own workgroup scores, chooses and attends (WHOLE) where there is a workgroup for each compute unit and rows do not share their
 // sequence's summaries, or these are little beside the keys and values and all items are at work at once.  us in one launch and in two or three: 64 single tokens behind 9000 to
 // 61000 positions over bf16 120 and 28 + 7 + 97, of head dimension 64 64 and 19 + 54, 256 behind 2000 to 20000 over e4m3 232 and 42 + 205; 12 rows of 32 heads of
-// their own 24.7 and 5 + 21; but 4 tokens each of 64 sequences (2048 items) 107 and 6.6 + 95.
+// their own 24.7 and 5 + 21; but 4 tokens each of 64 sequences (2048 items) 107 and 6.6 + 95.  With fewer items it does so where a workgroup scores a sequence in one or two steps:
+// one token of 32 heads in one launch and in three behind 120 blocks 26.9 and 27.5 (codes 30.4 and 31.2), 250 blocks 27.7 and 28.5 (31.3 and 32.1), 500 blocks 29.9 and 28.6
+// (33.5 and 31.9), 1000 blocks 33.6 and 28.4; 8 tokens behind 250 blocks 29.7 and 30.8, 500 blocks 32.0 and 30.7.
 int choice_from(const Paged& c, int max_len, const Sparse& sp) {
   if (sp.given) return GIVEN;
   const long nb = blocks_of(c, max_len), row = (long)c.D * (c.kept == c.dtype ? 2 : 1);
   const bool alone = 2l * c.T <= 3l * c.S, cheap = (long)c.T * c.H <= slots_of(c) && nb * (2 * c.D + 4) * 4 <= ((long)sp.top << c.page_shift) * 2 * row;
-  return (long)c.T * c.H >= 256 && nb <= OWN_BLOCKS && (alone || cheap) ? WHOLE : SCORES;
+  return (long)c.T * c.H < 256 ? (nb <= 256 ? WHOLE : SCORES) : (nb <= OWN_BLOCKS && (alone || cheap) ? WHOLE : SCORES);
 }
 
 template <int DT, int D>

@@ -453,3 +453,27 @@ def test_arrays_without_sense_stay_inside_their_memory(chosen, T, S):
         for room, n in rooms:
             assert bool((room[:512] == 0x5A).all()) and bool((room[512 + n:] == 0x5A).all())
         assert bool((ws[at - ws.data_ptr() + need:] == 0x5A).all())
+
+
+@pytest.mark.parametrize("heads", [2, 20])
+@pytest.mark.parametrize("new,length,top", [([3], [600], 4), ([2], [6000], 4), ([140], [6000], 4), ([1, 2], [5000, 4800], 40)])
+def test_scales_of_any_nan_come_first_and_choose_no_more_than_top(heads, new, length, top):
+    """A summary's scale that is a NaN of either sign and any payload, quiet or not: the largest score, ties to the lower block, and the list ends where it ends."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(heads + sum(new))
+    b = Batch(rng, new, length, 16)
+    k, v, q, q32 = make(rng, b, heads, 1, 64, "bf16", "bf16")
+    codes, scale = summaries(b, k32_of(k), 1, 64)
+    bits = scale.view(np.uint32)
+    for s in range(b.S):
+        for i, blk in enumerate(range(3, 3 + 2 * 9, 2)):
+            bits[b.pages[s][blk], 0] = [0x7FC00000, 0xFFC00000, 0x7FFFFFFF, 0xFFFFFFFF, 0x7F800001, 0xFF800001, 0x7FFFFFFE, 0xFFFFFFFE, 0x7FA00000][i]
+    p = C.SparseParams(C.AttendParams(b.params(1, 64, "bf16", "bf16"), heads, max(length), 0.1), top, 1, 1)
+    room = torch.full((b.T * top + 512,), 77, dtype=torch.int32, device="cuda")
+    blocks = room[256:256 + b.T * top].view(b.T, 1, top)
+    _, _, got = C.sparse_attend(p, q.cuda(), *b.device(), upload(k, v), (torch.from_numpy(codes).cuda(), torch.from_numpy(scale).cuda()), blocks_out=blocks)
+    want = wanted_blocks(b, codes, scale, q32, heads, 1, top, 1, 1, False, max(length))
+    np.testing.assert_array_equal(got.cpu().numpy()[:sum(new)], want[:sum(new)])
+    assert bool((room[:256] == 77).all()) and bool((room[256 + b.T * top:] == 77).all())
+    assert set(want[0, 0]) >= {0, *range(3, 3 + 2 * min(9, top - 2), 2)}
