@@ -633,7 +633,7 @@ int covspec_rotary_steps(const covspec_rotary_scaling* s, int32_t rotary_dim, ui
  *   positions [n_axes, n_tokens] int32, or NULL: a row's position in its sequence, by start and length, for every axis
  *   axis      [rotary_dim / 2] int32, which of the positions turns a pair; a value outside counts as the nearest axis; NULL: the first, for all
  *   start, length: the batch, as above; padding rows are left as they were.  covspec_rotate with positions may have both NULL: all rows are rotated.
- * Limits: head_dim 64, 96 or 128; rotary_dim a multiple of 16 up to head_dim; n_axes from 1 to 4; n_tokens * (n_heads + n_kv_heads) below 2^30, n_seq
+ * Limits: head_dim 64, 96 or 128; rotary_dim a multiple of 16 up to head_dim; n_axes from 1 to 4; n_tokens * (n_heads + n_kv_heads) below 2^28, n_seq
  * below 2^30; pitches multiples of 8, not below a row; for covspec_rotate_write those of the cache as well (its row_pitch is not used), whose n_seq,
  * n_tokens, n_kv_heads, head_dim and dtype have to be the same.  No workspace; one launch on `stream`, does not synchronise, allocates nothing.
  */

@@ -960,7 +960,7 @@ static int rotary_check(const covspec_rotary_params* p, Paged* c, Rotate* r) {
     if (pitch[i] != 0 && (pitch[i] < (i < 2 ? dq : dk) || pitch[i] % 8 != 0)) return COVSPEC_INVALID_ARG;
   if (p->head_dim != 64 && p->head_dim != 96 && p->head_dim != 128) return COVSPEC_UNSUPPORTED;
   if (p->rotary_dim % 16 != 0 || p->n_axes > 4 || p->n_seq >= 1 << 30) return COVSPEC_UNSUPPORTED;
-  if ((int64_t)p->n_tokens * ((int64_t)p->n_heads + p->n_kv_heads) >= 1 << 30) return COVSPEC_UNSUPPORTED;
+  if ((int64_t)p->n_tokens * ((int64_t)p->n_heads + p->n_kv_heads) >= 1 << 28) return COVSPEC_UNSUPPORTED;      // eight threads a row, fewer than 2^32
   for (const int64_t x : pitch)
     if (x > far) return COVSPEC_UNSUPPORTED;
   *c = Paged{};

@@ -93,7 +93,7 @@ def test_rotations_are_checked():
                        (dict(head_dim=-1), Bd.INVALID_ARG), (dict(rotary_dim=-16), Bd.INVALID_ARG), (dict(rotary_dim=144), Bd.INVALID_ARG), (dict(n_axes=0), Bd.INVALID_ARG),
                        (dict(dtype=C.FP32), Bd.INVALID_ARG), (dict(dtype=C.INT8), Bd.INVALID_ARG), (dict(magnitude=float("nan")), Bd.INVALID_ARG),
                        (dict(magnitude=float("inf")), Bd.INVALID_ARG), (dict(interleaved=2), Bd.INVALID_ARG), (dict(head_dim=80), Bd.UNSUPPORTED), (dict(head_dim=256), Bd.UNSUPPORTED),
-                       (dict(rotary_dim=24), Bd.UNSUPPORTED), (dict(n_axes=5), Bd.UNSUPPORTED), (dict(n_tokens=1 << 26), Bd.UNSUPPORTED), (dict(n_seq=1 << 30), Bd.UNSUPPORTED)]:
+                       (dict(rotary_dim=24), Bd.UNSUPPORTED), (dict(n_axes=5), Bd.UNSUPPORTED), (dict(n_tokens=1 << 26), Bd.UNSUPPORTED), (dict(n_tokens=-(-(1 << 28) // 24)), Bd.UNSUPPORTED), (dict(n_seq=1 << 30), Bd.UNSUPPORTED)]:
         cs = C.RotaryParams(**{**good, **kw}).c_struct()
         assert lib.covspec_rotate(ctypes.byref(cs), *a()) == status, kw
         assert lib.covspec_rotate_write(ctypes.byref(cs), ctypes.byref(cc), *w()) == status, kw
