@@ -685,10 +685,14 @@ __global__ __launch_bounds__(256) void choose_rows_kernel(Paged c, int max_len, 
 // ---- attention over the choice
 
 // Bound by memory: 64 single tokens of 2048 positions each over e4m3, scores and choice included, 75 us, 350 MB, 4.7 TB/s; trees of eight tokens, 1536 positions each over bf16,
-// 113 us, 7.1 TB/s with what rows of a sequence have in common.  An item is the query heads of one key head of one row, M of them, over its blocks one behind the other: positions v = 0 .. top page_size - 1 of a list.  They all
-// see the same.  The list is the caller's (GIVEN), or chosen first: by scores of an earlier launch (SCORES), or by the workgroup's own (WHOLE), for whom keys and values
-// of the choice and all summaries are read at once.  Four waves take every fourth tile of 32; `pieces` workgroups share a long list, sparse_join_kernel adds them up.  Forms of tiles, products and
-// softmax as in the attention over whole caches (attend.hip); what the row does not see is -infinity among the scores and zeros in V.
+// 105 us, 7.7 TB/s with what rows of a sequence have in common.  Few items: by the chain of a tile's instructions, 2500 cycles.  An item is the query heads of one key head of one
+// row, M of them, over its blocks one behind the other: positions v = 0 .. top page_size - 1 of a list.  They all see the same.  The list is the caller's (GIVEN), or chosen
+// first: by scores of an earlier launch (SCORES), or by the workgroup's own (WHOLE), for whom keys and values of the choice and all summaries are read at once.  KW waves take
+// every KW-th tile of 32; `pieces` workgroups share a long list, sparse_join_kernel adds them up.  Forms of tiles, products and softmax as in the attention over whole caches
+// (attend.hip); what the row does not see is -infinity among the scores and zeros in V.
+// A wave has two tiles in LDS, one on its way while the other is computed; 16-bit rows of more than 64 elements one, whose keys are replaced by the next once they are in
+// registers, and its values then: two waves on each unit instead of one that holds twice as much (us of a call, 1024 items of 1536 positions 158 and 149, 512 of 2048 137 and
+// 128, 1024 of 2048 229 and 215).  Four tiles of codes for a wave measured the same for few items.
 constexpr int KT = 32;
 enum { GIVEN, SCORES, WHOLE };
 struct Listed {
@@ -703,7 +707,8 @@ template <int DT, int KEPT, int D, int M, int KW> struct Sizes {
   typedef Form<DT, KEPT, D> F;
   static constexpr bool CODES = KEPT != DT;
   static constexpr int TILE = KT * F::ROWB, STAGE = 2 * TILE + (CODES ? 8 * KT : 0), SLOT = D * M * 4 + 512;
-  static constexpr int TILES = KW * 2 * STAGE, JOIN = (KW - 1) * SLOT;
+  static constexpr bool ONE = !CODES && D > 64;       // room for one tile of a wave, else for two
+  static constexpr int TILES = KW * (ONE ? 1 : 2) * STAGE, JOIN = (KW - 1) * SLOT;
   static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
 };
 
@@ -712,7 +717,7 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   typedef Sizes<DT, KEPT, D, M, KW> Z;
   constexpr int THREADS = 64 * KW;
   typedef Form<DT, KEPT, D> F;
-  constexpr bool CODES = KEPT != DT;
+  constexpr bool CODES = KEPT != DT, ONE = Z::ONE;
   constexpr int VDT = CODES ? DT_BF16 : DT;
   // p (v_scale) in two 16-bit parts, as single tokens of the whole cache have it
   constexpr bool SPLIT_P = CODES || DT == DT_BF16;
@@ -822,7 +827,7 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   for (int k = 0; k < KS; ++k) q[k] = __builtin_bit_cast(vec, raw_q[k] ^ flip);
 
   // ---- tiles into LDS
-  const unsigned base = (unsigned)(uintptr_t)(lds_char*)smem + kw * 2 * STAGE;
+  const unsigned base = (unsigned)(uintptr_t)(lds_char*)smem + kw * (ONE ? 1 : 2) * STAGE;
   // 16 positions of the list from v on: their page (-1: nothing there) and block
   struct Groups { int page[2], block[2]; };
   auto look_up = [&](int tile) {
@@ -835,7 +840,8 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
     }
     return r;
   };
-  auto fetch = [&](int tile, const Groups& w, int stage) {
+  // a tile's keys, values or both (with the scales of codes)
+  auto fetch = [&](int tile, const Groups& w, int stage, bool keys, bool values) __attribute__((always_inline)) {
     const unsigned to = base + stage * STAGE;
     long at[2];
 #pragma unroll
@@ -850,8 +856,8 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
       if (F::PIECES == F::CH || part_of < F::PIECES) {
         const long where = uniform(at[x0 / 16]);
         const unsigned off = (unsigned)xr * (D * F::ESZ) + part_of * 16;
-        load16_lds(to + x0 * F::ROWB, (const char*)a.kc + where * (D * F::ESZ), off);
-        load16_lds(to + TILE + x0 * F::ROWB, (const char*)a.vc + where * (D * F::ESZ), off);
+        if (keys) load16_lds(to + x0 * F::ROWB, (const char*)a.kc + where * (D * F::ESZ), off);
+        if (values) load16_lds(to + TILE + x0 * F::ROWB, (const char*)a.vc + where * (D * F::ESZ), off);
       }
     }
   };
@@ -900,18 +906,20 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
   }
   typedef std::conditional_t<CODES, u32x2_t, u32x4_t> raw_t;
 
-  auto work = [&](uint32_t see, int stage) __attribute__((always_inline)) {
+  // ONE: with the keys of the tile there and its values behind them; `next` is the tile to come, if there is one
+  auto work = [&](uint32_t see, int stage, int tile, const Groups& next, bool more) __attribute__((always_inline)) {
     const lds_char* const kt = (const lds_char*)(base + stage * STAGE);
     lds_char* const vt = (lds_char*)(base + stage * STAGE + TILE);
     const __attribute__((address_space(3))) float* const scales = (const __attribute__((address_space(3))) float*)(base + stage * STAGE + 2 * TILE);
     const bool partial = see != ~0u;
-    if (partial) {                                                     // 0 * v is NaN where v is not finite
+    auto clear_unseen = [&] {                                          // 0 * v is NaN where v is not finite
 #pragma unroll
       for (int i = 0; i < KT * F::CH / 64; ++i) {
         const int y = (i * 64 + lane) / F::CH;
         if (!(see >> y & 1)) *(__attribute__((address_space(3))) u32x4_t*)(vt + (i * 64 + lane) * 16) = (u32x4_t){};
       }
-    }
+    };
+    if (!ONE && partial) clear_unseen();
     raw_t kf[ST][KS];
 #pragma unroll
     for (int st = 0; st < ST; ++st)
@@ -919,6 +927,10 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
       for (int k = 0; k < KS; ++k)
         kf[st][k] = *(const __attribute__((address_space(3))) raw_t*)(kt + (M == 16 ? st / 2 : st) * 32 * F::ROWB + (kbase[M == 16 ? st & 1 : 0] ^ k * KM * F::ESZ));
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (ONE) {
+      wait_lds();
+      if (more) fetch(tile, next, 0, true, false);
+    }
     acc sc[ST];
 #pragma unroll
     for (int st = 0; st < ST; ++st)
@@ -992,7 +1004,7 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
         }
       }
     };
-    load_v(0);
+    if constexpr (!ONE) load_v(0);
     if (__builtin_expect(far, 0)) {
       const float from = m == -INFINITY ? 0.f : m;                     // then all scores are -infinity or NaN: zeros or NaN
 #pragma unroll
@@ -1041,10 +1053,24 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
           if constexpr (SPLIT_P) rest[y][e] = Half<VDT>::pack(a0 - bf16lo_to_f32(prob[y][e]), a1 - bf16hi_to_f32(prob[y][e]));
         }
       }
+    if constexpr (ONE) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) wait_loads<LOADS>(); else wait_loads<0>();
+      __builtin_amdgcn_sched_barrier(0);
+      if (partial) clear_unseen();
+      load_v(0);
+    }
 #pragma unroll
     for (int y = 0; y < NX; ++y) {
       if (y + 1 < NX) load_v(y + 1);
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (ONE) {
+        if (y + 1 == NX) {
+          wait_lds();
+          if (more) fetch(tile, next, 0, false, true);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
 #pragma unroll
       for (int d = 0; d < DM; ++d) {
         u32x4_t w;
@@ -1057,29 +1083,49 @@ __global__ __launch_bounds__(64 * KW, 2) void sparse_attend_kernel(Paged c, Atte
 
   if (mine > 0) {
     Groups now = look_up(kw), next = {};
-    fetch(kw, now, 0);
+    fetch(kw, now, 0, true, !ONE);
+    if constexpr (ONE) fetch(kw, now, 0, false, true);
     if (mine > 1) next = look_up(kw + KW);
     for (int i = 0; i < mine; ++i) {
       const Groups here = now;
-      if (i + 1 < mine) {
-        fetch(kw + (i + 1) * KW, next, (i + 1) & 1);
+      const bool more = i + 1 < mine;
+      const int behind = kw + (i + 1) * KW;                            // the tile to come
+      if constexpr (ONE) {
+        const uint32_t see = seen_in(kw + i * KW, here);
+        wait_loads<LOADS>();                                           // the keys
+        __builtin_amdgcn_sched_barrier(0);
+        if (see != 0) {
+          work(see, 0, behind, next, more);
+        } else {
+          wait_loads<0>();
+          if (more) {
+            fetch(behind, next, 0, true, false);
+            fetch(behind, next, 0, false, true);
+          }
+        }
         now = next;
-        if (i + 2 < mine) next = look_up(kw + (i + 2) * KW);
-        wait_loads<2 * LOADS + (CODES ? 1 : 0)>();
+        if (i + 2 < mine) next = look_up(behind + KW);
       } else {
-        wait_loads<0>();
+        if (more) {
+          fetch(behind, next, (i + 1) & 1, true, true);
+          now = next;
+          if (i + 2 < mine) next = look_up(behind + KW);
+          wait_loads<2 * LOADS + (CODES ? 1 : 0)>();
+        } else {
+          wait_loads<0>();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t see = seen_in(kw + i * KW, here);
+        if (see != 0) work(see, i & 1, 0, next, false);
+        __builtin_amdgcn_sched_barrier(0);
+        wait_lds();                                                    // nothing reads the stage that is filled next
       }
-      __builtin_amdgcn_sched_barrier(0);
-      const uint32_t see = seen_in(kw + i * KW, here);
-      if (see != 0) work(see, i & 1);
-      __builtin_amdgcn_sched_barrier(0);
-      wait_lds();                                                      // nothing reads the stage that is filled next
     }
   }
   sum = row_sum<M>(sum);
   m *= unit;                                                           // in units of the scores
 
-  // ---- the four waves
+  // ---- the waves
   __syncthreads();
   if (kw > 0) {
     char* const to = smem + (kw - 1) * Z::SLOT;
@@ -1180,18 +1226,18 @@ int run_of(int G) {
   return gp;
 }
 
-// Workgroups of the attention at work at once, by their LDS: 128 KB of tiles, or half of it.
+// Workgroups that lists are cut for: two to a compute unit, or one where tiles are 16 KB and two share its loads (192 items of 2048 positions, us of a call: 50.2, cut for 512 53.7).
 int slots_of(const Paged& c) { return c.kept == c.dtype && c.D > 64 ? 256 : 512; }
 
-// Where the items would not fill half of the device their lists are cut, into pieces of 512 positions or more.  us of the attention and of joining, for 16 items of 8192
-// positions (4 rows behind a million, int8): pieces of 256 positions 13.1 and 5.8, of 512 12.2 and 4.2, of 1024 17.7 and 3.9; for 2 items of 1024 positions two pieces 13.5 and
-// 3.9, one piece 17.6 and a launch less.
+// Where the items would not fill half of the device their lists are cut, into up to 16 pieces of 256 positions or more.  us of a call in a graph, one token of 8 key heads over
+// bf16: 1536 positions in one piece 29.9, in six 24.7; 2048 in four 26.2, in eight 25.0; 4096 in eight 26.6, in 16 26.1; 8192 in 16 29.4, in 32 31.0.  1024 positions 26.7 and in
+// four pieces 24.5, but the launch that joins them takes the host 3 us: only tiles of 32 heads, in four waves, are cut there (34.1 and 28.3).
 struct Pieces { int pieces, span; };
 Pieces pieces_of(const Paged& c, int heads, int top) {
   const int G = heads / c.H, M = G <= 16 ? 16 : 32;
   const long items = (long)c.T * c.H * ((G + M - 1) / M), positions = (long)top << c.page_shift;
   const int slots = slots_of(c);
-  long pieces = 2 * items > slots || positions < 2048 ? 1 : std::min<long>(slots / items, positions / 512);
+  long pieces = 2 * items > slots || positions < (M == 16 ? 1536 : 1024) ? 1 : std::min<long>(slots / items, std::min<long>(positions / 256, 16));
   long span = ((positions + pieces - 1) / pieces + 127) / 128 * 128;
   pieces = (positions + span - 1) / span;
   return Pieces{(int)pieces, (int)span};
@@ -1339,14 +1385,10 @@ hipError_t launch_summary(const Paged& c, const void* kc, const float* ks, int8_
 hipError_t launch_sparse(const Paged& c, const Attend& a, const Sparse& sp, void* ws, hipStream_t stream) {
   return with_forms(c, [&](auto dt, auto kept, auto dim) {
     const int G = a.heads / c.H;
-    if constexpr (kept.value == dt.value && dim.value > 64) {
-      // Two waves where the workgroups are more than the compute units: two of them on each, so that one's beginning is hidden by the other's tiles.  us with four
-      // and with two: 1024 items of 1536 positions 121 and 114, 2048 of 2048 402 and 385, of 1024 154 and 135; but 64 workgroups 12 and 14.
-      if ((long)c.T * c.H * ((G + 31) / 32) * pieces_of(c, a.heads, sp.top).pieces > 256) {
-        if (G <= 16) return launch_form<dt.value, kept.value, dim.value, 16, 2>(c, a, sp, ws, stream);
-        return launch_form<dt.value, kept.value, dim.value, 32, 2>(c, a, sp, ws, stream);
-      }
-    }
+    // Eight waves, two on each unit of a compute unit, where there is half a workgroup for each: a tile is 2500 cycles of instructions that wait for one another.  us of a call
+    // with four waves and with eight: a token of 32 / 8 heads 28.7 and 26.1 (head dimension 64 23.7 and 21.2, e4m3 32.3 and 29.2), 16 tokens 28.3 and 26.0; but 32 tokens 40.1
+    // and 41.6, and with tiles of 32 heads 16 tokens of two key heads 35.7 and 40.4.
+    if (G <= 16 && (long)c.T * c.H * pieces_of(c, a.heads, sp.top).pieces <= 128) return launch_form<dt.value, kept.value, dim.value, 16, 8>(c, a, sp, ws, stream);
     if (G <= 16) return launch_form<dt.value, kept.value, dim.value, 16, 4>(c, a, sp, ws, stream);
     return launch_form<dt.value, kept.value, dim.value, 32, 4>(c, a, sp, ws, stream);
   });
