@@ -1249,11 +1249,12 @@ size_t key_bytes(const Paged& c, int max_len, const Sparse& sp) {
 }
 
 // Which way the choice goes.  An item's own workgroup scores, chooses and attends (WHOLE) where there is a workgroup for each compute unit and rows do not share their
-// sequence's summaries, or these are little beside the keys and values and all items are at work at once.  us in one launch and in two or three: 64 single tokens behind 9000 to
-// 61000 positions over bf16 120 and 28 + 7 + 97, of head dimension 64 64 and 19 + 54, 256 behind 2000 to 20000 over e4m3 232 and 42 + 205; 12 rows of 32 heads of
-// their own 24.7 and 5 + 21; but 4 tokens each of 64 sequences (2048 items) 107 and 6.6 + 95.  With fewer items it does so where a workgroup scores a sequence in one or two steps:
-// one token of 32 heads in one launch and in three behind 120 blocks 26.9 and 27.5 (codes 30.4 and 31.2), 250 blocks 27.7 and 28.5 (31.3 and 32.1), 500 blocks 29.9 and 28.6
-// (33.5 and 31.9), 1000 blocks 33.6 and 28.4; 8 tokens behind 250 blocks 29.7 and 30.8, 500 blocks 32.0 and 30.7.
+// sequence's summaries, or these are little beside the keys and values and all items are at work at once.  us of a call and its summaries with the choice in one launch, in two
+// (SCORES), in three (apart, below): 64 single tokens behind 9000 to 61000 positions over bf16 136, 149, 152, of head dimension 64 67, 76, 80, over e4m3 85, 99, 103; 256 behind
+// 2000 to 20000 over e4m3 254, 271, 269; 12 rows of 32 heads of their own 34.5, 35.8, 37.8; but 4 tokens each of 64 sequences (2048 items) over bf16 184, 182, 176.  With fewer
+// items it does so where a workgroup scores a sequence in one or two steps: one token of 32 heads in one launch and in three behind 120 blocks 26.9 and 27.5 (codes 30.4 and
+// 31.2), 250 blocks 27.7 and 28.5 (31.3 and 32.1), 500 blocks 29.9 and 28.6 (33.5 and 31.9), 1000 blocks 33.6 and 28.4; 8 tokens behind 250 blocks 29.7 and 30.8, 500 blocks
+// 32.0 and 30.7 (with four waves each; eight take 2 to 3 us less of all).
 int choice_from(const Paged& c, int max_len, const Sparse& sp) {
   if (sp.given) return GIVEN;
   const long nb = blocks_of(c, max_len), row = (long)c.D * (c.kept == c.dtype ? 2 : 1);
@@ -1293,8 +1294,9 @@ hipError_t launch_form(const Paged& c, const Attend& a, const Sparse& sp, void* 
   const Pieces pc = pieces_of(c, a.heads, sp.top);
   int from = choice_from(c, a.max_len, sp);
   const int nb = blocks_of(c, a.max_len), pitch = key_pitch(c, a.max_len);
-  // A launch of its own chooses where many pieces, or some thousand workgroups at a compute unit each or two, would do it beside their loads.  us inside and apart:
-  // 2048 items over e4m3 99.5 and 5.3 + 87, 1024 over bf16 125 and 8.6 + 114.5, 768 over e4m3 73.8 and 6 + 67.8; 16 items in 16 pieces of 15626 blocks 104 and 13 + 12.
+  // A launch of its own chooses where many pieces, or some thousand workgroups at a compute unit each or two, would do it beside their loads.  us of a call inside and apart:
+  // 2048 items over e4m3 125 and 116, over bf16 182 and 176, 1024 over bf16 114 and 113, 768 over e4m3 68.7 and 68.1; but 512 over bf16 62.1 and 64.4, 256 41.7 and 44.0.  The
+  // attention alone for 16 items in 16 pieces of 15626 blocks: 104, and 13 + 12 apart.
   const bool apart = from == SCORES && (nb > OWN_BLOCKS || (long)pc.pieces * nb > 8192 || (long)c.T * c.H * pc.pieces >= 1024);
   const size_t lds = std::max<size_t>(Sizes<DT, KEPT, D, M, KW>::LDS, from == GIVEN || apart ? 0 : choice_lds(nb));
   static PerDeviceInt raised;
