@@ -943,10 +943,10 @@ def pages_step(p: PagesParams, state, want, rows, workspace=None, want_slots=Tru
     args = _given(dev, (want, "want", one, i32), (rows, "rows", one, i32), (pages, "pages", (S, p.max_pages), i32), (held, "held", one, i32), (borrowed, "borrowed", one, i32),
                   (free, "free_pages", (p.n_pages,), i32), (n_free, "n_free", (1,), i32))
     if out is None:
-        # one allocation for what is int32: an allocation takes longer than its part of the split
+        # one allocation for what is int32: an allocation takes longer than its part of the split (which is unsafe for gradients alone)
         slots, empty = want_slots and T > 0, types["torch"].empty
         whole = empty(3 * S + 1 + (T if slots else 0), dtype=i32, device=dev)
-        parts, at = whole.split((S + 1, S, S, T) if slots else (S + 1, S, S)), whole.data_ptr()
+        parts, at = whole.unsafe_split_with_sizes((S + 1, S, S, T) if slots else (S + 1, S, S)), whole.data_ptr()
         out = PagesStep(*parts[:3], empty(T, dtype=types["i64"], device=dev) if slots else None, parts[3] if slots else None)
         args += [at, at + 4 * (S + 1), at + 4 * (2 * S + 1), out[3].data_ptr() if slots else None, at + 4 * (3 * S + 1) if slots else None]
     else:
