@@ -367,13 +367,16 @@ __device__ __forceinline__ void score_blocks(const Scored<D>& b, const Codes<D, 
   }
 }
 
-// Scores in a launch of their own, the blocks spread over the device: a workgroup takes 256 blocks for as many tokens of a sequence as 16 NT columns hold, whose codes each
-// wave makes for itself.  Bound by vector instructions, 14 for a score, where the columns are full (8 tokens of 8 heads for each key head, 16 sequences of 375 to 1500 blocks:
-// 23 us, 31 MB of summaries), else by latency: 5 us for a token's 2001 blocks, 8 for four tokens' 15626.
+// Scores in a launch of their own, the blocks spread over the device: a workgroup takes 256 blocks for as many tokens of a sequence as 16 NT columns hold; of 64 columns each wave
+// makes the codes of 16 for all (with every wave making all of them 24 us instead of 19 below).  Bound by vector instructions, 9 for a score, where the columns are full (8 tokens
+// of 8 heads for each key head, 16 sequences of 375 to 1500 blocks: 19 us, 31 MB of summaries), else by latency: 5 us for a token's 2001 blocks, 7.5 for four tokens' 15626.
 constexpr int SCORED = 256;
 template <int DT, int D, int NT>
-__global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, int chunks, int pitch, const int8_t* __restrict__ summary,
+__global__ __launch_bounds__(256, 2) void score_kernel(Paged c, Attend a, int gp, int chunks, int pitch, const int8_t* __restrict__ summary,
                                                     const float* __restrict__ scales, uint32_t* __restrict__ keys) {
+  static_assert(NT == 1 || NT == 4, "a wave makes the codes of 16 columns");
+  __shared__ i32x4_t made[NT > 1 ? NT : 1][kSteps<D>][NT > 1 ? 64 : 1];
+  __shared__ f32x2_t factors[NT > 1 ? NT : 1][NT > 1 ? 64 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.heads / c.H, tokens = 16 * NT / gp;
   const long item = blockIdx.x / c.H;
@@ -397,19 +400,40 @@ __global__ __launch_bounds__(256) void score_kernel(Paged c, Attend a, int gp, i
   if (s < 0) return;
   const Row r = {s, row0, n, (int)max((long)len - n, -(1l << 30))};
   const int i1 = min(i0 + tokens, n), nb = blocks_up_to(c, seen_end(c, r, i1 - 1, a.max_len, a.visible != nullptr)), b0 = chunk * SCORED + wave * 64;
-  if (b0 >= nb) return;
+  if (chunk * SCORED >= nb) return;
   const int id = block_id(c, s, b0 + lane, nb);
-  const int shift = __builtin_ctz(gp);
-  Queries<D, NT> raw;
-  load_queries<D, NT>([&](int y) -> const uint16_t* {
+  const int shift = __builtin_ctz(gp), columns = (i1 - i0) * gp;
+  auto query = [&](int y) -> const uint16_t* {
     const int x = 16 * y + (lane & 15), i = i0 + (x >> shift), h = x & (gp - 1);
     return i < i1 && h < G ? (const uint16_t*)a.q + (long)(row0 + i) * a.q_pitch + (long)(g * G + h) * D : nullptr;
-  }, raw);
+  };
+  Queries<D, 1> raw;
+  load_queries<D, 1>([&](int) { return query(NT > 1 ? wave : 0); }, raw);
   Scored<D> b;
-  load_blocks<D>(c, g, summary, scales, id, b);
+  load_blocks<D>(c, g, summary, scales, id, b);                        // of the pool's first page where there are no more blocks
   Codes<D, NT> q;
-  query_codes<DT, D, NT>(raw, (i1 - i0) * gp, q);
-  score_blocks<D, NT>(b, q, gp, (i1 - i0) * gp, [&](int y, int j, u32x4_t key) {
+  if constexpr (NT > 1) {
+    Codes<D, 1> own;
+    query_codes<DT, D, 1>(raw, 16, own);
+#pragma unroll
+    for (int k = 0; k < kSteps<D>; ++k) made[wave][k][lane] = own.q[0][k];
+    factors[wave][lane] = (f32x2_t){own.scale[0], own.bias[0]};
+    __syncthreads();
+    if (b0 >= nb) return;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (16 * n >= columns) break;
+#pragma unroll
+      for (int k = 0; k < kSteps<D>; ++k) q.q[n][k] = made[n][k][lane];
+      const f32x2_t f = factors[n][lane];
+      q.scale[n] = f[0];
+      q.bias[n] = f[1];
+    }
+  } else {
+    if (b0 >= nb) return;
+    query_codes<DT, D, 1>(raw, columns, q);
+  }
+  score_blocks<D, NT>(b, q, gp, columns, [&](int y, int j, u32x4_t key) {
     const int i = i0 + ((16 * y + (lane & 15)) >> shift);
     if (i < i1) *(u32x4_t*)(keys + ((long)(row0 + i) * c.H + g) * pitch + b0 + 16 * j + 4 * (lane >> 4)) = key;
   });
