@@ -477,3 +477,15 @@ def test_scales_of_any_nan_come_first_and_choose_no_more_than_top(heads, new, le
     np.testing.assert_array_equal(got.cpu().numpy()[:sum(new)], want[:sum(new)])
     assert bool((room[:256] == 77).all()) and bool((room[256 + b.T * top:] == 77).all())
     assert set(want[0, 0]) >= {0, *range(3, 3 + 2 * min(9, top - 2), 2)}
+
+
+@pytest.mark.parametrize("dtype,kept", KINDS)
+@pytest.mark.parametrize("D,heads,H,page,top,tree", [(128, 8, 4, 16, 9, False), (128, 8, 8, 32, 5, True), (96, 10, 5, 16, 6, False), (64, 16, 4, 16, 7, True), (128, 51, 3, 64, 3, False)])
+def test_many_rows(dtype, kept, D, heads, H, page, top, tree):
+    """More items than workgroups of eight waves are for: chunks of many rows beside single tokens and padding, positions that do not exist."""
+    rng = np.random.default_rng(D + heads + top)
+    new = [33, 1, 0, 13, 2]
+    b = Batch(rng, new, [333, 400, 20, 13, 1], page)
+    b.pages[0, 2], b.pages[1, 0] = -1, b.n_pages
+    bits = rng.integers(-2 ** 63, 2 ** 63, b.T, dtype=np.int64) if tree else None
+    run(b, heads, H, D, dtype, kept, top, seed=top, visible=bits)
