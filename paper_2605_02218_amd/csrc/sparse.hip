@@ -1396,7 +1396,8 @@ hipError_t launch_summary(const Paged& c, const void* kc, const float* ks, int8_
   return with_forms(c, [&](auto dt, auto kept, auto dim) {
     bool by_row;
     const long items = touched_pages(c, &by_row) * c.H;
-    const bool large = c.page_shift >= 8;
+    // pages of 128 as well where those that the sequences end in and fill are no more than the compute units (us of 256 items 6.8 and 5.9, over e4m3 8.7 and 8.0; of 320 8.7 and 9.8)
+    const bool large = c.page_shift >= 8 || (c.page_shift == 7 && std::min<long>(c.T, (c.T >> 7) + c.S) * c.H <= 256);
     auto go = [&](auto kernel, int per) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, stream, c, items, kc, ks, summary, scales);
       return hipGetLastError();

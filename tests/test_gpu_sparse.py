@@ -489,3 +489,26 @@ def test_many_rows(dtype, kept, D, heads, H, page, top, tree):
     b.pages[0, 2], b.pages[1, 0] = -1, b.n_pages
     bits = rng.integers(-2 ** 63, 2 ** 63, b.T, dtype=np.int64) if tree else None
     run(b, heads, H, D, dtype, kept, top, seed=top, visible=bits)
+
+
+@pytest.mark.parametrize("dtype,kept", KINDS)
+@pytest.mark.parametrize("D,H,new,length", [(64, 2, [1, 0, 5, 130], [129, 7, 4, 300]), (96, 3, [1], [128]), (128, 9, [1] * 40, [131 * s % 300 + 1 for s in range(40)])])
+def test_summaries_of_pages_of_128(dtype, kept, D, H, new, length):
+    """By workgroups where they are few, by waves beyond."""
+    import torch
+    import paper_2605_02218_amd as C
+    rng = np.random.default_rng(D)
+    b = Batch(rng, new, length, 128)
+    k, v, _, _ = make(rng, b, H, H, D, dtype, kept)
+    cache = b.params(H, D, dtype, kept)
+    summary = C.block_alloc(cache)
+    summary[0].fill_(7)
+    summary[1].fill_(1e30)
+    C.block_summary(cache, *b.device(), upload(k, v), summary)
+    codes, scale = summaries(b, k32_of(k), H, D)
+    touched = {int(b.pages[s][x // 128]) for s in range(b.S) for x in range(max(length[s] - new[s], 0), length[s])}
+    for page in range(b.n_pages):
+        if page not in touched:
+            codes[page], scale[page] = 7, 1e30
+    np.testing.assert_array_equal(summary[0].cpu().numpy(), codes)
+    np.testing.assert_array_equal(summary[1].cpu().numpy(), scale)
