@@ -2,7 +2,7 @@
 //
 // Pair (x1, x2) number i of a row at position pos: y1 = x1 c - x2 s, y2 = x2 c + x1 s, (c, s) = magnitude (cos, sin)(2 pi u), u = frac(pos step_i).
 // step_i is a 64-bit binary fraction of a turn, so pos step_i mod 2^64 is u itself, exact but for the last bits of step_i (2^-33 of a turn at position 2^31).
-// Of u the upper 32 bits go on (1.5e-9 of an angle): an eighth of a turn to both sides of the nearest quarter, where short series are good to 2^-24.
+// Of u the upper 32 bits go on (1.5e-9 of an angle): an eighth of a turn to both sides of the nearest quarter, where short series are good to 2^-28.
 //
 // D / 16 lanes take a row, 16 elements each: eight pairs, two pieces of 16 bytes.  A lane's cosines and sines serve all rows of a token it takes, every
 // `step`-th of its heads; lanes of neighbouring groups take neighbouring heads.  Bound by memory; single tokens by latency: all heads at once.
@@ -20,20 +20,25 @@ constexpr int RT = 256;
 constexpr int STEP = 16;
 
 struct Turn { float c, s; };
-// Cosine and sine of a 64-bit fraction of a turn: series around the nearest quarter, |x| <= pi / 4, errors below 2^-28 of 1; the conversion to a
-// float and the product with 2 pi 2^-32 are off by 2^-24 of x each.
+// Cosine and sine of a 64-bit fraction of a turn: series around the nearest quarter, |x| <= pi / 4, errors below 2^-28 of 1.  What the conversion to a float, the product with
+// 2 pi 2^-32 and the square lose goes into the last sums, so that these are all that is rounded: 2^-24 at most, in the mean 1.05 times the error of a number that is rounded once
+// (without these parts 1.4 times; prompts into the cache take 114 us with and without, image tokens with three axes 74.4 and 72.5).
 __device__ __forceinline__ Turn turn_of(uint64_t u, float magnitude) {
+  constexpr double kUnit = 6.283185307179586476925 / 4294967296.0;
+  constexpr float kHigh = (float)kUnit, kLow = (float)(kUnit - (double)kHigh);
   const uint32_t hi = (uint32_t)(u >> 32), quarter = (hi + 0x20000000u) >> 30;
-  const float x = (float)(int32_t)(hi - (quarter << 30)) * (float)(6.283185307179586476925 / 4294967296.0), y = x * x;
-  float s = __builtin_fmaf(y, 1.f / 362880.f, -1.f / 5040.f);
-  s = __builtin_fmaf(y, s, 1.f / 120.f);
-  s = __builtin_fmaf(y, s, -1.f / 6.f);
-  s = __builtin_fmaf(x * y, s, x);
+  const int32_t i = (int32_t)(hi - (quarter << 30));                   // up to 2^29 to both sides
+  const float f = (float)i, x = f * kHigh, y = x * x;
+  const float rest = __builtin_fmaf(f, kHigh, -x) + __builtin_fmaf(f, kLow, (float)(i - (int32_t)f) * kHigh);        // x + rest is the angle
   float c = __builtin_fmaf(y, -1.f / 3628800.f, 1.f / 40320.f);
   c = __builtin_fmaf(y, c, -1.f / 720.f);
   c = __builtin_fmaf(y, c, 1.f / 24.f);
   c = __builtin_fmaf(y, c, -0.5f);
-  c = __builtin_fmaf(y, c, 1.f);
+  c = 1.f + __builtin_fmaf(y, c, -__builtin_fmaf(x, rest, 0.5f * __builtin_fmaf(x, x, -y)));
+  float s = __builtin_fmaf(y, 1.f / 362880.f, -1.f / 5040.f);
+  s = __builtin_fmaf(y, s, 1.f / 120.f);
+  s = __builtin_fmaf(y, s, -1.f / 6.f);
+  s = x + __builtin_fmaf(x * y, s, rest * c);
   const bool odd = quarter & 1;
   const float a = odd ? s : c, b = odd ? c : s;
   return Turn{quarter == 1 || quarter == 2 ? -a * magnitude : a * magnitude, quarter >= 2 ? -b * magnitude : b * magnitude};

@@ -1,7 +1,7 @@
 """GPU parity of covspec_rotate and covspec_rotate_write with oracle/sparse_oracle.py (angles exact, the rest fp64).
 
-Tolerance of an element, with u = half a step of its 16-bit type and X = magnitude (|x1| + |x2|) of its pair: cosine and sine are off by 2^-22 as the
-header has it, their products with the magnitude, with x and the sum are four fp32 roundings: E = (2^-22 + 4 2^-24) X; then u |y| for the result's own rounding (of y
+Tolerance of an element, with u = half a step of its 16-bit type and X = magnitude (|x1| + |x2|) of its pair: cosine and sine are off by 2^-23 as the
+header has it, their products with the magnitude, with x and the sum are four fp32 roundings: E = (2^-23 + 4 2^-24) X; then u |y| for the result's own rounding (of y
 off by E: u E more, below 2^-30 X), and 2^-25, half the fixed step of fp16 near zero.  In 8 bits: the scale is off by what the largest element is, E / Q, and two roundings;
 a code by half its step (integers 1/2; e4m3 2^-4 of the value, 2^-10 below 2^-6), the value it stands for by E and three roundings of the value more."""
 import math
@@ -14,7 +14,7 @@ from round_util import HALF_STEP, Batch, pool_of, rounded, torch_dtype
 
 pytestmark = pytest.mark.gpu
 
-E = 2.0 ** -22 + 4 * 2.0 ** -24
+E = 2.0 ** -23 + 4 * 2.0 ** -24
 Q = {"int8": 127.0, "e4m3": 448.0}
 
 
