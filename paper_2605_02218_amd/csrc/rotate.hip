@@ -15,14 +15,15 @@ namespace covspec {
 namespace {
 
 constexpr int RT = 256;
-// Groups of lanes that share a token's heads, at most, where there are rows enough to fill the device.  us with 4, 8 and 16: 8 x 3008 tokens of 40 + 8 heads of 128 into a
-// 16-bit cache 129, 120, 114 (5.2 TB/s); 20480 tokens of 32 heads with three axes 75, 70.5, 72.5: fewer rows a lane even out better, more share its angles.
-constexpr int STEP = 16;
+// Rows of a lane, about, where there are rows enough to fill the device: its angles serve them all, and fewer rows even out better.  us with two, four and eight: 20480 tokens
+// of 32 heads with three axes 77.9, 73.4, 76.8; 8 x 3008 tokens of 32 + 8 heads of 128 into a 16-bit cache -, 118, 123; 16000 of 64 + 8 heads -, 128, 134; 24064 of 16 + 16 heads
+// of 64 39.4, 36.8, 36.2; of 8 + 1 heads with one row 22.1, with three 18.2.
+constexpr int EACH = 4;
 
 struct Turn { float c, s; };
 // Cosine and sine of a 64-bit fraction of a turn: series around the nearest quarter, |x| <= pi / 4, errors below 2^-28 of 1.  What the conversion to a float, the product with
 // 2 pi 2^-32 and the square lose goes into the last sums, so that these are all that is rounded: 2^-24 at most, in the mean 1.05 times the error of a number that is rounded once
-// (without these parts 1.4 times; prompts into the cache take 114 us with and without, image tokens with three axes 74.4 and 72.5).
+// (without these parts 1.4 times; prompts into the cache take 114 us with and without, image tokens with three axes 2 more).
 __device__ __forceinline__ Turn turn_of(uint64_t u, float magnitude) {
   constexpr double kUnit = 6.283185307179586476925 / 4294967296.0;
   constexpr float kHigh = (float)kUnit, kLow = (float)(kUnit - (double)kHigh);
@@ -194,7 +195,7 @@ hipError_t launch_dim(const Paged& c, Rotate r, hipStream_t stream) {
   constexpr int LANES = D == 64 ? 4 : 8;
   const int rows = (r.q ? r.heads : 0) + (r.k ? c.H : 0);
   r.step = rows;
-  while (r.step > STEP && (long)c.T * r.step * LANES > 256l * 2048) r.step = (r.step + 1) / 2;
+  while (r.step > (rows + EACH - 1) / EACH && (long)c.T * r.step * LANES > 256l * 2048) r.step = (r.step + 1) / 2;
   const unsigned grid = (unsigned)(((long)c.T * r.step * LANES + RT - 1) / RT);
   if (r.interleaved)
     hipLaunchKernelGGL((rotate_kernel<DT, KEPT, D, false>), dim3(grid), dim3(RT), 0, stream, c, r);
