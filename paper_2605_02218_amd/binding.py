@@ -888,7 +888,8 @@ def _launch(dev, name, *args):
 
 
 def _scratch(dev, workspace, size, p, name, *how):
-    """(address, bytes) of the caller's workspace, or of a new one."""
+    """(tensor, address, bytes) of the caller's workspace, or of a new one.  Hold the tensor until the library has been called: what is allocated after a tensor has
+    died may be its memory."""
     if workspace is None:
         n = size(p, *how)
         if n == 0:
@@ -896,7 +897,7 @@ def _scratch(dev, workspace, size, p, name, *how):
         workspace = _types()["torch"].empty(n + 256, dtype=_types()["u8"], device=dev)
     elif workspace.device != dev:
         raise ValueError("the workspace must be on %s" % dev)
-    return _ws_args(workspace)
+    return (workspace, *_ws_args(workspace))
 
 
 @dataclass
@@ -938,7 +939,7 @@ def pages_step(p: PagesParams, state, want, rows, workspace=None, want_slots=Tru
     pages, held, borrowed, free, n_free = state
     dev, types = _device_of(want), _types()
     i32, S, T = types["i32"], p.n_seq, p.n_tokens
-    wp, wb = _scratch(dev, workspace, pages_workspace_size, p, "covspec_pages_workspace_size")
+    workspace, wp, wb = _scratch(dev, workspace, pages_workspace_size, p, "covspec_pages_workspace_size")
     one, row = (S,), (T,)
     args = _given(dev, (want, "want", one, i32), (rows, "rows", one, i32), (pages, "pages", (S, p.max_pages), i32), (held, "held", one, i32), (borrowed, "borrowed", one, i32),
                   (free, "free_pages", (p.n_pages,), i32), (n_free, "n_free", (1,), i32))
@@ -1104,7 +1105,7 @@ def sparse_attend(p: SparseParams, q, start, length, pages, cache, summary, visi
         bp = blocks.data_ptr()
     bits = _given(dev, (visible, "visible", (T,), types["i64"]))[0] if visible is not None else None
     made = (None, None) if summary is None else _summary_args(dev, c, summary)
-    wp, wb = _scratch(dev, workspace, sparse_workspace_size, p, "covspec_sparse_workspace_size", given)
+    workspace, wp, wb = _scratch(dev, workspace, sparse_workspace_size, p, "covspec_sparse_workspace_size", given)
     lse = empty((T, a.n_heads), dtype=types["f32"], device=dev) if want_lse else None
     _launch(dev, "covspec_sparse_attend", ctypes.byref(p.c_struct(q_pitch, out_pitch, given)), qp, *batch, *pool, *made, bits, bp, op, None if lse is None else lse.data_ptr(), wp, wb)
     return out, lse, blocks
