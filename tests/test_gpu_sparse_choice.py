@@ -1,0 +1,57 @@
+"""The choice of pages where rows times key heads are many, which a launch with a wave for each of them makes (1024 and more, several rows a sequence), and beside it in its
+other forms: by a workgroup each, by the attention's own.  Lists are compared with oracle/sparse_oracle.py as they are, between marked words."""
+import numpy as np
+import pytest
+
+import test_gpu_sparse as TS
+from round_util import Batch
+
+pytestmark = pytest.mark.gpu
+
+PAGE, D = 16, 64
+
+
+def patterned(rng, b, H, kinds):
+    """Codes and scales of all pages, of `kinds` different ones, so that many tie."""
+    codes = rng.integers(-127, 128, (kinds, H, 2, D)).astype(np.int8)
+    codes.sort(axis=2)
+    codes = codes[:, :, ::-1]                               # the largest first
+    scale = rng.uniform(0.01, 0.05, (kinds, H)).astype(np.float32)
+    kind = rng.integers(0, kinds, b.n_pages)
+    return np.ascontiguousarray(codes[kind]), scale[kind]
+
+
+def check(rng, b, heads, H, codes, scale, top, first=1, recent=1, visible=None, rows=(), negate=False):
+    import torch
+    import paper_2605_02218_amd as C
+    k, v, q, q32 = TS.make(rng, b, heads, H, D, "bf16", "bf16")
+    if negate:                                              # every score has the sign of its page's codes
+        q, q32 = q.abs(), np.abs(q32)
+    cap = min(max(b.length), b.width * b.page)
+    p = C.SparseParams(C.AttendParams(b.params(H, D, "bf16", "bf16"), heads, cap, 0.125), top, first, recent)
+    room = torch.full((b.T * H * top + 4096,), 77, dtype=torch.int32, device="cuda")
+    blocks = room[2048:2048 + b.T * H * top].view(b.T, H, top)
+    vis = None if visible is None else torch.from_numpy(visible).cuda()
+    out, lse, got = C.sparse_attend(p, q.cuda(), *b.device(), TS.upload(k, v), (torch.from_numpy(codes).cuda(), torch.from_numpy(scale).cuda()), visible=vis, blocks_out=blocks,
+                                    want_lse=True)
+    torch.cuda.synchronize()
+    n = int(b.start[-1])
+    want = TS.wanted_blocks(b, codes, scale, q32, heads, H, top, first, recent, visible is not None, cap)
+    np.testing.assert_array_equal(got.cpu().numpy()[:n], want[:n])
+    assert bool((room[:2048] == 77).all()) and bool((room[2048 + n * H * top:] == 77).all())
+    TS.check_rows(b, want, heads, H, D, "bf16", "bf16", k[2], v[2], q32, out, lse, 0.125, visible, cap, set(rows))
+    return want
+
+
+@pytest.mark.parametrize("nb", [300, 500, 1500, 2000])
+@pytest.mark.parametrize("T,H", [(130, 8), (6, 2), (1, 1)])
+def test_more_nan_scales_than_places_beside_negative_scores(nb, T, H):
+    rng = np.random.default_rng(nb + T)
+    b = Batch(rng, [T], [PAGE * nb], PAGE, pad=2)
+    codes = np.full((b.n_pages, H, 2, D), 90, dtype=np.int8)
+    scale = np.full((b.n_pages, H), 0.02, dtype=np.float32)
+    scale[b.pages[0, rng.permutation(np.arange(1, nb - 12))[:100]]] = np.nan
+    low = int(np.flatnonzero(~np.isnan(scale[b.pages[0, 1:], 0]))[0]) + 1
+    codes[b.pages[0, low]] = -90
+    want = check(rng, b, 2 * H, H, codes, scale, 48, rows=[0, T - 1], negate=True)
+    assert np.isnan(scale[b.pages[0, want[0, 0, 1:47]], 0]).all()
