@@ -55,3 +55,30 @@ def test_more_nan_scales_than_places_beside_negative_scores(nb, T, H):
     codes[b.pages[0, low]] = -90
     want = check(rng, b, 2 * H, H, codes, scale, 48, rows=[0, T - 1], negate=True)
     assert np.isnan(scale[b.pages[0, want[0, 0, 1:47]], 0]).all()
+
+
+@pytest.mark.parametrize("nb", [9, 255, 256, 257, 1000, 2047, 2048])
+@pytest.mark.parametrize("top,first,recent", [(1, 0, 0), (7, 1, 2), (48, 0, 1), (300, 3, 3)])
+def test_many_rows_of_a_sequence(nb, top, first, recent):
+    """Up to the most blocks that a wave holds; pages that tie, some of no score, some that do not exist; lists longer than the sequence."""
+    rng = np.random.default_rng(nb + top)
+    b = Batch(rng, [130], [PAGE * nb], PAGE, pad=1)
+    H = 8
+    codes, scale = patterned(rng, b, H, 7)
+    scale[b.pages[0, nb // 2]], scale[b.pages[0, nb // 3]] = np.nan, 0.0
+    b.pages[0, nb // 4], b.pages[0, nb - 2] = -1, b.n_pages
+    check(rng, b, H, H, codes, scale, top, first, recent, rows=[0, 64, 129])
+
+
+@pytest.mark.parametrize("kinds", [1, 3, 10 ** 6])
+@pytest.mark.parametrize("heads,H", [(16, 16), (24, 8), (40, 4)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_many_rows_of_sequences_of_all_lengths(kinds, heads, H, tree):
+    rng = np.random.default_rng(kinds % 97 + heads)
+    scaled = 16 // H
+    new = [40 * scaled, 0, 65 * scaled, 1, 25 * scaled]
+    b = Batch(rng, new, [20000, 40, 16 * 1023 + 5, 1, 25 * scaled], PAGE, pad=3)
+    codes, scale = patterned(rng, b, H, min(kinds, b.n_pages))
+    b.pages[0, [3, 700]], b.pages[2, 11] = -5, 1 << 30
+    visible = rng.integers(-2 ** 63, 2 ** 63, b.T, dtype=np.int64) if tree else None
+    check(rng, b, heads, H, codes, scale, 20, 2, 2, visible=visible, rows=range(0, b.T, 29))
