@@ -585,10 +585,15 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, const See
 }
 
 // Keys of a lane's four blocks b .. b + 3 of nb as the choice takes them.  kAlways is left to the first and recent ones, so that no more than `top` are taken whatever lies there.
+// -0, a negative score below half of the smallest number, is +0 here, where there is one key for all heads of a group.
 __device__ __forceinline__ u32x4_t keys_of(const Sparse& sp, int nb, int b, u32x4_t scored) {
+  constexpr uint32_t kMinusZero = 0x7FFFFFFFu;
   u32x4_t k;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) k[e] = b + e >= nb ? kNone : b + e < sp.first || b + e >= nb - sp.recent ? kAlways : min(scored[e], kAlways - 1);
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t key = min(scored[e], kAlways - 1) + (scored[e] == kMinusZero ? 1u : 0u);
+    k[e] = b + e >= nb ? kNone : b + e < sp.first || b + e >= nb - sp.recent ? kAlways : key;
+  }
   return k;
 }
 // A row's scores of an earlier launch into LDS, four loads on their way at a time.

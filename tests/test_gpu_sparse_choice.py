@@ -21,11 +21,12 @@ def patterned(rng, b, H, kinds):
     return np.ascontiguousarray(codes[kind]), scale[kind]
 
 
-def check(rng, b, heads, H, codes, scale, top, first=1, recent=1, visible=None, rows=(), negate=False):
+def check(rng, b, heads, H, codes, scale, top, first=1, recent=1, visible=None, rows=(), positive=False, shrink=1.0):
     import torch
     import paper_2605_02218_amd as C
     k, v, q, q32 = TS.make(rng, b, heads, H, D, "bf16", "bf16")
-    if negate:                                              # every score has the sign of its page's codes
+    q, q32 = q * shrink, q32 * np.float32(shrink)           # a power of two
+    if positive:                                            # every score has the sign of its page's codes
         q, q32 = q.abs(), np.abs(q32)
     cap = min(max(b.length), b.width * b.page)
     p = C.SparseParams(C.AttendParams(b.params(H, D, "bf16", "bf16"), heads, cap, 0.125), top, first, recent)
@@ -53,7 +54,7 @@ def test_more_nan_scales_than_places_beside_negative_scores(nb, T, H):
     scale[b.pages[0, rng.permutation(np.arange(1, nb - 12))[:100]]] = np.nan
     low = int(np.flatnonzero(~np.isnan(scale[b.pages[0, 1:], 0]))[0]) + 1
     codes[b.pages[0, low]] = -90
-    want = check(rng, b, 2 * H, H, codes, scale, 48, rows=[0, T - 1], negate=True)
+    want = check(rng, b, 2 * H, H, codes, scale, 48, rows=[0, T - 1], positive=True)
     assert np.isnan(scale[b.pages[0, want[0, 0, 1:47]], 0]).all()
 
 
@@ -82,3 +83,25 @@ def test_many_rows_of_sequences_of_all_lengths(kinds, heads, H, tree):
     b.pages[0, [3, 700]], b.pages[2, 11] = -5, 1 << 30
     visible = rng.integers(-2 ** 63, 2 ** 63, b.T, dtype=np.int64) if tree else None
     check(rng, b, heads, H, codes, scale, 20, 2, 2, visible=visible, rows=range(0, b.T, 29))
+
+
+@pytest.mark.parametrize("nb", [250, 1500])
+@pytest.mark.parametrize("T,H", [(130, 8), (6, 2), (1, 1)])
+def test_scores_that_round_to_zero_tie_whatever_their_sign(nb, T, H):
+    """Below half of the smallest number a negative score is -0 and a positive one +0: equal, so the lower blocks are taken."""
+    rng = np.random.default_rng(nb + T)
+    b = Batch(rng, [T], [PAGE * nb], PAGE)
+    codes = np.full((b.n_pages, H, 2, D), 127, dtype=np.int8)
+    codes[b.pages[0, 1:nb:2]] = -127
+    scale = np.full((b.n_pages, H), 2.0 ** -95, dtype=np.float32)
+    want = check(rng, b, H, H, codes, scale, 12, rows=[0, T - 1], positive=True, shrink=2.0 ** -85)
+    assert want[0, 0, :11].tolist() == list(range(11))
+
+
+@pytest.mark.parametrize("nb", [250, 1500])
+@pytest.mark.parametrize("T,H", [(130, 8), (6, 2), (1, 1)])
+def test_scores_below_the_normal_numbers(nb, T, H):
+    rng = np.random.default_rng(nb + T)
+    b = Batch(rng, [T], [PAGE * nb], PAGE)
+    codes, scale = patterned(rng, b, H, 10 ** 4)
+    check(rng, b, 2 * H, H, codes, scale * np.float32(2.0 ** -60), 12, rows=[0, T - 1], shrink=2.0 ** -82)
