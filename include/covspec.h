@@ -601,7 +601,7 @@ int covspec_pages_step(const covspec_pages_params* p, const int32_t* want, const
  *   y1 = magnitude (x1 cos - x2 sin),  y2 = magnitude (x2 cos + x1 sin);  the other elements stay as they are.
  * f_i is given as steps[i], the part of a turn from one position to the next as a 64-bit binary fraction, so that pos * steps[i] mod 2^64 is the angle
  * of any position without a rounding.  Cosine and sine are off by at most 2^-23, products and sums are fp32, then one rounding to dtype.
- * Negative positions turn the other way: with positions negated the call undoes a rotation, and is its gradient.
+ * Negative positions turn the other way: with positions negated the call is a rotation's gradient, and with 1 / magnitude in magnitude's place as well it undoes it.
  *
  * covspec_rotary_steps (HOST) writes steps[rotary_dim / 2] from f_i = base^(-2i / rotary_dim) and a way to scale it for longer contexts:
  *   LINEAR  f / factor
