@@ -584,16 +584,13 @@ __device__ __forceinline__ int choose(const uint32_t* keys, int count, const See
   return ups + min(eqs, more);
 }
 
-// Keys of a lane's four blocks b .. b + 3 of nb as the choice takes them.  kAlways is left to the first and recent ones, so that no more than `top` are taken whatever lies there.
-// -0, a negative score below half of the smallest number, is +0 here, where there is one key for all heads of a group.
+// Keys of a lane's four blocks b .. b + 3 of nb as the choice takes them.  Those from +0 on go down by one: with that -0, a negative score below half of the smallest number, is
+// equal to +0, and kAlways is left to the first and recent ones, so that no more than `top` are taken whatever lies there.  (By a comparison with -0's key 2.5 us of 37 to 58
+// with groups of more than 16 heads of 128 over codes, where registers are short.)
 __device__ __forceinline__ u32x4_t keys_of(const Sparse& sp, int nb, int b, u32x4_t scored) {
-  constexpr uint32_t kMinusZero = 0x7FFFFFFFu;
   u32x4_t k;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t key = min(scored[e], kAlways - 1) + (scored[e] == kMinusZero ? 1u : 0u);
-    k[e] = b + e >= nb ? kNone : b + e < sp.first || b + e >= nb - sp.recent ? kAlways : key;
-  }
+  for (int e = 0; e < 4; ++e) k[e] = b + e >= nb ? kNone : b + e < sp.first || b + e >= nb - sp.recent ? kAlways : scored[e] - (scored[e] >> 31);
   return k;
 }
 // A row's scores of an earlier launch into LDS, four loads on their way at a time.
