@@ -73,7 +73,8 @@ __device__ __forceinline__ float over_rows(float x, F f) {
   return over_groups<16>(x, f);
 }
 
-// Bound by memory for prompts (8 x 3008 tokens of 8 heads of 128 in 16 bits 11.4 us, 4.3 TB/s), by latency for single tokens (64: 8 us, three loads one behind the other).
+// Bound by memory for prompts in 16 bits (8 x 3008 tokens of 8 heads of 128 11.4 us, 4.3 TB/s), by latency for those in 8 (11.8 us for half the bytes) and for single tokens (64 in
+// 16 bits 5.1 us, in 8 7.9): start and length, the page's number, its rows and the reduction, one behind the other.
 // A wave takes a page of a key head, or (WAVES = 4) a workgroup a large one: four waves on a page of 64 took 20 us instead of 11 for 256 single tokens.  BY_ROW: an item is a row, the first of its sequence's on the page does the work;
 // else items are the pages that each sequence's rows touch, one sequence behind the other.
 template <int DT, int KEPT, int D, int WAVES, bool BY_ROW>
@@ -637,7 +638,7 @@ __global__ __launch_bounds__(CHOOSERS) void choose_kernel(Paged c, int max_len, 
 }
 
 // A wave for each row and key head: for many rows of up to 2048 blocks, 32 keys in a lane.  The same steps with 256 parts; nobody waits for others (1024 rows of up to
-// 1500 blocks 8.3 us, by workgroups of four waves 9.7).
+// 1500 blocks 8.6 us, by workgroups of four waves 9.7).
 constexpr int ROW_BLOCKS = 2048;
 __global__ __launch_bounds__(256) void choose_rows_kernel(Paged c, int max_len, bool tree, Sparse sp, int pitch, const uint32_t* __restrict__ scores) {
   constexpr int TRIPS = ROW_BLOCKS / 256;
@@ -1245,7 +1246,7 @@ int slots_of(const Paged& c) { return c.kept == c.dtype && c.D > 64 ? 256 : 512;
 
 // Where the items would not fill half of the device their lists are cut, into up to 16 pieces of 256 positions or more.  us of a call in a graph, one token of 8 key heads over
 // bf16: 1536 positions in one piece 29.9, in six 24.7; 2048 in four 26.2, in eight 25.0; 4096 in eight 26.6, in 16 26.1; 8192 in 16 29.4, in 32 31.0.  1024 positions 26.7 and in
-// four pieces 24.5, but the launch that joins them takes the host 3 us: only tiles of 32 heads, in four waves, are cut there (34.1 and 28.3).
+// four pieces 24.5, but the launch that joins them takes the host 3 us, which calls from Python wait for: only tiles of 32 heads, in four waves, are cut there (34.1 and 28.3).
 struct Pieces { int pieces, span; };
 Pieces pieces_of(const Paged& c, int heads, int top) {
   const int G = heads / c.H, M = G <= 16 ? 16 : 32;
