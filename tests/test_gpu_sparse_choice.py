@@ -105,3 +105,14 @@ def test_scores_below_the_normal_numbers(nb, T, H):
     b = Batch(rng, [T], [PAGE * nb], PAGE)
     codes, scale = patterned(rng, b, H, 10 ** 4)
     check(rng, b, 2 * H, H, codes, scale * np.float32(2.0 ** -60), 12, rows=[0, T - 1], shrink=2.0 ** -82)
+
+
+@pytest.mark.parametrize("nb,T,H,top", [(32768, 2, 1, 1024), (32768, 1, 1, 1), (32767, 3, 1, 48), (2049, 130, 8, 48), (4200, 130, 8, 7)])
+def test_more_blocks_than_a_wave_holds(nb, T, H, top):
+    """By a workgroup each: up to the most blocks there can be, and many rows."""
+    rng = np.random.default_rng(nb + T)
+    b = Batch(rng, [T], [PAGE * nb], PAGE, pad=1)
+    codes, scale = patterned(rng, b, H, 5000)
+    scale[b.pages[0, nb // 2:nb // 2 + 60]] = np.nan
+    b.pages[0, [nb // 4, nb - 5]] = -1, b.n_pages
+    check(rng, b, H, H, codes, scale, top, min(top, 2) - 1, min(top, 2) - 1, rows=[0, T - 1])

@@ -9,7 +9,7 @@ from test_gpu_pages import Both
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("S,T", [(64, 5000), (1024, 4097), (1025, 3000), (1100, 20000), (2, 100)])
+@pytest.mark.parametrize("S,T", [(64, 5000), (1024, 4097), (1025, 3000), (1100, 20000), (2, 100), (65536, 300000)])
 def test_page_steps_equal_the_oracle(S, T):
     import torch
     import paper_2605_02218_amd as C
